@@ -368,6 +368,113 @@ int ems_decode_step(const ems_params* p, const ems_decode_state* state, int32_t 
                     float* attn_opt, int32_t* decision_opt, float* sim_opt,
                     void* ws, size_t ws_bytes, void* hip_stream);
 
+/*
+ * Attention of one new token over the compact cache: the output that goes with the weights of ems_decode_step's
+ * phase 1, for the layer to go on with.  Enqueue it before that token's ems_decode_step, which changes the state.
+ * The rows are the state's live table elements (key (tok_norm / row_norm[row]) * k_cache[row], value
+ * v_cache[row]; a row of norm 0 has key 0) and the new token itself; p_t = exp(scale q.key_t):
+ *     out = sum_t p_t value_t / sum_t p_t        lse = ln sum_t p_t
+ *   state        in : only k_cache, v_cache, row_norm, tok_row and tok_norm are read (the others may be NULL)
+ *   q_new        in : device [B, Hq, D] `dtype`;  k_new, v_new in: device [B, Hkv, D] `dtype`, 16-byte aligned
+ *   out          out: device [B, Hq, D] `dtype`, 16-byte aligned
+ *   lse_opt      out: device [B, Hq] f32, or NULL
+ *   ws           device scratch of at least ems_decode_attention_workspace_bytes
+ * Any Hq / Hkv.  Table elements whose row is outside [0, budget) are taken as free.
+ */
+int ems_decode_attention_workspace_bytes(const ems_params* p, size_t* attention_ws);
+int ems_decode_attention(const ems_params* p, const ems_decode_state* state,
+                         const void* q_new, const void* k_new, const void* v_new,
+                         void* out, float* lse_opt, void* ws, size_t ws_bytes, void* hip_stream);
+
+/*
+ * A paged cache of keys and values, for a generation whose cache grows: a pool of pages of `page_size` rows per
+ * kv-head, and for every sequence a table of its pages in order.  It may hold a layer's raw cache, or the
+ * expansion of a compressed one (ems_expand), whose evicted rows are masked head by head through `positions`.
+ *   k_pages, v_pages [num_pages, Hkv, page_size, D] `dtype`, 16-byte aligned
+ *   positions        [num_pages, Hkv, page_size] i32 position of every row, or NULL.  Rows with a negative one
+ *                    are masked: they take no part in the attention, whatever they hold (evicted rows of
+ *                    ems_expand have -1).
+ *   page_table       [B, max_pages] i32.  Row t of sequence b is row t % page_size of page
+ *                    page_table[b][t / page_size].  Sequences may share pages that nobody writes.
+ * The table and the lengths are device data and cannot be checked on the host: rows whose page is outside
+ * [0, num_pages) are neither written nor attended, lengths are clamped to [0, max_pages * page_size].
+ */
+typedef struct {
+    int32_t batch;         /* B >= 1 sequences */
+    int32_t q_heads;       /* Hq >= 1 */
+    int32_t kv_heads;      /* Hkv >= 1, divides Hq */
+    int32_t head_dim;      /* D in {64, 128} */
+    int32_t page_size;     /* rows of a page, >= 1, any */
+    int32_t num_pages;     /* pages of the pool, >= 1 (num_pages * Hkv * page_size < 2^31) */
+    int32_t max_pages;     /* columns of the table, >= 1 (max_pages * page_size <= 2^30) */
+    float   softmax_scale; /* <= 0 means 1/sqrt(D) */
+    int32_t dtype;         /* ems_dtype of keys, values, queries and the output */
+} ems_paged_params;
+
+typedef struct {
+    void* k_pages;
+    void* v_pages;
+    int32_t* positions;          /* or NULL */
+    const int32_t* page_table;
+} ems_paged_cache;
+
+/* Distances in elements between neighbours of a dimension; a row's D elements are adjacent. */
+typedef struct {
+    int64_t batch, head, token;
+} ems_strides;
+
+/*
+ * Appends up to n_new tokens to every sequence and applies the position rotation on the way.  Token i of
+ * sequence b goes to row start[b] + i of the sequence.  Its keys (and queries) are rotated: with inv_freq f
+ * [rot_dim / 2], pair e of the first rot_dim elements, (x[e], x[e + rot_dim/2]) or, interleaved,
+ * (x[2e], x[2e+1]), becomes
+ *     (x1 cos a - x2 sin a, x2 cos a + x1 sin a),   a = position * f[e]
+ * with the angle formed in 64 bits and one rounding to `dtype`; other elements, and values, are copied bit for bit.
+ *   n_new          tokens per sequence in k, v and q, >= 1
+ *   start          in : device [B] i32 rows the sequence holds already.  Tokens whose row falls outside the table
+ *                       are not stored.
+ *   new_len_opt    in : device [B] i32 how many of the n_new tokens there are (a padded batch), or NULL = all.
+ *                       What stands behind them is not read, the rows behind them are left as they are.
+ *   k, v           in : device [B, Hkv, n_new, D] with any strides (token-major projections, views)
+ *   positions_opt  in : device [B, Hkv, n_new] i32 with any strides (head stride 0: shared by the heads), or NULL:
+ *                       the position is the row, start[b] + i
+ *   inv_freq_opt   in : device [rot_dim / 2] f32; NULL iff rot_dim == 0 (no rotation)
+ *   rot_dim        multiple of 16, at most D
+ *   q_opt, q_out   device [B, Hq, n_new, D] with any strides: queries to rotate (by the positions of their
+ *                  kv-head), or both NULL.  q_out may be q itself (same strides); other overlaps are not allowed.
+ *   len_out_opt    out: device [B] i32 start[b] + its tokens, clamped to the table: the lengths for
+ *                       ems_paged_attention and the next call's `start`; it must not be `start` itself
+ * Writes the cache (its positions too, where it has them).  No workspace.  Two sequences that write the same page
+ * row race.
+ */
+int ems_paged_append(const ems_paged_params* p, const ems_paged_cache* cache, int32_t n_new,
+                     const int32_t* start, const int32_t* new_len_opt,
+                     const void* k, const ems_strides* k_strides,
+                     const void* v, const ems_strides* v_strides,
+                     const int32_t* positions_opt, const ems_strides* positions_strides,
+                     const float* inv_freq_opt, int32_t rot_dim, int32_t interleaved,
+                     const void* q_opt, const ems_strides* q_strides,
+                     void* q_out, const ems_strides* q_out_strides,
+                     int32_t* len_out_opt, void* hip_stream);
+
+/*
+ * Attention of one new token per sequence over its pages (the token's own key and value appended before):
+ * over the live rows t < lens[b] of the kv-head, with p_t = exp(scale q.k_t),
+ *     out = sum_t p_t v_t / sum_t p_t        lse = ln sum_t p_t
+ * A sequence-head without a live row (length 0, or every row masked) gives zeros and -inf.  What masked rows and
+ * rows behind the length hold does not matter; a NaN or an infinity in a live row gives what is not finite.
+ *   lens           in : device [B] i32 rows of every sequence
+ *   q              in : device [B, Hq, D] with any strides (batch, head; token is unused)
+ *   out            out: device [B, Hq, D] `dtype`, contiguous, 16-byte aligned
+ *   lse_opt        out: device [B, Hq] f32, or NULL
+ *   ws             device scratch of at least ems_paged_workspace_bytes
+ * The result depends on nothing but the arguments (no atomics); how the work is split depends on the lengths.
+ */
+int ems_paged_workspace_bytes(const ems_paged_params* p, size_t* attention_ws);
+int ems_paged_attention(const ems_paged_params* p, const ems_paged_cache* cache, const int32_t* lens,
+                        const void* q, const ems_strides* q_strides, void* out, float* lse_opt,
+                        void* ws, size_t ws_bytes, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

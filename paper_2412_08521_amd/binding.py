@@ -31,7 +31,9 @@ EXPORTS = ("ems_version", "ems_strerror", "ems_partition_sizes", "ems_workspace_
            "ems_global_local_score", "ems_attention_lse", "ems_global_local_score_from_lse",
            "ems_select", "ems_evict_merge", "ems_evict_merge_variant", "ems_evict_merge_static", "ems_expand",
            "ems_decode_workspace_bytes", "ems_decode_init", "ems_decode_step",
-           "ems_sparsity_rate", "ems_redundancy_rate")
+           "ems_sparsity_rate", "ems_redundancy_rate",
+           "ems_decode_attention_workspace_bytes", "ems_decode_attention",
+           "ems_paged_workspace_bytes", "ems_paged_append", "ems_paged_attention")
 
 
 class ems_params(C.Structure):
@@ -47,6 +49,19 @@ STATE_FIELDS = ("k_cache", "v_cache", "row_norm", "entry_count", "entry_tok", "t
 
 class ems_decode_state(C.Structure):
     _fields_ = [(name, C.c_void_p) for name in STATE_FIELDS]
+
+
+class ems_paged_params(C.Structure):
+    _fields_ = [(name, C.c_int32) for name in ("batch", "q_heads", "kv_heads", "head_dim", "page_size", "num_pages",
+                                               "max_pages")] + [("softmax_scale", C.c_float), ("dtype", C.c_int32)]
+
+
+class ems_paged_cache(C.Structure):
+    _fields_ = [(name, C.c_void_p) for name in ("k_pages", "v_pages", "positions", "page_table")]
+
+
+class ems_strides(C.Structure):
+    _fields_ = [(name, C.c_int64) for name in ("batch", "head", "token")]
 
 
 class EmsError(RuntimeError):
@@ -74,6 +89,27 @@ class EmsParams:
         return ems_params(self.batch, self.q_heads, self.kv_heads, self.head_dim, self.seq_len,
                           self.window, self.budget, self.merge_ratio, self.tau,
                           self.pool_kernel, self.softmax_scale, self.dtype)
+
+    @property
+    def torch_dtype(self):
+        return torch.float32 if self.dtype == EMS_F32 else torch.bfloat16
+
+
+@dataclass
+class PagedParams:
+    batch: int
+    q_heads: int
+    kv_heads: int
+    head_dim: int
+    page_size: int
+    num_pages: int
+    max_pages: int
+    softmax_scale: float = 0.0
+    dtype: int = EMS_BF16
+
+    def c(self) -> ems_paged_params:
+        return ems_paged_params(self.batch, self.q_heads, self.kv_heads, self.head_dim, self.page_size, self.num_pages,
+                                self.max_pages, self.softmax_scale, self.dtype)
 
     @property
     def torch_dtype(self):
@@ -110,6 +146,14 @@ def lib():
         l.ems_decode_workspace_bytes.argtypes = [P, C.POINTER(C.c_size_t)]
         l.ems_decode_init.argtypes = [P] + [C.c_void_p] * 7 + [S, C.c_void_p]
         l.ems_decode_step.argtypes = [P, S, C.c_int32] + [C.c_void_p] * 6 + [C.c_void_p, C.c_size_t, C.c_void_p]
+        l.ems_decode_attention_workspace_bytes.argtypes = [P, C.POINTER(C.c_size_t)]
+        l.ems_decode_attention.argtypes = [P, S] + [C.c_void_p] * 6 + [C.c_size_t, C.c_void_p]
+        PP, PC, ST = C.POINTER(ems_paged_params), C.POINTER(ems_paged_cache), C.POINTER(ems_strides)
+        l.ems_paged_workspace_bytes.argtypes = [PP, C.POINTER(C.c_size_t)]
+        l.ems_paged_append.argtypes = ([PP, PC, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, ST, C.c_void_p, ST,
+                                        C.c_void_p, ST, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, ST, C.c_void_p, ST,
+                                        C.c_void_p, C.c_void_p])
+        l.ems_paged_attention.argtypes = [PP, PC, C.c_void_p, C.c_void_p, ST] + [C.c_void_p] * 3 + [C.c_size_t, C.c_void_p]
         for name in EXPORTS[2:]:
             getattr(l, name).restype = C.c_int
         _lib = l
@@ -492,3 +536,183 @@ def ems_redundancy_rate(p: EmsParams, k, v):
     if rc != EMS_OK:
         raise EmsError(rc, "ems_redundancy_rate")
     return rate, best
+
+
+def _check_here(t, dtype, name, shape=None):
+    """A device tensor of the current device (the launch goes to it), of a shape where one is given."""
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name} must be a tensor of the current device")
+    if t.dtype != dtype or (shape is not None and t.shape != shape):
+        raise ValueError(f"{name}: expected {dtype} {shape if shape is None else tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+
+
+def _check_ws(ws, need, device):
+    if ws is None:
+        return torch.empty(max(need, 256), dtype=torch.uint8, device=device)
+    _check_here(ws, torch.uint8, "ws")
+    return ws
+
+
+def _check_dense(t, dtype, name, shape):
+    _check_here(t, dtype, name, shape)
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+
+
+def ems_decode_attention_workspace_bytes(p: EmsParams) -> int:
+    n = C.c_size_t(0)
+    cp = p.c()
+    rc = lib().ems_decode_attention_workspace_bytes(C.byref(cp), C.byref(n))
+    if rc != EMS_OK:
+        raise EmsError(rc, "ems_decode_attention_workspace_bytes")
+    return int(n.value)
+
+
+def ems_decode_attention(p: EmsParams, st: DecodeState, q_new, k_new, v_new, want_lse=False, ws=None, out=None):
+    """Attention of one new token over the compact cache and itself -> out [B,Hq,D] (or (out, lse [B,Hq] f32) with
+    want_lse).  Call it before the token's ems_decode_step.  `out`: (out, lse or None) to write to."""
+    heads, shape = (p.batch, p.q_heads), (p.batch, p.kv_heads, p.head_dim)
+    dt = p.torch_dtype
+    _check_dense(q_new, dt, "q_new", heads + (p.head_dim,))
+    _check_dense(k_new, dt, "k_new", shape)
+    _check_dense(v_new, dt, "v_new", shape)
+    n_imp, n_tbm = _partition_sizes(p.c())
+    _check_dense(st.k_cache, dt, "k_cache", (p.batch, p.kv_heads, p.budget + 1, p.head_dim))
+    _check_dense(st.tok_row, torch.int32, "tok_row", (p.batch, p.kv_heads, n_imp + n_tbm + p.window))
+    ws = _check_ws(ws, ems_decode_attention_workspace_bytes(p) if ws is None else 0, q_new.device)
+    o, lse = _attention_out(out, want_lse, heads, p.head_dim, dt, q_new.device)
+    cp, cs = p.c(), st.c()
+    rc = lib().ems_decode_attention(C.byref(cp), C.byref(cs), _ptr(q_new), _ptr(k_new), _ptr(v_new), _ptr(o), _ptr(lse),
+                                    _ptr(ws), ws.numel(), _stream())
+    if rc != EMS_OK:
+        raise EmsError(rc, "ems_decode_attention")
+    return (o, lse) if want_lse else o
+
+
+def _attention_out(out, want_lse, heads, head_dim, dtype, device):
+    if out is None:
+        return (torch.empty(heads + (head_dim,), dtype=dtype, device=device),
+                torch.empty(heads, dtype=torch.float32, device=device) if want_lse else None)
+    o, lse = out
+    _check_dense(o, dtype, "out", heads + (head_dim,))
+    if want_lse and lse is None:
+        raise ValueError("out: a tensor for the log-sum-exp is wanted")
+    if lse is not None:
+        _check_dense(lse, torch.float32, "lse", heads)
+    return o, lse if want_lse else None
+
+
+class PagedCache:
+    """Device tensors of a paged cache (see ems_paged_cache in include/ems.h): k_pages, v_pages
+    [num_pages, Hkv, page_size, D], page_table [B, max_pages] int32, and with `positions` [num_pages, Hkv, page_size]
+    int32 the position of every row, negative = masked."""
+
+    def __init__(self, p: PagedParams, k_pages, v_pages, page_table, positions=None):
+        rows = (p.num_pages, p.kv_heads, p.page_size)
+        _check_dense(k_pages, p.torch_dtype, "k_pages", rows + (p.head_dim,))
+        _check_dense(v_pages, p.torch_dtype, "v_pages", rows + (p.head_dim,))
+        _check_dense(page_table, torch.int32, "page_table", (p.batch, p.max_pages))
+        if positions is not None:
+            _check_dense(positions, torch.int32, "positions", rows)
+        self.k_pages, self.v_pages, self.page_table, self.positions = k_pages, v_pages, page_table, positions
+
+    def _check(self, p: PagedParams):
+        rows = self.k_pages.shape
+        if (p.num_pages, p.kv_heads, p.page_size, p.head_dim) != rows or (p.batch, p.max_pages) != self.page_table.shape \
+                or p.torch_dtype != self.k_pages.dtype:
+            raise ValueError(f"cache of {tuple(rows)} pages, {tuple(self.page_table.shape)} table does not fit {p}")
+
+    def c(self) -> ems_paged_cache:
+        return ems_paged_cache(_ptr(self.k_pages), _ptr(self.v_pages), _ptr(self.positions), _ptr(self.page_table))
+
+
+def alloc_paged_cache(p: PagedParams, page_table, positions: bool = False) -> PagedCache:
+    """A cache of `p.num_pages` pages for the sequences of `page_table`; with `positions` every row starts masked."""
+    rows = (p.num_pages, p.kv_heads, p.page_size)
+    dev = page_table.device
+    return PagedCache(p, torch.zeros(rows + (p.head_dim,), dtype=p.torch_dtype, device=dev),
+                      torch.zeros(rows + (p.head_dim,), dtype=p.torch_dtype, device=dev), page_table,
+                      torch.full(rows, -1, dtype=torch.int32, device=dev) if positions else None)
+
+
+def _rows(t, heads, n, p, name):
+    """[B, heads, n, D], or [B, heads, D] for one token, with any strides but the last -> its strides."""
+    shape = (p.batch, heads, n, p.head_dim) if t.dim() == 4 else (p.batch, heads, p.head_dim)
+    _check_here(t, p.torch_dtype, name, shape)
+    s = t.stride()
+    if s[-1] != 1:
+        raise ValueError(f"{name}: the elements of a row must be adjacent")
+    return ems_strides(s[0], s[1], s[2] if t.dim() == 4 else 0)
+
+
+def ems_paged_append(p: PagedParams, cache: PagedCache, start, k, v, positions=None, new_len=None, inv_freq=None,
+                     interleaved=False, q=None, q_out=None, len_out=None):
+    """Append k, v [B,Hkv,N,D] ([B,Hkv,D]: one token) from row start [B] int32 of every sequence on; keys and the
+    queries q [B,Hq,N,D] are rotated by inv_freq [rot/2] f32 at their positions ([B,N] or [B,Hkv,N] int32, default
+    the row).  new_len [B] int32: tokens there are of the N.  -> q_out (q's shape; pass q to rotate in place), None
+    without q.  len_out [B] int32 is written start + new tokens."""
+    cache._check(p)
+    n = k.shape[2] if k.dim() == 4 else 1
+    ks, vs = _rows(k, p.kv_heads, n, p, "k"), _rows(v, p.kv_heads, n, p, "v")
+    _check_dense(start, torch.int32, "start", (p.batch,))
+    if new_len is not None:
+        _check_dense(new_len, torch.int32, "new_len", (p.batch,))
+    if len_out is not None:
+        _check_dense(len_out, torch.int32, "len_out", (p.batch,))
+    ps = None
+    if positions is not None:
+        shared = positions.dim() == 2
+        _check_here(positions, torch.int32, "positions", (p.batch, n) if shared else (p.batch, p.kv_heads, n))
+        s = positions.stride()
+        ps = ems_strides(s[0], 0 if shared else s[1], s[-1])
+    rot = 0
+    if inv_freq is not None:
+        _check_dense(inv_freq, torch.float32, "inv_freq", (inv_freq.numel(),))
+        rot = 2 * inv_freq.numel()
+    qs = qos = None
+    if q is not None:
+        qs = _rows(q, p.q_heads, n, p, "q")
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        qos = _rows(q_out, p.q_heads, n, p, "q_out")
+        if q_out.dim() != q.dim() or any(m > 1 and step == 0 for m, step in zip(q_out.shape, q_out.stride())):
+            raise ValueError("q_out: a tensor of q's shape, every row in a place of its own")
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    cp, cc = p.c(), cache.c()
+    ref = lambda x: None if x is None else C.byref(x)  # noqa: E731
+    rc = lib().ems_paged_append(C.byref(cp), C.byref(cc), n, _ptr(start), _ptr(new_len), _ptr(k), C.byref(ks), _ptr(v),
+                                C.byref(vs), _ptr(positions), ref(ps), _ptr(inv_freq), rot, int(bool(interleaved)),
+                                _ptr(q), ref(qs), _ptr(q_out), ref(qos), _ptr(len_out), _stream())
+    if rc != EMS_OK:
+        raise EmsError(rc, "ems_paged_append")
+    return q_out
+
+
+def ems_paged_workspace_bytes(p: PagedParams) -> int:
+    n = C.c_size_t(0)
+    cp = p.c()
+    rc = lib().ems_paged_workspace_bytes(C.byref(cp), C.byref(n))
+    if rc != EMS_OK:
+        raise EmsError(rc, "ems_paged_workspace_bytes")
+    return int(n.value)
+
+
+def ems_paged_attention(p: PagedParams, cache: PagedCache, lens, q, want_lse=False, ws=None, out=None):
+    """Attention of one new token per sequence, q [B,Hq,D], over the first lens [B] int32 rows of its pages
+    -> out [B,Hq,D] (or (out, lse [B,Hq] f32) with want_lse).  `out`: (out, lse or None) to write to."""
+    heads = (p.batch, p.q_heads)
+    _check_here(q, p.torch_dtype, "q", heads + (p.head_dim,))
+    s = q.stride()
+    if s[2] != 1:
+        raise ValueError("q: the elements of a row must be adjacent")
+    _check_dense(lens, torch.int32, "lens", (p.batch,))
+    cache._check(p)
+    ws = _check_ws(ws, ems_paged_workspace_bytes(p) if ws is None else 0, q.device)
+    o, lse = _attention_out(out, want_lse, heads, p.head_dim, p.torch_dtype, q.device)
+    cp, cc, cs = p.c(), cache.c(), ems_strides(s[0], s[1], 0)
+    rc = lib().ems_paged_attention(C.byref(cp), C.byref(cc), _ptr(lens), _ptr(q), C.byref(cs), _ptr(o), _ptr(lse),
+                                   _ptr(ws), ws.numel(), _stream())
+    if rc != EMS_OK:
+        raise EmsError(rc, "ems_paged_attention")
+    return (o, lse) if want_lse else o

@@ -13,7 +13,8 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 OBJ_DIR = os.path.join(_HERE, "_build")
 LIB = os.path.join(_HERE, "libems_hip.so")
-SOURCES = ["ems_api.hip", "score.hip", "score_m16.hip", "score_f32.hip", "select.hip", "merge.hip", "decode.hip", "stats.hip"]
+SOURCES = ["ems_api.hip", "score.hip", "score_m16.hip", "score_f32.hip", "select.hip", "merge.hip", "decode.hip", "stats.hip",
+           "append.hip", "attend.hip"]
 HEADERS = ["ems_common.h", "ems_kernels.h", "ems_red_weights.h", "ems_rows.h", "ems_score.h", "ems_stream.h", os.path.join("..", "..", "include", "ems.h")]
 # the benchmark's ceiling measurements: a library of their own, outside the product's interface
 PROBE_DIR = os.path.join(_HERE, "bench_probe")

@@ -575,4 +575,177 @@ int ems_decode_step(const ems_params* p, const ems_decode_state* state, int32_t 
     return e == hipSuccess ? EMS_OK : EMS_ERR_LAUNCH;
 }
 
+// ---- attention of one new token, paged cache
+
+static float scale_log2e(float softmax_scale, int head_dim)
+{
+    const double scale = softmax_scale > 0.f ? (double)softmax_scale : 1.0 / std::sqrt((double)head_dim);
+    return (float)(scale * 1.4426950408889634074);
+}
+
+static bool aligned16(const void* p) { return ((uintptr_t)p % 16) == 0; }
+
+// rows of `dtype` that start at multiples of 16 bytes, whatever the index
+static bool wide_rows(const void* p, const ems_strides& s, bool f32)
+{
+    const int64_t per = f32 ? 4 : 8;
+    return aligned16(p) && s.batch % per == 0 && s.head % per == 0 && s.token % per == 0;
+}
+
+// Attention workspace: what the workers of a kv-head found of sequences that they share, two of them at most.
+struct AttendPlan { int workers; size_t off_ml, total; };
+
+static AttendPlan plan_attend(int batch, int kv_heads, int group, int head_dim, long long max_len)
+{
+    AttendPlan a{};
+    a.workers = ems::attend_workers(batch, kv_heads, group, max_len);
+    const int tiles = (group + ems::kAttendQ - 1) / ems::kAttendQ;
+    const size_t parts = (size_t)kv_heads * tiles * a.workers * 2 * ems::kAttendQ;
+    a.off_ml = align_up(sizeof(float) * parts * head_dim);
+    a.total = a.off_ml + align_up(sizeof(float) * parts * 2);
+    return a;
+}
+
+static int attend(ems::AttendArgs& a, const AttendPlan& plan, bool f32, void* ws, size_t ws_bytes, void* hip_stream)
+{
+    if (plan.total && !ws_ok(ws, ws_bytes, plan.total)) return EMS_ERR_WORKSPACE;
+    a.workers = plan.workers;
+    a.part_o = static_cast<float*>(ws);
+    a.part_ml = plan.total ? reinterpret_cast<float*>(static_cast<char*>(ws) + plan.off_ml) : nullptr;
+    const hipError_t e = ems::launch_attend(a, f32, static_cast<hipStream_t>(hip_stream));
+    return e == hipSuccess ? EMS_OK : EMS_ERR_LAUNCH;
+}
+
+static AttendPlan plan_decode_attention(const ems_params* p)
+{
+    int n_imp, n_tbm;
+    partition_sizes(p, &n_imp, &n_tbm);
+    return plan_attend(p->batch, p->kv_heads, p->q_heads / p->kv_heads, p->head_dim, (long long)n_imp + n_tbm + p->window + 1);
+}
+
+int ems_decode_attention_workspace_bytes(const ems_params* p, size_t* attention_ws)
+{
+    int why;
+    if (!full_params_ok(p, &why)) return why;
+    if (attention_ws) *attention_ws = plan_decode_attention(p).total;
+    return EMS_OK;
+}
+
+int ems_decode_attention(const ems_params* p, const ems_decode_state* state,
+                         const void* q_new, const void* k_new, const void* v_new,
+                         void* out, float* lse_opt, void* ws, size_t ws_bytes, void* hip_stream)
+{
+    int why;
+    if (!full_params_ok(p, &why)) return why;
+    if (!state || !state->k_cache || !state->v_cache || !state->row_norm || !state->tok_row || !state->tok_norm) return EMS_ERR_INVALID_ARG;
+    if (!q_new || !k_new || !v_new || !out) return EMS_ERR_INVALID_ARG;
+    if (!aligned16(state->k_cache) || !aligned16(state->v_cache) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(out))
+        return EMS_ERR_INVALID_ARG;
+    int n_imp, n_tbm;
+    partition_sizes(p, &n_imp, &n_tbm);
+    ems::AttendArgs a{};
+    a.q = q_new; a.q_sh = p->head_dim; a.q_sb = (long long)p->q_heads * p->head_dim; a.q_wide = aligned16(q_new);
+    a.k = state->k_cache; a.v = state->v_cache; a.out = out; a.lse = lse_opt;
+    a.tok_row = state->tok_row; a.tok_norm = state->tok_norm; a.row_norm = state->row_norm;
+    a.k_new = k_new; a.v_new = v_new; a.n_tok = n_imp + n_tbm + p->window; a.budget = p->budget;
+    a.batch = p->batch; a.kv_heads = p->kv_heads; a.group = p->q_heads / p->kv_heads; a.head_dim = p->head_dim;
+    a.scale_log2e = scale_log2e(p->softmax_scale, p->head_dim);
+    return attend(a, plan_decode_attention(p), p->dtype == EMS_F32, ws, ws_bytes, hip_stream);
+}
+
+static bool paged_params_ok(const ems_paged_params* p, int* why)
+{
+    *why = EMS_ERR_INVALID_ARG;
+    if (!p) return false;
+    if (p->batch < 1 || p->q_heads < 1 || p->kv_heads < 1 || p->head_dim < 1) return false;
+    if (p->q_heads % p->kv_heads) return false;
+    if (p->page_size < 1 || p->num_pages < 1 || p->max_pages < 1) return false;
+    if (p->dtype != EMS_BF16 && p->dtype != EMS_F32) return false;
+    if (std::isnan(p->softmax_scale) || std::isinf(p->softmax_scale)) return false;
+    *why = EMS_ERR_UNSUPPORTED;
+    if (p->head_dim != 64 && p->head_dim != 128) return false;
+    if ((long long)p->max_pages * p->page_size > (1ll << 30)) return false;
+    if ((long long)p->num_pages * p->page_size > 0x7fffffffll / p->kv_heads) return false;     // 32-bit row numbers
+    if ((long long)p->batch * p->q_heads > (1 << 24)) return false;                            // grid of the attention
+    return true;
+}
+
+static bool paged_cache_ok(const ems_paged_cache* c)
+{
+    return c && c->k_pages && c->v_pages && c->page_table && aligned16(c->k_pages) && aligned16(c->v_pages);
+}
+
+int ems_paged_append(const ems_paged_params* p, const ems_paged_cache* cache, int32_t n_new,
+                     const int32_t* start, const int32_t* new_len_opt,
+                     const void* k, const ems_strides* k_strides,
+                     const void* v, const ems_strides* v_strides,
+                     const int32_t* positions_opt, const ems_strides* positions_strides,
+                     const float* inv_freq_opt, int32_t rot_dim, int32_t interleaved,
+                     const void* q_opt, const ems_strides* q_strides,
+                     void* q_out, const ems_strides* q_out_strides,
+                     int32_t* len_out_opt, void* hip_stream)
+{
+    int why;
+    if (!paged_params_ok(p, &why)) return why;
+    if (!paged_cache_ok(cache) || n_new < 1 || !start || !k || !k_strides || !v || !v_strides) return EMS_ERR_INVALID_ARG;
+    if (positions_opt && !positions_strides) return EMS_ERR_INVALID_ARG;
+    if (rot_dim < 0 || rot_dim > p->head_dim || (rot_dim > 0) != (inv_freq_opt != nullptr)) return EMS_ERR_INVALID_ARG;
+    if ((q_opt != nullptr) != (q_out != nullptr) || (q_opt && (!q_strides || !q_out_strides))) return EMS_ERR_INVALID_ARG;
+    if (len_out_opt && len_out_opt == start) return EMS_ERR_INVALID_ARG;
+    if (rot_dim % 16) return EMS_ERR_UNSUPPORTED;
+    if ((long long)p->batch * n_new > 0x7fffffffll / (p->q_heads + 2 * p->kv_heads)) return EMS_ERR_UNSUPPORTED;
+    const bool f32 = p->dtype == EMS_F32;
+    ems::AppendArgs a{};
+    a.k = k; a.k_sb = k_strides->batch; a.k_sh = k_strides->head; a.k_sn = k_strides->token; a.k_wide = wide_rows(k, *k_strides, f32);
+    a.v = v; a.v_sb = v_strides->batch; a.v_sh = v_strides->head; a.v_sn = v_strides->token; a.v_wide = wide_rows(v, *v_strides, f32);
+    if (q_opt) {
+        a.q = q_opt; a.q_sb = q_strides->batch; a.q_sh = q_strides->head; a.q_sn = q_strides->token;
+        a.q_wide = wide_rows(q_opt, *q_strides, f32);
+        a.q_out = q_out; a.qo_sb = q_out_strides->batch; a.qo_sh = q_out_strides->head; a.qo_sn = q_out_strides->token;
+        a.qo_wide = wide_rows(q_out, *q_out_strides, f32);
+        a.q_heads_used = p->q_heads;
+    }
+    a.positions = positions_opt;
+    if (positions_opt) { a.pos_sb = positions_strides->batch; a.pos_sh = positions_strides->head; a.pos_sn = positions_strides->token; }
+    a.start = start; a.new_len = new_len_opt; a.inv_freq = inv_freq_opt; a.len_out = len_out_opt;
+    a.k_pages = cache->k_pages; a.v_pages = cache->v_pages; a.pos_pages = cache->positions; a.page_table = cache->page_table;
+    a.batch = p->batch; a.n_new = n_new; a.kv_heads = p->kv_heads; a.group = p->q_heads / p->kv_heads;
+    a.page_size = p->page_size; a.num_pages = p->num_pages; a.max_pages = p->max_pages; a.rot = rot_dim;
+    a.interleaved = interleaved != 0;
+    const hipError_t e = ems::launch_append(a, p->head_dim, f32, static_cast<hipStream_t>(hip_stream));
+    return e == hipSuccess ? EMS_OK : EMS_ERR_LAUNCH;
+}
+
+static AttendPlan plan_paged(const ems_paged_params* p)
+{
+    return plan_attend(p->batch, p->kv_heads, p->q_heads / p->kv_heads, p->head_dim, (long long)p->max_pages * p->page_size);
+}
+
+int ems_paged_workspace_bytes(const ems_paged_params* p, size_t* attention_ws)
+{
+    int why;
+    if (!paged_params_ok(p, &why)) return why;
+    if (attention_ws) *attention_ws = plan_paged(p).total;
+    return EMS_OK;
+}
+
+int ems_paged_attention(const ems_paged_params* p, const ems_paged_cache* cache, const int32_t* lens,
+                        const void* q, const ems_strides* q_strides, void* out, float* lse_opt,
+                        void* ws, size_t ws_bytes, void* hip_stream)
+{
+    int why;
+    if (!paged_params_ok(p, &why)) return why;
+    if (!paged_cache_ok(cache) || !lens || !q || !q_strides || !out || !aligned16(out)) return EMS_ERR_INVALID_ARG;
+    const bool f32 = p->dtype == EMS_F32;
+    ems::AttendArgs a{};
+    a.q = q; a.q_sb = q_strides->batch; a.q_sh = q_strides->head;
+    a.q_wide = wide_rows(q, ems_strides{q_strides->batch, q_strides->head, 0}, f32);
+    a.k = cache->k_pages; a.v = cache->v_pages; a.out = out; a.lse = lse_opt;
+    a.page_table = cache->page_table; a.lens = lens; a.pos_pages = cache->positions;
+    a.max_pages = p->max_pages; a.page_size = p->page_size; a.num_pages = p->num_pages;
+    a.batch = p->batch; a.kv_heads = p->kv_heads; a.group = p->q_heads / p->kv_heads; a.head_dim = p->head_dim;
+    a.scale_log2e = scale_log2e(p->softmax_scale, p->head_dim);
+    return attend(a, plan_paged(p), f32, ws, ws_bytes, hip_stream);
+}
+
 }  // extern "C"

@@ -161,6 +161,58 @@ struct StatsArgs {
     float zeta, tau;
 };
 
+// Strides (batch, head, token) in elements; *_wide: rows start at multiples of 16 bytes.
+struct AppendArgs {
+    const void* k;
+    const void* v;
+    const void* q;              // null: no queries
+    void* q_out;
+    long long k_sb, k_sh, k_sn, v_sb, v_sh, v_sn, q_sb, q_sh, q_sn, qo_sb, qo_sh, qo_sn, pos_sb, pos_sh, pos_sn;
+    const int32_t* start;       // [batch]
+    const int32_t* new_len;     // [batch] or null: all n_new
+    const int32_t* positions;   // null: the slot
+    const float* inv_freq;      // [rot / 2]
+    int32_t* len_out;           // [batch] or null
+    void* k_pages;              // [num_pages, kv_heads, page_size, D]
+    void* v_pages;
+    int32_t* pos_pages;         // [num_pages, kv_heads, page_size] or null
+    const int32_t* page_table;  // [batch, max_pages]
+    int batch, n_new, kv_heads, group, page_size, num_pages, max_pages, rot;
+    int q_heads_used;           // q heads, 0 without queries
+    bool interleaved, k_wide, v_wide, q_wide, qo_wide;
+};
+
+// Attention of one new token per sequence.  Rows are those of a paged cache (page_table), or of a compact cache whose
+// table elements name them (tok_row; one element more is the new token itself).
+struct AttendArgs {
+    const void* q;              // [batch, kv_heads * group, D] with strides q_sb, q_sh in elements
+    long long q_sb, q_sh;
+    const void* k;              // first row of the cache
+    const void* v;
+    void* out;                  // [batch, kv_heads * group, D]
+    float* lse;                 // [batch, kv_heads * group] or null
+    const int32_t* page_table;  // [batch, max_pages]
+    const int32_t* lens;        // [batch]
+    const int32_t* pos_pages;   // [num_pages, kv_heads, page_size] or null; < 0: masked
+    int max_pages, page_size, num_pages;
+    const int32_t* tok_row;     // [batch * kv_heads, n_tok]
+    const float* tok_norm;
+    const float* row_norm;      // [batch * kv_heads, budget]
+    const void* k_new;          // [batch * kv_heads, D]
+    const void* v_new;
+    int n_tok, budget;
+    int batch, kv_heads, group, head_dim;
+    int workers;                // per kv-head and tile of q-heads: they share its sequences evenly; 0 = a block per sequence
+    bool q_wide;                // q rows start at multiples of 16 bytes
+    float scale_log2e;
+    float* part_o;              // [kv_heads * tiles, workers, 2, 16, D] what a worker found of a sequence it shares (workspace)
+    float* part_ml;             // [.., 16, 2] its maximum and sum
+};
+constexpr int kAttendQ = 16;    // q-heads of a group that a block takes: the columns of a matrix product
+int attend_workers(int batch, int kv_heads, int group, long long max_len);      // AttendArgs::workers
+hipError_t launch_append(const AppendArgs& a, int head_dim, bool f32, hipStream_t st);
+hipError_t launch_attend(const AttendArgs& a, bool f32, hipStream_t st);
+
 int score_keys_per_block(int dtype_is_f32);
 // How the score passes of a launch are dealt: waves per head and stages per wave of each pass (0 waves:
 // the pass takes whole items), and the floats of one partial-result array.

@@ -1,0 +1,458 @@
+"""GPU parity of the paged cache (ems_paged_append, ems_paged_attention) with plain 64-bit forms."""
+import math
+import sys
+
+import pytest
+import torch
+
+from paged_ref import assert_within, attention, gather, half_step, pages_of, rotated
+from paper_2412_08521_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+BF16, F32 = B.EMS_BF16, B.EMS_F32
+
+
+def _log(*a):
+    print("[case]", *a, file=sys.stderr, flush=True)
+
+
+def _freq(rot, base=10000.0):
+    return (base ** (-torch.arange(0, rot, 2, dtype=torch.float64) / rot)).float() if rot else None
+
+
+# ---- append
+
+def _append_case(b, hq, hkv, d, ps, n, start, rot, mode, layout="packed", interleaved=False, with_q=True, new_len=None,
+                 positions=None, store=True, seed=0):
+    """One append checked whole: written rows, rows left as they were, positions, queries, lengths."""
+    dt = torch.float32 if mode == F32 else torch.bfloat16
+    gen = torch.Generator().manual_seed(seed)
+    lens = [min(n, max(0, m)) for m in (new_len or [n] * b)]
+    total = [s + m for s, m in zip(start, lens)]
+    columns = max(-(-(s + n) // ps) for s in start)
+    pool = sum(-(-t // ps) for t in total) + 3
+    table = pages_of(total, ps, pool, columns, gen)
+    p = B.PagedParams(b, hq, hkv, d, ps, pool, columns, dtype=mode)
+    kp, vp = (torch.randn((pool, hkv, ps, d), generator=gen).to(dt) for _ in range(2))
+    pp = torch.randint(-5, 100, (pool, hkv, ps), generator=gen, dtype=torch.int32) if store else None
+    nq = hq if with_q else 0
+    if layout == "packed":
+        x = torch.randn((b, n, nq + 2 * hkv, d), generator=gen).to(dt)
+        x_dev = x.cuda()
+        cut = lambda y: [y[:, :, i:j].transpose(1, 2) for i, j in ((0, nq), (nq, nq + hkv), (nq + hkv, nq + 2 * hkv))]  # noqa: E731
+        (q, k, v), (qd, kd, vd) = cut(x), cut(x_dev)
+    elif layout == "odd":                                   # rows one element apart from their neighbours, base off by one
+        wide = torch.randn((b * (nq + 2 * hkv) * n * (d + 1) + 1,), generator=gen).to(dt)
+        cut = lambda y: list(y[1:].view(b, nq + 2 * hkv, n, d + 1)[..., :d].split([nq, hkv, hkv], 1))  # noqa: E731
+        (q, k, v), (qd, kd, vd) = cut(wide), cut(wide.cuda())
+    else:
+        q, k, v = (torch.randn((b, m, n, d), generator=gen).to(dt) for m in (nq, hkv, hkv))
+        qd, kd, vd = q.cuda(), k.cuda(), v.cuda()
+    freq = _freq(rot)
+    cache = B.PagedCache(p, kp.cuda(), vp.cuda(), table.cuda(), positions=pp.cuda() if store else None)
+    int32 = lambda y: torch.tensor(y, dtype=torch.int32).cuda()  # noqa: E731
+    q_out = torch.full((b, hq, n, d), 7.0, dtype=dt).cuda() if with_q else None
+    len_out = torch.full((b,), -9, dtype=torch.int32).cuda()
+    got_q = B.ems_paged_append(p, cache, int32(start), kd, vd, positions=positions.cuda() if positions is not None else None,
+                               new_len=int32(new_len) if new_len else None, inv_freq=freq.cuda() if rot else None,
+                               interleaved=interleaved, q=qd if with_q else None, q_out=q_out, len_out=len_out)
+    torch.cuda.synchronize()
+    assert got_q is q_out
+    rk, rv, rp = kp.double(), vp.clone(), pp.clone() if store else None
+    bk = torch.zeros_like(rk)
+    rq = torch.full((b, hq, n, d), 7.0, dtype=torch.float64) if with_q else None
+    bq = torch.zeros_like(rq) if with_q else None
+    for i in range(b):
+        m = lens[i]
+        for h in range(hkv):
+            slot = torch.arange(start[i], start[i] + m)
+            pos = slot if positions is None else positions[i, :m] if positions.dim() == 2 else positions[i, h, :m]
+            page, at = table[i].long()[slot // ps], slot % ps
+            y, slack = rotated(k[i, h, :m], pos, freq, interleaved)
+            rk[page, h, at] = y
+            if rot:
+                bk[page, h, at, :rot] = (y.abs() * half_step(dt) + slack)[:, :rot]
+            rv[page, h, at] = v[i, h, :m]
+            if store:
+                rp[page, h, at] = pos.to(torch.int32)
+            for j in range(h * (hq // hkv), (h + 1) * (hq // hkv)) if with_q else ():
+                y, slack = rotated(q[i, j, :m], pos, freq, interleaved)
+                rq[i, j, :m] = y
+                if rot:
+                    bq[i, j, :m, :rot] = (y.abs() * half_step(dt) + slack)[:, :rot]
+    assert_within(cache.k_pages, rk, bk, "keys")            # bound 0 where nothing is rotated or written
+    assert torch.equal(cache.v_pages.cpu(), rv)
+    if store:
+        assert torch.equal(cache.positions.cpu(), rp)
+    if with_q:
+        assert_within(q_out, rq, bq, "queries")
+    assert len_out.tolist() == total
+
+
+@pytest.mark.parametrize("mode", [BF16, F32])
+@pytest.mark.parametrize("case", [
+    dict(b=1, hq=4, hkv=2, d=128, ps=16, n=1, start=[0], rot=128),
+    dict(b=3, hq=6, hkv=2, d=64, ps=16, n=1, start=[15, 16, 33], rot=64, interleaved=True),
+    dict(b=2, hq=8, hkv=8, d=128, ps=1, n=37, start=[0, 5], rot=64),
+    dict(b=5, hq=7, hkv=1, d=64, ps=24, n=131, start=[0, 23, 24, 1, 100], rot=32, new_len=[131, 0, 1, 77, 130]),
+    dict(b=2, hq=3, hkv=3, d=128, ps=100, n=65, start=[99, 0], rot=16, interleaved=True, layout="odd"),
+    dict(b=2, hq=2, hkv=1, d=64, ps=7, n=20, start=[3, 4], rot=64, layout="odd"),
+    dict(b=2, hq=4, hkv=4, d=128, ps=32, n=50, start=[7, 8], rot=0, layout="heads", with_q=False),
+    dict(b=2, hq=4, hkv=4, d=64, ps=32, n=50, start=[7, 8], rot=0, layout="packed", store=False),
+    dict(b=1, hq=32, hkv=8, d=128, ps=16, n=300, start=[1000], rot=128, new_len=[500]),
+    dict(b=1, hq=32, hkv=8, d=128, ps=16, n=9, start=[16], rot=128, new_len=[-3]),
+])
+def test_append_matches_64_bits(case, mode):
+    _log("append", case, mode)
+    _append_case(**case, mode=mode)
+
+
+@pytest.mark.parametrize("mode", [BF16, F32])
+@pytest.mark.parametrize("far", [0, 131072, 1 << 24, (1 << 31) - 64])
+def test_append_positions_far_and_per_head(far, mode):
+    """Angles of far positions, and positions of their own for every head, negative (masked) ones among them."""
+    _log("append far", far, mode)
+    gen = torch.Generator().manual_seed(1)
+    shared = torch.arange(2 * 21, dtype=torch.int32).view(2, 21) + far
+    _append_case(2, 4, 2, 128, 16, 21, [3, 40], 128, mode, positions=shared)
+    each = torch.randint(-1, 50, (2, 2, 21), generator=gen, dtype=torch.int32)
+    each = torch.where(each >= 0, each + far - 50 * (far > 0), each)
+    _append_case(2, 4, 2, 64, 16, 21, [3, 40], 32, mode, positions=each, interleaved=far == 131072)
+    _append_case(2, 4, 2, 64, 16, 21, [0, 0], 0, mode, positions=each, layout="heads", with_q=False)
+
+
+def test_append_of_one_token_without_a_token_dimension_and_in_place():
+    gen = torch.Generator().manual_seed(2)
+    p = B.PagedParams(2, 4, 2, 128, 16, 6, 3)
+    mk = lambda h: torch.randn((2, h, 128), generator=gen).bfloat16().cuda()  # noqa: E731
+    q, k, v = mk(4), mk(2), mk(2)
+    table = torch.tensor([[4, 1, 0], [2, 5, 3]], dtype=torch.int32).cuda()
+    start = torch.tensor([17, 31], dtype=torch.int32).cuda()
+    freq = _freq(128).cuda()
+    a, b = (B.alloc_paged_cache(p, table, positions=True) for _ in range(2))
+    q1 = B.ems_paged_append(p, a, start, k, v, inv_freq=freq, q=q)
+    q4 = B.ems_paged_append(p, b, start, k[:, :, None], v[:, :, None], inv_freq=freq, q=q[:, :, None])
+    assert q1.shape == q.shape and torch.equal(q1, q4[:, :, 0])
+    for x in ("k_pages", "v_pages", "positions"):
+        assert torch.equal(getattr(a, x), getattr(b, x))
+    assert (a.positions >= 0).sum() == 4 and a.positions[1, 0, 1] == 17 and a.positions[5, 1, 15] == 31
+    wide = torch.zeros((2, 6, 128), dtype=torch.bfloat16).cuda()
+    wide[:, :4] = q
+    mine = wide[:, :4]
+    assert B.ems_paged_append(p, a, start, k, v, inv_freq=freq, q=mine, q_out=mine) is mine
+    assert torch.equal(mine, q1) and not wide[:, 4:].any()
+
+
+def test_append_drops_tokens_without_a_place():
+    """Rows before the first and behind the last, pages that do not exist: nothing is written, queries are still turned."""
+    gen = torch.Generator().manual_seed(3)
+    p = B.PagedParams(3, 2, 1, 64, 8, 5, 2)
+    k, v, q = (torch.randn((3, h, 6, 64), generator=gen).bfloat16().cuda() for h in (1, 1, 2))
+    table = torch.tensor([[0, 1], [2, -1], [5, 3]], dtype=torch.int32).cuda()
+    start = torch.tensor([13, 5, -4], dtype=torch.int32).cuda()
+    cache = B.alloc_paged_cache(p, table)
+    pos = torch.arange(6, dtype=torch.int32).expand(3, 6).contiguous().cuda()
+    len_out = torch.zeros(3, dtype=torch.int32).cuda()
+    got = B.ems_paged_append(p, cache, start, k, v, positions=pos, inv_freq=_freq(64).cuda(), q=q, len_out=len_out)
+    want = torch.zeros((5, 1, 8, 64), dtype=torch.bfloat16)
+    want[1, 0, 5:8] = v[0, 0, :3].cpu()
+    want[2, 0, 5:8] = v[1, 0, :3].cpu()               # the rest of the second lies on page -1, all of the third before 0 or on page 5
+    assert torch.equal(cache.v_pages.cpu(), want)
+    assert ((cache.k_pages != 0).any(-1) == (cache.v_pages != 0).any(-1)).all()
+    assert len_out.tolist() == [16, 11, 2]
+    y, slack = rotated(q.cpu(), pos[:, None].cpu(), _freq(64), False)
+    assert_within(got, y, y.abs() * half_step(torch.bfloat16) + slack, "queries")
+
+
+def test_append_copies_values_bit_for_bit():
+    bits = torch.arange(0, 1 << 16, dtype=torch.int32).to(torch.int16).view(1, 4, 128, 128)      # every pattern, NaNs too
+    v = bits.view(torch.bfloat16).cuda()
+    p = B.PagedParams(1, 4, 4, 128, 16, 9, 9)
+    cache = B.alloc_paged_cache(p, torch.arange(8, -1, -1, dtype=torch.int32)[None].contiguous().cuda())
+    B.ems_paged_append(p, cache, torch.tensor([5], dtype=torch.int32).cuda(), v, v, inv_freq=None)
+    for pages in (cache.k_pages, cache.v_pages):
+        rows = pages.flip(0).transpose(0, 1).reshape(4, 144, 128)[:, 5:133]
+        assert torch.equal(rows.view(torch.int16).cpu(), bits[0])
+
+
+# ---- attention
+
+def _attend_case(b, hq, hkv, d, ps, lens, mode, masked=None, columns=None, layout="dense", scale=0.0, seed=0, poison=True):
+    """masked: share of the rows that are masked (None: a cache without positions).  poison: rows that take no part
+    (behind the length, masked, on pages of nobody) hold NaN and infinities."""
+    dt = torch.float32 if mode == F32 else torch.bfloat16
+    gen = torch.Generator().manual_seed(seed)
+    columns = columns or max(1, max(-(-n // ps) for n in lens))
+    pool = sum(-(-n // ps) for n in lens) + 2
+    table = pages_of(lens, ps, pool, columns, gen)
+    u = torch.randn((hkv, 1, d), generator=gen)
+    u /= u.norm(dim=-1, keepdim=True)
+    kp = torch.randn((pool, hkv, ps, d), generator=gen)
+    kp += 0.25 * math.sqrt(d) * -torch.rand((pool, hkv, ps, 1), generator=gen).log() * u
+    kp = kp.to(dt)
+    vp = torch.randn((pool, hkv, ps, d), generator=gen).to(dt)
+    pp = None
+    if masked is not None:
+        pp = torch.randint(0, 1 << 20, (pool, hkv, ps), generator=gen, dtype=torch.int32)
+        pp[torch.rand((pool, hkv, ps), generator=gen) < masked] = -1
+        pp[torch.rand((pool, hkv, ps), generator=gen) < masked / 8] = -(1 << 31)
+    on = torch.zeros((pool, hkv, ps), dtype=torch.bool)
+    for i, n in enumerate(lens):
+        for t in range(0, n, ps):
+            on[table[i, t // ps].item(), :, :min(ps, n - t)] = True
+    if pp is not None:
+        on &= pp >= 0
+    if poison:
+        bad = torch.tensor([math.nan, math.inf, -math.inf, torch.finfo(dt).max])
+        for x in (kp, vp):
+            x[~on] = bad[torch.randint(0, 4, (int((~on).sum()), d), generator=gen)].to(dt)
+    q = (torch.randn((b, hkv, hq // hkv, d), generator=gen) + 4.0 * u).view(b, hq, d).to(dt)
+    if layout == "dense":
+        qd = q.cuda()
+    else:                                                   # a slice of wider rows, off by one element
+        wide = torch.zeros((b, hq * d + 13), dtype=dt)
+        wide[:, 1:1 + hq * d] = q.view(b, hq * d)
+        qd = wide.cuda()[:, 1:1 + hq * d].view(b, hq, d)
+    p = B.PagedParams(b, hq, hkv, d, ps, pool, columns, softmax_scale=scale, dtype=mode)
+    cache = B.PagedCache(p, kp.cuda(), vp.cuda(), table.cuda(), positions=pp.cuda() if pp is not None else None)
+    lens_d = torch.tensor(lens, dtype=torch.int32).cuda()
+    out, lse = B.ems_paged_attention(p, cache, lens_d, qd, want_lse=True)
+    again = B.ems_paged_attention(p, cache, lens_d, qd)
+    torch.cuda.synchronize()
+    assert torch.equal(out, again)
+    sc = scale if scale > 0 else d ** -0.5
+    g = hq // hkv
+    for i, n in enumerate(lens):
+        for h in range(hkv):
+            live = gather(on, table[i], h, n)
+            ref = attention(q[i, h * g:(h + 1) * g], gather(kp, table[i], h, n), gather(vp, table[i], h, n), live, sc, dt)
+            assert_within(out[i, h * g:(h + 1) * g], ref[0], ref[2], f"out of {i}, {h} ({n} rows)")
+            assert_within(lse[i, h * g:(h + 1) * g], ref[1], ref[3], f"lse of {i}, {h} ({n} rows)")
+    return p, cache, lens_d, qd, out
+
+
+ATTEND = [
+    # (b, hq, hkv, d, ps, lens): one block a sequence (tables of up to 256 rows), then shared by several
+    (1, 1, 1, 64, 16, [1]),
+    (4, 4, 4, 64, 16, [0, 1, 16, 17]),
+    (3, 8, 2, 128, 16, [256, 255, 65]),
+    (2, 6, 2, 128, 1, [63, 64]),
+    (2, 7, 1, 64, 7, [200, 33]),
+    (1, 16, 1, 128, 100, [199]),
+    (2, 20, 1, 128, 32, [31, 129]),
+    (2, 33, 1, 64, 8, [0, 100]),
+    (1, 8, 2, 128, 16, [257]),
+    (1, 4, 4, 64, 16, [1024]),
+    (3, 21, 3, 64, 24, [1500, 1, 777]),
+    (2, 8, 1, 128, 256, [3000, 511]),
+    (5, 2, 2, 128, 16, [0, 2500, 0, 300, 1]),
+    (2, 40, 2, 64, 5, [1200, 40]),
+    (40, 2, 1, 64, 16, [(37 * i * i) % 700 for i in range(40)]),
+]
+
+
+@pytest.mark.parametrize("mode", [BF16, F32])
+@pytest.mark.parametrize("masked", [None, 0.0, 0.4, 0.97])
+@pytest.mark.parametrize("shape", ATTEND)
+def test_attention_matches_64_bits(shape, masked, mode):
+    _log("attend", shape, masked, mode)
+    _attend_case(*shape, mode, masked=masked)
+
+
+@pytest.mark.parametrize("mode", [BF16, F32])
+def test_attention_of_heads_without_a_live_row(mode):
+    """Every row of some sequence-heads masked: zeros and -inf, whatever the rows hold."""
+    for lens in ([3, 200], [300, 600]):
+        p, cache, lens_d, q, _ = _attend_case(2, 4, 2, 64, 16, lens, mode, masked=0.5)
+        cache.positions[:, 1] = -1
+        out, lse = B.ems_paged_attention(p, cache, lens_d, q, want_lse=True)
+        assert (out[:, 2:] == 0).all() and (lse[:, 2:] == -math.inf).all()
+        assert out[:, :2].isfinite().all() and lse[1, :2].isfinite().all()
+
+
+def test_attention_layouts_scales_and_long_tables():
+    for mode in (BF16, F32):
+        _attend_case(3, 12, 4, 128, 16, [70, 500, 3], mode, layout="off")
+        _attend_case(2, 6, 6, 64, 16, [70, 500], mode, scale=0.31, masked=0.2)
+        _attend_case(2, 8, 2, 128, 16, [5, 40], mode, columns=600)          # a table much longer than its sequences
+        _attend_case(2, 8, 2, 128, 16, [16 * 40, 7], mode, layout="off", columns=41)
+
+
+def test_attention_clamps_lengths_and_skips_pages_that_do_not_exist():
+    gen = torch.Generator().manual_seed(5)
+    p = B.PagedParams(2, 2, 1, 64, 16, 8, 4)
+    table = torch.tensor([[3, 8, 1, -1], [0, 2, 4, 5]], dtype=torch.int32)
+    cache = B.PagedCache(p, *(torch.randn((8, 1, 16, 64), generator=gen).bfloat16().cuda() for _ in range(2)), table.cuda())
+    q = torch.randn((2, 2, 64), generator=gen).bfloat16().cuda()
+    out = B.ems_paged_attention(p, cache, torch.tensor([64, 1 << 30], dtype=torch.int32).cuda(), q)
+    rows = [[3, 1], [0, 2, 4, 5]]
+    for i in range(2):
+        k, v = (x[rows[i], 0].flatten(0, 1).cpu() for x in (cache.k_pages, cache.v_pages))
+        ref = attention(q[i].cpu(), k, v, torch.ones(len(k), dtype=torch.bool), 0.125, torch.bfloat16)
+        assert_within(out[i], ref[0], ref[2], f"out of {i}")
+    none = B.ems_paged_attention(p, cache, torch.tensor([-5, 0], dtype=torch.int32).cuda(), q)
+    assert (none == 0).all()
+
+
+def test_attention_of_extreme_logits():
+    """Logits of 1e4 and more, equal logits, a row of -inf weights among finite ones."""
+    p = B.PagedParams(1, 2, 1, 64, 16, 40, 40, dtype=F32)
+    table = torch.arange(40, dtype=torch.int32)[None].contiguous().cuda()
+    k = torch.zeros((40, 1, 16, 64))
+    v = torch.randn((40, 1, 16, 64), generator=torch.Generator().manual_seed(6))
+    q = torch.zeros((1, 2, 64))
+    q[0, :, 0] = torch.tensor([1e3, -1e3])
+    cache = lambda k: B.PagedCache(p, k.cuda(), v.cuda(), table)  # noqa: E731
+    n = torch.tensor([640], dtype=torch.int32).cuda()
+    rows = v.view(640, 64).double()
+    out = B.ems_paged_attention(p, cache(k), n, q.cuda())                   # all logits 0: the mean
+    assert_within(out[0], rows.mean(0).expand(2, 64), rows.abs().mean(0) * 2000 * 2.0 ** -24, "mean")
+    k.view(640, 64)[:, 0] = torch.arange(640) * 1.0                         # 125 apart: the last row, the first row
+    out = B.ems_paged_attention(p, cache(k), n, q.cuda())
+    assert torch.equal(out[0].cpu(), v.view(640, 64)[[639, 0]])
+    k.view(640, 64)[5, 0] = math.inf                                        # weight NaN for one head, 0 for the other
+    out = B.ems_paged_attention(p, cache(k), n, q.cuda())
+    assert out[0, 0].isnan().all() and torch.equal(out[0, 1].cpu(), v.view(640, 64)[0])
+
+
+def test_offsets_past_32_bits():
+    """A pool whose last rows start 5 GB behind its first: they are written and read where they are."""
+    hkv, ps, d = 8, 64, 128
+    pool = (5 << 30) // (hkv * ps * d * 2)
+    p = B.PagedParams(1, 8, hkv, d, ps, pool, 3)
+    table = torch.tensor([[pool - 1, 0, pool - 2]], dtype=torch.int32).cuda()
+    pages = [torch.empty((pool, hkv, ps, d), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    for x in pages:
+        x[[0, 1, pool - 3]] = 0
+    cache = B.PagedCache(p, *pages, table)
+    gen = torch.Generator().manual_seed(7)
+    k, v = (torch.randn((1, hkv, 150, d), generator=gen).bfloat16() for _ in range(2))
+    q = torch.randn((1, 8, d), generator=gen).bfloat16()
+    lens = torch.zeros(1, dtype=torch.int32).cuda()
+    B.ems_paged_append(p, cache, torch.zeros(1, dtype=torch.int32).cuda(), k.cuda(), v.cuda(), len_out=lens)
+    out = B.ems_paged_attention(p, cache, lens, q.cuda())
+    for x, y in zip(pages, (k, v)):
+        assert torch.equal(x[pool - 1].cpu(), y[0, :, :64]) and torch.equal(x[0].cpu(), y[0, :, 64:128])
+        assert torch.equal(x[pool - 2, :, :22].cpu(), y[0, :, 128:]) and not x[1].any() and not x[pool - 3].any()
+    for h in range(8):
+        ref = attention(q[0, h:h + 1], k[0, h], v[0, h], torch.ones(150, dtype=torch.bool), d ** -0.5, torch.bfloat16)
+        assert_within(out[0, h:h + 1], ref[0], ref[2], f"head {h}")
+
+
+# ---- how a program uses them
+
+def _loop(p, cache, steps, seed):
+    """Tokens for `steps` rounds and what append and attention have to leave, from the cache's contents now."""
+    gen = torch.Generator().manual_seed(seed)
+    return [[torch.randn((p.batch, h, p.head_dim), generator=gen).to(p.torch_dtype) for h in (p.q_heads, p.kv_heads, p.kv_heads)]
+            for _ in range(steps)]
+
+
+def test_generation_over_pages_replays_from_a_graph():
+    """append + attention of a token, captured once and replayed for token after token, against eager calls on a copy;
+    another captured graph on the same workspace runs in between."""
+    b, hq, hkv, d, ps, cols = 3, 8, 2, 128, 16, 40
+    pool = b * cols
+    p = B.PagedParams(b, hq, hkv, d, ps, pool, cols)
+    table = torch.randperm(pool, generator=torch.Generator().manual_seed(1)).to(torch.int32).view(b, cols).cuda()
+    caches = [B.alloc_paged_cache(p, table, positions=True) for _ in range(2)]
+    start = torch.tensor([0, 255, 600], dtype=torch.int32).cuda()
+    fill = [torch.randn((b, hkv, 601, d), generator=torch.Generator().manual_seed(i)).bfloat16().cuda() for i in (2, 3)]
+    for c in caches:
+        B.ems_paged_append(p, c, torch.zeros_like(start), *fill, new_len=start)
+    freq = _freq(d).cuda()
+    ws = torch.empty(max(256, B.ems_paged_workspace_bytes(p)), dtype=torch.uint8, device="cuda")
+    toks = [[x.cuda() for x in t] for t in _loop(p, caches[0], 6, 4)]
+    buf = [x.clone() for x in toks[0]]
+    lens, after = [start.clone() for _ in range(2)], [start.clone() for _ in range(2)]
+    q_out = torch.empty_like(buf[0])
+    outs = [(torch.empty_like(q_out), torch.empty((b, hq), device="cuda")) for _ in range(2)]
+
+    def step(i, t):
+        q = B.ems_paged_append(p, caches[i], lens[i], t[1], t[2], inv_freq=freq, q=t[0], q_out=q_out, len_out=after[i])
+        B.ems_paged_attention(p, caches[i], after[i], q, want_lse=True, ws=ws, out=outs[i])
+        lens[i].copy_(after[i])
+
+    side = torch.cuda.Stream()
+    graphs = []
+    for i in (1, 0):                                                       # the second graph steps the eager copy's cache
+        graph = torch.cuda.CUDAGraph()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+            step(i, buf)
+        graphs.append(graph)
+    torch.cuda.synchronize()
+    for n, t in enumerate(toks):
+        for x, y in zip(buf, t):
+            x.copy_(y)
+        if n == 3:
+            graphs[1].replay()                                             # both caches move on, one by each graph
+        else:
+            step(0, t)
+        torch.cuda.synchronize()
+        eager = [x.clone() for x in outs[0]]
+        q_out.zero_()
+        graphs[0].replay()
+        torch.cuda.synchronize()
+        assert torch.equal(outs[1][0], eager[0]) and torch.equal(outs[1][1], eager[1]), n
+        for x in ("k_pages", "v_pages", "positions"):
+            assert torch.equal(getattr(caches[0], x), getattr(caches[1], x)), (n, x)
+        assert lens[0].tolist() == lens[1].tolist() == [n + 1, 256 + n, 601 + n]
+
+
+def test_calls_on_a_stream_of_their_own():
+    p, cache, lens, q, want = _attend_case(2, 8, 2, 128, 16, [700, 90], BF16, masked=0.1)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = B.ems_paged_attention(p, cache, lens, q)
+    side.synchronize()
+    assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("mode", [BF16, F32])
+def test_compressed_prompt_goes_on_over_pages(mode):
+    """A prompt is scored, compressed and expanded; the expansion becomes the start of a paged generation, evicted rows
+    masked head by head; new tokens are rotated, appended and attended.  Against the same in 64 bits from the rows the
+    library expanded."""
+    import ems_inputs
+    from gpu_util import dev_tensor
+    b, hq, hkv, d, n, w, nb, ps = 2, 8, 2, 64, 700, 16, 120, 16
+    dt = torch.float32 if mode == F32 else torch.bfloat16
+    inp = ems_inputs.small(b, hq, hkv, d, n, seed=9)
+    ep = B.EmsParams(b, hq, hkv, d, n, w, nb, merge_ratio=2.0, tau=0.25, dtype=mode)
+    q, k, v = (dev_tensor(getattr(inp, x), mode) for x in "qkv")
+    imp, tbm = B.ems_select(ep, *B.ems_global_local_score(ep, q, k))
+    rows = B.ems_expand(ep, B.ems_evict_merge(ep, k, v, imp, tbm), tbm)
+    n_exp = rows[2].shape[2]
+    assert (rows[2] < 0).any()
+    cols = -(-(n_exp + 4) // ps)
+    p = B.PagedParams(b, hq, hkv, d, ps, b * cols, cols, dtype=mode)
+    table = torch.arange(b * cols - 1, -1, -1, dtype=torch.int32).view(b, cols).cuda()
+    cache = B.alloc_paged_cache(p, table, positions=True)
+    lens, after = torch.zeros(b, dtype=torch.int32).cuda(), torch.zeros(b, dtype=torch.int32).cuda()
+    B.ems_paged_append(p, cache, lens, rows[0], rows[1], positions=rows[2], len_out=after)
+    freq = _freq(d)
+    host = [x.cpu() for x in rows]
+    ks, vs, live = host[0].double(), host[1].double(), host[2] >= 0
+    for t, (qn, kn, vn) in enumerate(_loop(p, cache, 4, 10)):
+        lens, after = after, lens
+        pos = torch.full((b, 1), n + t, dtype=torch.int32)
+        qr = B.ems_paged_append(p, cache, lens, kn.cuda(), vn.cuda(), positions=pos.cuda(), inv_freq=freq.cuda(),
+                                q=qn.cuda(), len_out=after)
+        out = B.ems_paged_attention(p, cache, after, qr)
+        assert after.tolist() == [n_exp + t + 1] * b
+        # the key the library stored (its rotation is tested above): rounding it here again could go the other way
+        at = n_exp + t
+        page = table[:, at // ps].long()
+        kr = cache.k_pages[page, :, at % ps].cpu().double()
+        y, slack = rotated(kn, torch.full((b, hkv), n + t), freq, False)
+        assert_within(kr, y, y.abs() * half_step(dt) + slack, "new key")
+        ks, vs = torch.cat((ks, kr[:, :, None]), 2), torch.cat((vs, vn[:, :, None].double()), 2)
+        live = torch.cat((live, torch.ones((b, hkv, 1), dtype=torch.bool)), 2)
+        g = hq // hkv
+        for i in range(b):
+            for h in range(hkv):
+                ref = attention(qr[i, h * g:(h + 1) * g].cpu(), ks[i, h], vs[i, h], live[i, h], d ** -0.5, dt)
+                assert_within(out[i, h * g:(h + 1) * g], ref[0], ref[2], f"token {t} of {i}, {h}")
