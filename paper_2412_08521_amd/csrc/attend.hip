@@ -25,8 +25,10 @@ constexpr int kWaves = 4;
 constexpr int kNewRow = -2;      // the row of the new token itself (compact cache)
 constexpr int kNoRow = -1;
 
-template <typename T> constexpr int kStep = 128 / (int)sizeof(T);      // rows of a wave's step: 64 or 32
-template <typename T> constexpr int kUnit = kWaves * kStep<T>;         // rows of a block's: what stretches are counted in
+constexpr int kLook = 64;                 // rows that a wave looks up at a time, a lane each
+constexpr int kUnit = kWaves * kLook;     // rows of a block's turn: what stretches are counted in
+
+template <typename T, int D> constexpr int kRowBytesOf = D * (int)sizeof(T);
 
 __device__ __forceinline__ int live_len(const AttendArgs& a, bool table, int b)
 {
@@ -35,19 +37,25 @@ __device__ __forceinline__ int live_len(const AttendArgs& a, bool table, int b)
     return (int)min((long long)max(a.lens[b], 0), most);
 }
 
-template <typename T> __device__ __forceinline__ int units_of(int len) { return len / kUnit<T> + (len % kUnit<T> > 0); }
+__device__ __forceinline__ int units_of(int len) { return (len + kUnit - 1) / kUnit; }
+
+// a value that is the same in every lane, for the scalar registers
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ long long uniform(long long x)
+{
+    return (long long)(unsigned)uniform((int)x) | (long long)uniform((int)(x >> 32)) << 32;
+}
 
 // Units of sequences 0..b-1, or of all of them (b = batch); the same in every lane.
-template <typename T>
 __device__ __forceinline__ long long units_before(const AttendArgs& a, bool table, int b)
 {
-    if (table) return (long long)b * units_of<T>(a.n_tok + 1);
+    if (table) return (long long)b * units_of(a.n_tok + 1);
     const int lane = threadIdx.x % kWave;
     long long n = 0;
-    for (int i = lane; i < b; i += kWave) n += units_of<T>(live_len(a, table, i));
+    for (int i = lane; i < b; i += kWave) n += units_of(live_len(a, table, i));
 #pragma unroll
     for (int s = 1; s < kWave; s *= 2) n += __shfl_xor(n, s);
-    return n;
+    return uniform(n);
 }
 
 // Max or sum over the four lanes l % 16 + 16 n that share a column.
@@ -58,24 +66,27 @@ __device__ __forceinline__ float column_reduce(float v)
     return comb<kMax>(v, __shfl_xor(v, 32));
 }
 
-template <typename T, int D> struct Acc { static constexpr int kTiles = D / 16; };
-
 }  // namespace
 
 template <typename T, int D, bool kTable>
-__global__ __launch_bounds__(256) void attend_kernel(AttendArgs a)
+__global__ __launch_bounds__(256, sizeof(T) == 2 && !(kTable && D == 128) ? 3 : 2) void attend_kernel(AttendArgs a)
 {
-    constexpr int kRows = kStep<T>, kTiles = kRows / 16;       // rows and 16-row tiles of a step
+    constexpr int kTiles = kRowBytesOf<T, D> <= 256 ? 2 : 1;    // 16-row tiles of a step: their keys and values wait in registers
+    constexpr int kStep = 16 * kTiles, kSteps = kLook / kStep;
     constexpr int kPieces = D * (int)sizeof(T) / 64;           // 16-byte pieces of a key row that a lane reads
     constexpr int kOut = D / 16;                               // output tiles (16 columns of V each)
     constexpr int kCols = D / 16;                              // columns of V that a lane holds of a row
-    constexpr size_t kRowBytes = D * sizeof(T);
-    __shared__ __align__(16) int row_of[kWaves][kRows];
-    __shared__ __align__(16) float factor_of[kWaves][kTable ? kRows : 4];
+    constexpr size_t kRowBytes = kRowBytesOf<T, D>;
+    // a piece of a value row: kCols columns at kCols col (16-bit elements), or four at 4 col of every 64 (float32)
+    constexpr int kVec = sizeof(T) == 2 ? kCols / 2 : 4;       // dwords
+    constexpr int kParts = sizeof(T) == 2 ? 1 : D / 64;
+    typedef int vec_t __attribute__((ext_vector_type(kVec)));
+    __shared__ __align__(16) int row_of[kWaves][2][kLook];
+    __shared__ __align__(16) float factor_of[kWaves][2][kTable ? kLook : 4];
     __shared__ __align__(16) float red_o[kWaves][kAttendQ][D + 4];
     __shared__ float red_ml[kWaves][kAttendQ][2];
 
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int lane = threadIdx.x % kWave, wave = uniform((int)threadIdx.x / kWave);
     const int col = lane % 16, quad = lane / 16;
     const int group_tiles = (a.group + kAttendQ - 1) / kAttendQ;
 
@@ -86,14 +97,14 @@ __global__ __launch_bounds__(256) void attend_kernel(AttendArgs a)
         worker = blockIdx.x % a.workers;
         const int ht = blockIdx.x / a.workers;
         head = ht % a.kv_heads; tile = ht / a.kv_heads;
-        const long long total = units_before<T>(a, kTable, a.batch);
+        const long long total = units_before(a, kTable, a.batch);
         const long long workers = min((long long)a.workers, total);               // none without a unit
         if (worker >= workers) return;
         u = worker * total / workers;
         u_end = (worker + 1) * total / workers;
         base = 0;
         for (b = 0; b < a.batch - 1; ++b) {
-            const int n = units_of<T>(live_len(a, kTable, b));
+            const int n = units_of(live_len(a, kTable, b));
             if (u < base + n) break;
             base += n;
         }
@@ -102,14 +113,14 @@ __global__ __launch_bounds__(256) void attend_kernel(AttendArgs a)
         const int ht = blockIdx.x / a.batch;
         head = ht % a.kv_heads; tile = ht / a.kv_heads;
         base = 0; u = 0;
-        u_end = units_of<T>(live_len(a, kTable, b));
+        u_end = units_of(live_len(a, kTable, b));
     }
     (void)group_tiles;
     const int q0 = tile * kAttendQ, n_q = min(a.group - q0, kAttendQ);
 
     do {
         const int len = live_len(a, kTable, b);
-        const long long seq_units = units_of<T>(len);
+        const long long seq_units = units_of(len);
         const long long first = u - base, last = min(u_end - base, seq_units);      // units of this sequence
         const int unit = b * a.kv_heads + head;
         const size_t q_head = (size_t)unit * a.group + q0;                          // = b * Hq + head * group + q0
@@ -139,71 +150,75 @@ __global__ __launch_bounds__(256) void attend_kernel(AttendArgs a)
         for (int i = 0; i < kOut; ++i) o[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         float m = -INFINITY, l = 0.f;                          // of column `col`; l: this lane's rows only
 
-        for (long long t0 = first * kUnit<T> + wave * kRows; t0 < min(last * kUnit<T>, (long long)len); t0 += kUnit<T>) {
-            // the step's rows, a lane each
-            const int t = (int)t0 + lane;
-            int row = kNoRow;
-            float factor = 0.f;
-            if (lane < kRows && t < len) {
-                if constexpr (kTable) {
-                    if (t == a.n_tok) { row = kNewRow; factor = 1.f; }
-                    else {
-                        row = a.tok_row[(size_t)unit * a.n_tok + t];
-                        if (row >= 0 && row < a.budget) {
-                            const float norm = a.row_norm[(size_t)unit * a.budget + row];
-                            factor = norm > 0.f ? a.tok_norm[(size_t)unit * a.n_tok + t] / norm : 0.f;
-                        } else row = kNoRow;
-                    }
-                } else {
-                    const int page = a.page_table[(size_t)b * a.max_pages + t / a.page_size];
-                    if (page >= 0 && page < a.num_pages) {
-                        row = (page * a.kv_heads + head) * a.page_size + t % a.page_size;
-                        if (a.pos_pages && a.pos_pages[row] < 0) row = kNoRow;
-                    }
+        // Rows are looked up a batch of 64 ahead in two trips (the table; the position, or the norms), keys and values are
+        // requested a step ahead, as soon as the registers that take them are free.
+        const int t_end = (int)min(last * kUnit, (long long)len);
+        const int t_first = (int)(first * kUnit) + wave * kLook + lane;
+        const int n_batches = t_end > t_first - lane ? (t_end - (t_first - lane) + kUnit - 1) / kUnit : 0;
+        struct Look { int row, mask; float norm; };            // mask: the position; norms of the token and of its row
+        const auto table_trip = [&](int t) -> int {
+            if constexpr (kTable) return t < a.n_tok ? a.tok_row[(size_t)unit * a.n_tok + t] : t == a.n_tok ? kNewRow : kNoRow;
+            return t < t_end ? a.page_table[(size_t)b * a.max_pages + t / a.page_size] : kNoRow;
+        };
+        const auto row_trip = [&](int t, int entry) -> Look {
+            Look r{kNoRow, 0, 0.f};
+            if constexpr (kTable) {
+                r.row = entry;
+                if (entry >= a.budget || entry < kNewRow) r.row = kNoRow;
+                if (r.row >= 0) {
+                    r.norm = a.row_norm[(size_t)unit * a.budget + entry];
+                    r.mask = __builtin_bit_cast(int, a.tok_norm[(size_t)unit * a.n_tok + t]);
                 }
+            } else if (t < t_end && entry >= 0 && entry < a.num_pages) {
+                r.row = (entry * a.kv_heads + head) * a.page_size + t % a.page_size;
+                if (a.pos_pages) r.mask = a.pos_pages[r.row];
             }
+            return r;
+        };
+        // the batch's rows to LDS; which of them are live.  Dead rows are read as the first live one, which is in bounds
+        // and in the cache already (row 0 where none is live).
+        const auto settle = [&](int t, const Look& k, int buf) -> unsigned long long {
+            int row = k.row;
+            if constexpr (kTable) {
+                if (t >= t_end) row = kNoRow;
+                factor_of[wave][buf][lane] = row == kNewRow ? 1.f : k.norm > 0.f ? __builtin_bit_cast(float, k.mask) / k.norm : 0.f;
+            } else if (k.mask < 0) row = kNoRow;
             const unsigned long long live = __ballot(row != kNoRow);
-            if (!live) continue;
-            // dead rows are read as the first live one: in bounds, and in the cache already
-            const int spare = __builtin_amdgcn_readlane(row, __builtin_ctzll(live));
-            if (lane < kRows) {
-                row_of[wave][lane] = row != kNoRow ? row : spare;
-                if constexpr (kTable) factor_of[wave][lane] = factor;
-            }
+            const int spare = live ? __builtin_amdgcn_readlane(row, __builtin_ctzll(live)) : 0;
+            row_of[wave][buf][lane] = row != kNoRow ? row : spare;
             __builtin_amdgcn_wave_barrier();
-
-            const auto address = [&](const void* rows, const void* fresh, int r) {
-                const char* p = reinterpret_cast<const char*>(rows);
-                if constexpr (kTable) {
-                    p += (size_t)unit * (a.budget + 1) * kRowBytes;
-                    return r == kNewRow ? reinterpret_cast<const char*>(fresh) + unit * kRowBytes : p + (size_t)r * kRowBytes;
-                }
-                return p + (size_t)(unsigned)r * kRowBytes;
-            };
-
-            // keys, then values
-            frag_t kf[kTiles][kPieces];
+            return live;
+        };
+        const auto address = [&](const void* rows, const void* fresh, int r) -> const char* {
+            const char* p = reinterpret_cast<const char*>(rows);
+            if constexpr (kTable) {
+                p += (size_t)unit * (a.budget + 1) * kRowBytes;
+                return r == kNewRow ? reinterpret_cast<const char*>(fresh) + unit * kRowBytes : p + (size_t)(unsigned)r * kRowBytes;
+            }
+            return p + (size_t)(unsigned)r * kRowBytes;
+        };
+        frag_t kf[kTiles][kPieces];
+        const auto load_keys = [&](int buf, int at) {
 #pragma unroll
             for (int i = 0; i < kTiles; ++i) {
-                const char* p = address(a.k, a.k_new, row_of[wave][16 * i + col]) + 16 * quad;
+                const char* p = address(a.k, a.k_new, row_of[wave][buf][kStep * at + 16 * i + col]) + 16 * quad;
 #pragma unroll
                 for (int c = 0; c < kPieces; ++c) kf[i][c] = *reinterpret_cast<const frag_t*>(p + 64 * c);
             }
-            // value rows 16 i + 4 quad + r; a lane's columns are kCols ones at kCols col (16-bit elements), or four at 4 col
-            // of every 64 (float32)
-            constexpr int kVec = sizeof(T) == 2 ? kCols * 2 / 4 : 4;                // dwords of a piece
-            constexpr int kParts = sizeof(T) == 2 ? 1 : D / 64;
-            typedef int vec_t __attribute__((ext_vector_type(kVec)));
-            vec_t vf[kTiles][4][kParts];
+        };
+        vec_t vf[kTiles][4][kParts];                           // rows 16 i + 4 quad + r
+        const auto load_values = [&](int buf, int at) {
 #pragma unroll
             for (int i = 0; i < kTiles; ++i)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const char* p = address(a.v, a.v_new, row_of[wave][16 * i + 4 * quad + r]) + 4 * kVec * col;
+                    const char* p = address(a.v, a.v_new, row_of[wave][buf][kStep * at + 16 * i + 4 * quad + r]) + 4 * kVec * col;
 #pragma unroll
                     for (int h = 0; h < kParts; ++h) vf[i][r][h] = *reinterpret_cast<const vec_t*>(p + 256 * h);
                 }
-
+        };
+        // one step on the rows in kf and vf, which the rows of (next_buf, next_at) then take
+        const auto step = [&](unsigned live, int buf, int at, int next_buf, int next_at) {
             f32x4_t s[kTiles];
 #pragma unroll
             for (int i = 0; i < kTiles; ++i) {
@@ -220,16 +235,19 @@ __global__ __launch_bounds__(256) void attend_kernel(AttendArgs a)
                     }
                 }
             }
+            __builtin_amdgcn_sched_barrier(0);
+            load_keys(next_buf, next_at);
+            __builtin_amdgcn_sched_barrier(0);
             // logits in units of ln 2, dead rows -inf whatever their products are
+            live >>= 4 * quad;
             float top = -INFINITY;
 #pragma unroll
             for (int i = 0; i < kTiles; ++i) {
                 f32x4_t f = {a.scale_log2e, a.scale_log2e, a.scale_log2e, a.scale_log2e};
-                if constexpr (kTable) f *= *reinterpret_cast<const f32x4_t*>(&factor_of[wave][16 * i + 4 * quad]);
+                if constexpr (kTable) f *= *reinterpret_cast<const f32x4_t*>(&factor_of[wave][buf][kStep * at + 16 * i + 4 * quad]);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const bool on = (live >> (16 * i + 4 * quad + r)) & 1;
-                    s[i][r] = on ? s[i][r] * f[r] : -INFINITY;
+                    s[i][r] = (live >> (16 * i + r)) & 1 ? s[i][r] * f[r] : -INFINITY;
                     top = fmaxf(top, s[i][r]);
                 }
             }
@@ -247,40 +265,34 @@ __global__ __launch_bounds__(256) void attend_kernel(AttendArgs a)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) { s[i][r] = exp2_fast(s[i][r] - ref); l += s[i][r]; }
             // what stands in a dead row must not meet its zero weight
-            if (live != (kRows == 64 ? ~0ull : (1ull << kRows) - 1)) {
+            constexpr unsigned kMine = kTiles == 2 ? 0x000f000f : 0xf;
+            if (!__all((live & kMine) == kMine)) {
 #pragma unroll
                 for (int i = 0; i < kTiles; ++i)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const bool on = (live >> (16 * i + 4 * quad + r)) & 1;
+                    for (int r = 0; r < 4; ++r)
 #pragma unroll
                         for (int h = 0; h < kParts; ++h)
 #pragma unroll
-                            for (int w = 0; w < kVec; ++w) vf[i][r][h][w] = on ? vf[i][r][h][w] : 0;
-                    }
+                            for (int w = 0; w < kVec; ++w) vf[i][r][h][w] = (live >> (16 * i + r)) & 1 ? vf[i][r][h][w] : 0;
             }
             if constexpr (sizeof(T) == 2) {
+                bf16x8_t high, rest;
 #pragma unroll
-                for (int i = 0; i < kTiles; i += 2) {
-                    bf16x8_t high, rest;
+                for (int r = 0; r < 8; ++r) {
+                    const float p = s[r / 4][r % 4];
+                    high[r] = (bf16_t)p;
+                    rest[r] = (bf16_t)(p - (float)high[r]);
+                }
 #pragma unroll
-                    for (int r = 0; r < 8; ++r) {
-                        const float p = s[i + r / 4][r % 4];
-                        high[r] = (bf16_t)p;
-                        rest[r] = (bf16_t)(p - (float)high[r]);
-                    }
+                for (int e = 0; e < kCols; ++e) {
+                    frag_t x;
 #pragma unroll
-                    for (int e = 0; e < kCols; ++e) {
-                        frag_t x;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const int r = 2 * j;
-                            x[j] = __builtin_amdgcn_perm(vf[i + (r + 1) / 4][(r + 1) % 4][0][e / 2], vf[i + r / 4][r % 4][0][e / 2],
-                                                         e % 2 ? 0x07060302 : 0x05040100);
-                        }
-                        o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, x), high, o[e], 0, 0, 0);
-                        o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, x), rest, o[e], 0, 0, 0);
-                    }
+                    for (int j = 0; j < 4; ++j)
+                        x[j] = __builtin_amdgcn_perm(vf[(2 * j + 1) / 4][(2 * j + 1) % 4][0][e / 2], vf[2 * j / 4][2 * j % 4][0][e / 2],
+                                                     e % 2 ? 0x07060302 : 0x05040100);
+                    o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, x), high, o[e], 0, 0, 0);
+                    o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, x), rest, o[e], 0, 0, 0);
                 }
             } else {
 #pragma unroll
@@ -295,7 +307,27 @@ __global__ __launch_bounds__(256) void attend_kernel(AttendArgs a)
                                 o[4 * h + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], s[i][r], o[4 * h + e], 0, 0, 0);
                         }
             }
-            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_sched_barrier(0);
+            load_values(next_buf, next_at);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+
+        if (n_batches) {
+            int entry = table_trip(t_first);
+            unsigned long long live = settle(t_first, row_trip(t_first, entry), 0);
+            entry = table_trip(t_first + kUnit);
+            load_keys(0, 0);
+            load_values(0, 0);
+            for (int j = 0, t = t_first + kUnit; j < n_batches; ++j, t += kUnit) {          // t: the lane's row of batch j + 1
+                const int buf = j & 1;
+                const Look next = row_trip(t, entry);
+                entry = table_trip(t + kUnit);
+#pragma unroll
+                for (int i = 0; i < kSteps - 1; ++i) step((unsigned)(live >> (kStep * i)), buf, i, buf, i + 1);
+                const unsigned rest = (unsigned)(live >> (kLook - kStep));
+                live = settle(t, next, 1 - buf);
+                step(rest, buf, kSteps - 1, 1 - buf, 0);
+            }
         }
         l = column_reduce<false>(l);
 
@@ -361,11 +393,11 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a)
         if (a.lse && threadIdx.x == 0) a.lse[blockIdx.x] = -INFINITY;
         return;
     }
-    const long long total = units_before<T>(a, kTable, a.batch), base = units_before<T>(a, kTable, b);
+    const long long total = units_before(a, kTable, a.batch), base = units_before(a, kTable, b);
     // worker w takes units [w total / workers, (w + 1) total / workers)
     const long long workers = min((long long)a.workers, total);
     const auto worker_of = [&](long long unit) { return (int)(((unit + 1) * workers - 1) / total); };
-    const int w0 = worker_of(base), w1 = worker_of(base + units_of<T>(len) - 1);
+    const int w0 = worker_of(base), w1 = worker_of(base + units_of(len) - 1);
     if (w0 == w1) return;                                      // one worker had all of it
 
     const int grp = threadIdx.x / kLanes, d = threadIdx.x % kLanes * 4;
@@ -406,7 +438,7 @@ int attend_workers(int batch, int kv_heads, int group, long long max_len)
 {
     if (max_len <= 256) return 0;
     const long long columns = (long long)kv_heads * ((group + kAttendQ - 1) / kAttendQ);
-    const long long want = (512 + columns - 1) / columns;      // two blocks a compute unit
+    const long long want = (768 + columns - 1) / columns;      // three blocks a compute unit
     return (int)want;
 }
 
