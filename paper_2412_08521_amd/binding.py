@@ -7,6 +7,7 @@ built, importing the entry points raises.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from dataclasses import dataclass
 
@@ -95,7 +96,7 @@ class EmsParams:
         return torch.float32 if self.dtype == EMS_F32 else torch.bfloat16
 
 
-@dataclass
+@dataclass(frozen=True)
 class PagedParams:
     batch: int
     q_heads: int
@@ -107,13 +108,17 @@ class PagedParams:
     softmax_scale: float = 0.0
     dtype: int = EMS_BF16
 
-    def c(self) -> ems_paged_params:
-        return ems_paged_params(self.batch, self.q_heads, self.kv_heads, self.head_dim, self.page_size, self.num_pages,
-                                self.max_pages, self.softmax_scale, self.dtype)
+    def __post_init__(self):                       # what every call needs of them, made once (they do not change)
+        put = lambda name, x: object.__setattr__(self, name, x)  # noqa: E731
+        put("_c", ems_paged_params(self.batch, self.q_heads, self.kv_heads, self.head_dim, self.page_size, self.num_pages,
+                                   self.max_pages, self.softmax_scale, self.dtype))
+        put("torch_dtype", torch.float32 if self.dtype == EMS_F32 else torch.bfloat16)
+        put("_q_row", (self.batch, self.q_heads, self.head_dim))
+        put("_pages", (self.num_pages, self.kv_heads, self.page_size, self.head_dim))
+        put("_table", (self.batch, self.max_pages))
 
-    @property
-    def torch_dtype(self):
-        return torch.float32 if self.dtype == EMS_F32 else torch.bfloat16
+    def c(self) -> ems_paged_params:
+        return self._c
 
 
 _lib = None
@@ -538,25 +543,46 @@ def ems_redundancy_rate(p: EmsParams, k, v):
     return rate, best
 
 
-def _check_here(t, dtype, name, shape=None):
-    """A device tensor of the current device (the launch goes to it), of a shape where one is given."""
-    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+# The calls of a generation's step are short: like the others they cost the host more than the device, and a check is
+# most of what a call does here.  The current device is asked for once a call.
+def _check(t, dev, dtype, shape, name):
+    """A device tensor of the current device (the launch goes to it)."""
+    if t.get_device() != dev:
         raise ValueError(f"{name} must be a tensor of the current device")
-    if t.dtype != dtype or (shape is not None and t.shape != shape):
-        raise ValueError(f"{name}: expected {dtype} {shape if shape is None else tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    if t.dtype != dtype or t.shape != shape:
+        raise ValueError(f"{name}: expected {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
 
 
-def _check_ws(ws, need, device):
+def _check_dense(t, dev, dtype, shape, name):
+    _check(t, dev, dtype, shape, name)
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+
+
+def _current_device():
+    try:
+        return torch.cuda.current_device()
+    except (RuntimeError, AssertionError):            # no device: every tensor is refused
+        return None
+
+
+def _check_ws(ws, dev, need, p):
     if ws is None:
-        return torch.empty(max(need, 256), dtype=torch.uint8, device=device)
-    _check_here(ws, torch.uint8, "ws")
+        return torch.empty(max(need(p), 256), dtype=torch.uint8, device="cuda")
+    if ws.get_device() != dev or ws.dtype != torch.uint8 or not ws.is_contiguous():
+        raise ValueError("ws: contiguous bytes of the current device")
     return ws
 
 
-def _check_dense(t, dtype, name, shape):
-    _check_here(t, dtype, name, shape)
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
+@functools.lru_cache(maxsize=512)
+def _table_length(seq_len, window, budget, merge_ratio):
+    """Tokens of a decode state's table; it depends on nothing else of the parameters."""
+    return sum(_partition_sizes(EmsParams(1, 1, 1, 64, seq_len, window, budget, merge_ratio).c())) + window
+
+
+@functools.lru_cache(maxsize=512)
+def _strides(batch, head, token):
+    return C.byref(ems_strides(batch, head, token))
 
 
 def ems_decode_attention_workspace_bytes(p: EmsParams) -> int:
@@ -571,35 +597,36 @@ def ems_decode_attention_workspace_bytes(p: EmsParams) -> int:
 def ems_decode_attention(p: EmsParams, st: DecodeState, q_new, k_new, v_new, want_lse=False, ws=None, out=None):
     """Attention of one new token over the compact cache and itself -> out [B,Hq,D] (or (out, lse [B,Hq] f32) with
     want_lse).  Call it before the token's ems_decode_step.  `out`: (out, lse or None) to write to."""
+    dev, dt, cp = _current_device(), p.torch_dtype, p.c()
     heads, shape = (p.batch, p.q_heads), (p.batch, p.kv_heads, p.head_dim)
-    dt = p.torch_dtype
-    _check_dense(q_new, dt, "q_new", heads + (p.head_dim,))
-    _check_dense(k_new, dt, "k_new", shape)
-    _check_dense(v_new, dt, "v_new", shape)
-    n_imp, n_tbm = _partition_sizes(p.c())
-    _check_dense(st.k_cache, dt, "k_cache", (p.batch, p.kv_heads, p.budget + 1, p.head_dim))
-    _check_dense(st.tok_row, torch.int32, "tok_row", (p.batch, p.kv_heads, n_imp + n_tbm + p.window))
-    ws = _check_ws(ws, ems_decode_attention_workspace_bytes(p) if ws is None else 0, q_new.device)
-    o, lse = _attention_out(out, want_lse, heads, p.head_dim, dt, q_new.device)
-    cp, cs = p.c(), st.c()
-    rc = lib().ems_decode_attention(C.byref(cp), C.byref(cs), _ptr(q_new), _ptr(k_new), _ptr(v_new), _ptr(o), _ptr(lse),
-                                    _ptr(ws), ws.numel(), _stream())
+    _check_dense(q_new, dev, dt, heads + shape[2:], "q_new")
+    _check_dense(k_new, dev, dt, shape, "k_new")
+    _check_dense(v_new, dev, dt, shape, "v_new")
+    table = (p.batch, p.kv_heads, _table_length(p.seq_len, p.window, p.budget, p.merge_ratio))
+    _check_dense(st.k_cache, dev, dt, (p.batch, p.kv_heads, p.budget + 1, p.head_dim), "k_cache")
+    _check_dense(st.tok_row, dev, torch.int32, table, "tok_row")
+    ws = _check_ws(ws, dev, ems_decode_attention_workspace_bytes, p)
+    o, lse = _attention_out(out, dev, want_lse, heads + shape[2:], dt)
+    cs = st.c()
+    rc = lib().ems_decode_attention(C.byref(cp), C.byref(cs), q_new.data_ptr(), k_new.data_ptr(), v_new.data_ptr(),
+                                    o.data_ptr(), _ptr(lse), ws.data_ptr(), ws.numel(), _stream())
     if rc != EMS_OK:
         raise EmsError(rc, "ems_decode_attention")
     return (o, lse) if want_lse else o
 
 
-def _attention_out(out, want_lse, heads, head_dim, dtype, device):
+def _attention_out(out, dev, want_lse, shape, dtype):
     if out is None:
-        return (torch.empty(heads + (head_dim,), dtype=dtype, device=device),
-                torch.empty(heads, dtype=torch.float32, device=device) if want_lse else None)
+        return (torch.empty(shape, dtype=dtype, device="cuda"),
+                torch.empty(shape[:2], dtype=torch.float32, device="cuda") if want_lse else None)
     o, lse = out
-    _check_dense(o, dtype, "out", heads + (head_dim,))
-    if want_lse and lse is None:
+    _check_dense(o, dev, dtype, shape, "out")
+    if not want_lse:
+        return o, None
+    if lse is None:
         raise ValueError("out: a tensor for the log-sum-exp is wanted")
-    if lse is not None:
-        _check_dense(lse, torch.float32, "lse", heads)
-    return o, lse if want_lse else None
+    _check_dense(lse, dev, torch.float32, shape[:2], "lse")
+    return o, lse
 
 
 class PagedCache:
@@ -608,41 +635,40 @@ class PagedCache:
     int32 the position of every row, negative = masked."""
 
     def __init__(self, p: PagedParams, k_pages, v_pages, page_table, positions=None):
-        rows = (p.num_pages, p.kv_heads, p.page_size)
-        _check_dense(k_pages, p.torch_dtype, "k_pages", rows + (p.head_dim,))
-        _check_dense(v_pages, p.torch_dtype, "v_pages", rows + (p.head_dim,))
-        _check_dense(page_table, torch.int32, "page_table", (p.batch, p.max_pages))
+        dev = _current_device()
+        _check_dense(k_pages, dev, p.torch_dtype, p._pages, "k_pages")
+        _check_dense(v_pages, dev, p.torch_dtype, p._pages, "v_pages")
+        _check_dense(page_table, dev, torch.int32, p._table, "page_table")
         if positions is not None:
-            _check_dense(positions, torch.int32, "positions", rows)
+            _check_dense(positions, dev, torch.int32, p._pages[:3], "positions")
         self.k_pages, self.v_pages, self.page_table, self.positions = k_pages, v_pages, page_table, positions
+        self.device_index = dev
 
-    def _check(self, p: PagedParams):
-        rows = self.k_pages.shape
-        if (p.num_pages, p.kv_heads, p.page_size, p.head_dim) != rows or (p.batch, p.max_pages) != self.page_table.shape \
-                or p.torch_dtype != self.k_pages.dtype:
-            raise ValueError(f"cache of {tuple(rows)} pages, {tuple(self.page_table.shape)} table does not fit {p}")
-
-    def c(self) -> ems_paged_cache:
-        return ems_paged_cache(_ptr(self.k_pages), _ptr(self.v_pages), _ptr(self.positions), _ptr(self.page_table))
+    def _c(self, p: PagedParams, dev):
+        """The cache for a call on device `dev` with parameters that have to be those of its tensors."""
+        k = self.k_pages
+        if k.shape != p._pages or self.page_table.shape != p._table or k.dtype != p.torch_dtype:
+            raise ValueError(f"a cache of {tuple(k.shape)} rows with a table of {tuple(self.page_table.shape)} does not fit {p}")
+        if self.device_index != dev:
+            raise ValueError("the cache must be on the current device")
+        return C.byref(ems_paged_cache(k.data_ptr(), self.v_pages.data_ptr(), _ptr(self.positions), self.page_table.data_ptr()))
 
 
 def alloc_paged_cache(p: PagedParams, page_table, positions: bool = False) -> PagedCache:
     """A cache of `p.num_pages` pages for the sequences of `page_table`; with `positions` every row starts masked."""
-    rows = (p.num_pages, p.kv_heads, p.page_size)
     dev = page_table.device
-    return PagedCache(p, torch.zeros(rows + (p.head_dim,), dtype=p.torch_dtype, device=dev),
-                      torch.zeros(rows + (p.head_dim,), dtype=p.torch_dtype, device=dev), page_table,
-                      torch.full(rows, -1, dtype=torch.int32, device=dev) if positions else None)
+    return PagedCache(p, torch.zeros(p._pages, dtype=p.torch_dtype, device=dev),
+                      torch.zeros(p._pages, dtype=p.torch_dtype, device=dev), page_table,
+                      torch.full(p._pages[:3], -1, dtype=torch.int32, device=dev) if positions else None)
 
 
-def _rows(t, heads, n, p, name):
-    """[B, heads, n, D], or [B, heads, D] for one token, with any strides but the last -> its strides."""
-    shape = (p.batch, heads, n, p.head_dim) if t.dim() == 4 else (p.batch, heads, p.head_dim)
-    _check_here(t, p.torch_dtype, name, shape)
+def _rows(t, dev, dtype, shape, name):
+    """Rows [B, heads, n, D], or [B, heads, D] for one token, with any strides but the last -> their strides."""
+    _check(t, dev, dtype, shape, name)
     s = t.stride()
     if s[-1] != 1:
         raise ValueError(f"{name}: the elements of a row must be adjacent")
-    return ems_strides(s[0], s[1], s[2] if t.dim() == 4 else 0)
+    return _strides(s[0], s[1], s[2] if len(s) == 4 else 0)
 
 
 def ems_paged_append(p: PagedParams, cache: PagedCache, start, k, v, positions=None, new_len=None, inv_freq=None,
@@ -651,39 +677,42 @@ def ems_paged_append(p: PagedParams, cache: PagedCache, start, k, v, positions=N
     queries q [B,Hq,N,D] are rotated by inv_freq [rot/2] f32 at their positions ([B,N] or [B,Hkv,N] int32, default
     the row).  new_len [B] int32: tokens there are of the N.  -> q_out (q's shape; pass q to rotate in place), None
     without q.  len_out [B] int32 is written start + new tokens."""
-    cache._check(p)
-    n = k.shape[2] if k.dim() == 4 else 1
-    ks, vs = _rows(k, p.kv_heads, n, p, "k"), _rows(v, p.kv_heads, n, p, "v")
-    _check_dense(start, torch.int32, "start", (p.batch,))
+    dev, dt, b = _current_device(), p.torch_dtype, p.batch
+    cc = cache._c(p, dev)
+    single = k.dim() == 3
+    n = 1 if single else k.shape[2]
+    tail = (p.head_dim,) if single else (n, p.head_dim)
+    kv = (b, p.kv_heads) + tail
+    ks, vs = _rows(k, dev, dt, kv, "k"), _rows(v, dev, dt, kv, "v")
+    _check_dense(start, dev, torch.int32, (b,), "start")
     if new_len is not None:
-        _check_dense(new_len, torch.int32, "new_len", (p.batch,))
+        _check_dense(new_len, dev, torch.int32, (b,), "new_len")
     if len_out is not None:
-        _check_dense(len_out, torch.int32, "len_out", (p.batch,))
+        _check_dense(len_out, dev, torch.int32, (b,), "len_out")
     ps = None
     if positions is not None:
         shared = positions.dim() == 2
-        _check_here(positions, torch.int32, "positions", (p.batch, n) if shared else (p.batch, p.kv_heads, n))
+        _check(positions, dev, torch.int32, (b, n) if shared else (b, p.kv_heads, n), "positions")
         s = positions.stride()
-        ps = ems_strides(s[0], 0 if shared else s[1], s[-1])
+        ps = _strides(s[0], 0 if shared else s[1], s[-1])
     rot = 0
     if inv_freq is not None:
-        _check_dense(inv_freq, torch.float32, "inv_freq", (inv_freq.numel(),))
-        rot = 2 * inv_freq.numel()
+        rot = 2 * inv_freq.shape[0]
+        _check_dense(inv_freq, dev, torch.float32, (rot // 2,), "inv_freq")
     qs = qos = None
     if q is not None:
-        qs = _rows(q, p.q_heads, n, p, "q")
+        qt = (b, p.q_heads) + tail
+        qs = _rows(q, dev, dt, qt, "q")
         if q_out is None:
             q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        qos = _rows(q_out, p.q_heads, n, p, "q_out")
-        if q_out.dim() != q.dim() or any(m > 1 and step == 0 for m, step in zip(q_out.shape, q_out.stride())):
-            raise ValueError("q_out: a tensor of q's shape, every row in a place of its own")
+        qos = qs if q_out is q else _rows(q_out, dev, dt, qt, "q_out")
+        if not q_out.is_contiguous() and any(m > 1 and step == 0 for m, step in zip(q_out.shape, q_out.stride())):
+            raise ValueError("q_out: every row in a place of its own")
     elif q_out is not None:
         raise ValueError("q_out without q")
-    cp, cc = p.c(), cache.c()
-    ref = lambda x: None if x is None else C.byref(x)  # noqa: E731
-    rc = lib().ems_paged_append(C.byref(cp), C.byref(cc), n, _ptr(start), _ptr(new_len), _ptr(k), C.byref(ks), _ptr(v),
-                                C.byref(vs), _ptr(positions), ref(ps), _ptr(inv_freq), rot, int(bool(interleaved)),
-                                _ptr(q), ref(qs), _ptr(q_out), ref(qos), _ptr(len_out), _stream())
+    rc = lib().ems_paged_append(C.byref(p._c), cc, n, start.data_ptr(), _ptr(new_len), k.data_ptr(), ks, v.data_ptr(), vs,
+                                _ptr(positions), ps, _ptr(inv_freq), rot, 1 if interleaved else 0, _ptr(q), qs,
+                                _ptr(q_out), qos, _ptr(len_out), _stream())
     if rc != EMS_OK:
         raise EmsError(rc, "ems_paged_append")
     return q_out
@@ -691,8 +720,7 @@ def ems_paged_append(p: PagedParams, cache: PagedCache, start, k, v, positions=N
 
 def ems_paged_workspace_bytes(p: PagedParams) -> int:
     n = C.c_size_t(0)
-    cp = p.c()
-    rc = lib().ems_paged_workspace_bytes(C.byref(cp), C.byref(n))
+    rc = lib().ems_paged_workspace_bytes(C.byref(p._c), C.byref(n))
     if rc != EMS_OK:
         raise EmsError(rc, "ems_paged_workspace_bytes")
     return int(n.value)
@@ -701,18 +729,14 @@ def ems_paged_workspace_bytes(p: PagedParams) -> int:
 def ems_paged_attention(p: PagedParams, cache: PagedCache, lens, q, want_lse=False, ws=None, out=None):
     """Attention of one new token per sequence, q [B,Hq,D], over the first lens [B] int32 rows of its pages
     -> out [B,Hq,D] (or (out, lse [B,Hq] f32) with want_lse).  `out`: (out, lse or None) to write to."""
-    heads = (p.batch, p.q_heads)
-    _check_here(q, p.torch_dtype, "q", heads + (p.head_dim,))
-    s = q.stride()
-    if s[2] != 1:
-        raise ValueError("q: the elements of a row must be adjacent")
-    _check_dense(lens, torch.int32, "lens", (p.batch,))
-    cache._check(p)
-    ws = _check_ws(ws, ems_paged_workspace_bytes(p) if ws is None else 0, q.device)
-    o, lse = _attention_out(out, want_lse, heads, p.head_dim, p.torch_dtype, q.device)
-    cp, cc, cs = p.c(), cache.c(), ems_strides(s[0], s[1], 0)
-    rc = lib().ems_paged_attention(C.byref(cp), C.byref(cc), _ptr(lens), _ptr(q), C.byref(cs), _ptr(o), _ptr(lse),
-                                   _ptr(ws), ws.numel(), _stream())
+    dev = _current_device()
+    cc = cache._c(p, dev)
+    qs = _rows(q, dev, p.torch_dtype, p._q_row, "q")
+    _check_dense(lens, dev, torch.int32, (p.batch,), "lens")
+    ws = _check_ws(ws, dev, ems_paged_workspace_bytes, p)
+    o, lse = _attention_out(out, dev, want_lse, p._q_row, p.torch_dtype)
+    rc = lib().ems_paged_attention(C.byref(p._c), cc, lens.data_ptr(), q.data_ptr(), qs, o.data_ptr(), _ptr(lse),
+                                   ws.data_ptr(), ws.numel(), _stream())
     if rc != EMS_OK:
         raise EmsError(rc, "ems_paged_attention")
     return (o, lse) if want_lse else o

@@ -25,7 +25,7 @@ constexpr int kWaves = 4;
 constexpr int kNewRow = -2;      // the row of the new token itself (compact cache)
 constexpr int kNoRow = -1;
 
-constexpr int kLook = 64;                 // rows that a wave looks up at a time, a lane each
+constexpr int kLook = 32;                 // rows that a wave looks up at a time, a lane each
 constexpr int kUnit = kWaves * kLook;     // rows of a block's turn: what stretches are counted in
 
 template <typename T, int D> constexpr int kRowBytesOf = D * (int)sizeof(T);
@@ -39,23 +39,87 @@ __device__ __forceinline__ int live_len(const AttendArgs& a, bool table, int b)
 
 __device__ __forceinline__ int units_of(int len) { return (len + kUnit - 1) / kUnit; }
 
+// t / page_size: the magic number is 2^(31 + shift) / page_size, rounded up, with 2^shift >= page_size
+__device__ __forceinline__ int page_of(const AttendArgs& a, int t) { return (int)(__umulhi(2u * (unsigned)t, a.page_magic) >> a.page_shift); }
+
 // a value that is the same in every lane, for the scalar registers
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ long long uniform(long long x)
+
+// Inclusive sums over the lanes of a wave.
+template <int kCtrl, int kRowMask>
+__device__ __forceinline__ int dpp_or_zero(int v) { return __builtin_amdgcn_update_dpp(0, v, kCtrl, kRowMask, 0xf, false); }
+__device__ __forceinline__ int wave_scan(int v)
 {
-    return (long long)(unsigned)uniform((int)x) | (long long)uniform((int)(x >> 32)) << 32;
+    v += dpp_or_zero<0x111, 0xf>(v);       // one lane up inside each row of 16
+    v += dpp_or_zero<0x112, 0xf>(v);
+    v += dpp_or_zero<0x114, 0xf>(v);
+    v += dpp_or_zero<0x118, 0xf>(v);
+    v += dpp_or_zero<0x142, 0xa>(v);       // lane 15 of a row to the next row
+    v += dpp_or_zero<0x143, 0xc>(v);       // lane 31 to the upper half
+    return v;
 }
 
-// Units of sequences 0..b-1, or of all of them (b = batch); the same in every lane.
-__device__ __forceinline__ long long units_before(const AttendArgs& a, bool table, int b)
+// Workers share the units of a kv-head's sequences evenly: worker w takes `per` of them, one of the first `more` one more.
+struct Share {
+    int per, more, workers;
+    __device__ __forceinline__ Share(int total, int most) : per(total / most), more(total - per * most), workers(per ? most : more) {}
+    __device__ __forceinline__ int first_unit(int w) const { return w * per + min(w, more); }
+    __device__ __forceinline__ int worker_of(int unit) const
+    {
+        const int early = more * (per + 1);
+        return unit < early ? unit / (per + 1) : more + (unit - early) / per;
+    }
+};
+
+// The sequence of a worker's first unit, the units of those before it, its rows, and the worker's units; b = -1: it has none.
+struct Stretch { int b, before, len, u, u_end; };
+__device__ __forceinline__ Stretch stretch_of(const AttendArgs& a, bool table, int worker)
 {
-    if (table) return (long long)b * units_of(a.n_tok + 1);
+    if (table) {
+        const int len = a.n_tok + 1, n = units_of(len);
+        const Share share(n * a.batch, a.workers);
+        const int u = share.first_unit(worker);
+        return {worker < share.workers ? u / n : -1, u / n * n, len, u, share.first_unit(worker + 1)};
+    }
     const int lane = threadIdx.x % kWave;
-    long long n = 0;
-    for (int i = lane; i < b; i += kWave) n += units_of(live_len(a, table, i));
-#pragma unroll
-    for (int s = 1; s < kWave; s *= 2) n += __shfl_xor(n, s);
-    return uniform(n);
+    const int len0 = lane < a.batch ? live_len(a, table, lane) : 0, n0 = units_of(len0), sum0 = wave_scan(n0);
+    int total = 0;
+    for (int i = lane + kWave; i < a.batch; i += kWave) total += units_of(live_len(a, table, i));
+    total = __builtin_amdgcn_readlane(sum0, 63) + (a.batch > kWave ? __builtin_amdgcn_readlane(wave_scan(total), 63) : 0);
+    const Share share(total, a.workers);
+    Stretch s{-1, 0, 0, share.first_unit(worker), share.first_unit(worker + 1)};
+    if (worker >= share.workers) return s;
+    int len = len0, n = n0, sum = sum0;
+    for (int b0 = 0;;) {
+        const unsigned long long past = __ballot(sum > s.u);
+        if (past) {
+            const int at = __builtin_ctzll(past);
+            s.b = b0 + at;
+            s.before = __builtin_amdgcn_readlane(sum - n, at);
+            s.len = __builtin_amdgcn_readlane(len, at);
+            return s;
+        }
+        b0 += kWave;
+        if (b0 >= a.batch) return s;       // not for lengths that stay as they are
+        len = b0 + lane < a.batch ? live_len(a, table, b0 + lane) : 0;
+        n = units_of(len);
+        sum = __builtin_amdgcn_readlane(sum, 63) + wave_scan(n);
+    }
+}
+
+// Units of the sequences before b, and of all of them.
+struct Units { int before, total; };
+__device__ __forceinline__ Units count_units(const AttendArgs& a, bool table, int b)
+{
+    if (table) return {b * units_of(a.n_tok + 1), a.batch * units_of(a.n_tok + 1)};
+    const int lane = threadIdx.x % kWave;
+    int before = 0, total = 0;
+    for (int i = lane; i < a.batch; i += kWave) {
+        const int n = units_of(live_len(a, table, i));
+        total += n;
+        before += i < b ? n : 0;
+    }
+    return {__builtin_amdgcn_readlane(wave_scan(before), 63), __builtin_amdgcn_readlane(wave_scan(total), 63)};
 }
 
 // Max or sum over the four lanes l % 16 + 16 n that share a column.
@@ -69,7 +133,7 @@ __device__ __forceinline__ float column_reduce(float v)
 }  // namespace
 
 template <typename T, int D, bool kTable>
-__global__ __launch_bounds__(256, sizeof(T) == 2 && !(kTable && D == 128) ? 3 : 2) void attend_kernel(AttendArgs a)
+__global__ __launch_bounds__(256, 3) void attend_kernel(AttendArgs a)
 {
     constexpr int kTiles = kRowBytesOf<T, D> <= 256 ? 2 : 1;    // 16-row tiles of a step: their keys and values wait in registers
     constexpr int kStep = 16 * kTiles, kSteps = kLook / kStep;
@@ -88,40 +152,19 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && !(kTable && D == 128) ? 3 : 
 
     const int lane = threadIdx.x % kWave, wave = uniform((int)threadIdx.x / kWave);
     const int col = lane % 16, quad = lane / 16;
-    const int group_tiles = (a.group + kAttendQ - 1) / kAttendQ;
 
-    // which stretch: units [u, u_end) of the kv-head's sequences, one after the other
-    int b, tile, head, worker = 0;
-    long long u, u_end, base;                                  // base: units of the sequences before b
+    // which stretch: units [u, u_end) of the kv-head's sequences, one after the other; base: units of the sequences before b
+    const int head = blockIdx.y, tile = blockIdx.z, worker = a.workers ? blockIdx.x : 0;
+    int b = blockIdx.x, u = 0, u_end = 0, base = 0, len = 0;
     if (a.workers) {
-        worker = blockIdx.x % a.workers;
-        const int ht = blockIdx.x / a.workers;
-        head = ht % a.kv_heads; tile = ht / a.kv_heads;
-        const long long total = units_before(a, kTable, a.batch);
-        const long long workers = min((long long)a.workers, total);               // none without a unit
-        if (worker >= workers) return;
-        u = worker * total / workers;
-        u_end = (worker + 1) * total / workers;
-        base = 0;
-        for (b = 0; b < a.batch - 1; ++b) {
-            const int n = units_of(live_len(a, kTable, b));
-            if (u < base + n) break;
-            base += n;
-        }
-    } else {
-        b = blockIdx.x % a.batch;
-        const int ht = blockIdx.x / a.batch;
-        head = ht % a.kv_heads; tile = ht / a.kv_heads;
-        base = 0; u = 0;
-        u_end = units_of(live_len(a, kTable, b));
+        const Stretch s = stretch_of(a, kTable, worker);
+        if (s.b < 0) return;
+        b = s.b; base = s.before; len = s.len; u = s.u; u_end = s.u_end;
     }
-    (void)group_tiles;
     const int q0 = tile * kAttendQ, n_q = min(a.group - q0, kAttendQ);
 
-    do {
-        const int len = live_len(a, kTable, b);
-        const long long seq_units = units_of(len);
-        const long long first = u - base, last = min(u_end - base, seq_units);      // units of this sequence
+    for (;;) {
+        const int first = u - base;
         const int unit = b * a.kv_heads + head;
         const size_t q_head = (size_t)unit * a.group + q0;                          // = b * Hq + head * group + q0
 
@@ -152,13 +195,12 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && !(kTable && D == 128) ? 3 : 
 
         // Rows are looked up a batch of 64 ahead in two trips (the table; the position, or the norms), keys and values are
         // requested a step ahead, as soon as the registers that take them are free.
-        const int t_end = (int)min(last * kUnit, (long long)len);
-        const int t_first = (int)(first * kUnit) + wave * kLook + lane;
-        const int n_batches = t_end > t_first - lane ? (t_end - (t_first - lane) + kUnit - 1) / kUnit : 0;
+        const int t_first = first * kUnit + wave * kLook + lane % kLook;
+        int t_end = 0;                                         // set below: the first trip does not wait for the lengths
         struct Look { int row, mask; float norm; };            // mask: the position; norms of the token and of its row
         const auto table_trip = [&](int t) -> int {
             if constexpr (kTable) return t < a.n_tok ? a.tok_row[(size_t)unit * a.n_tok + t] : t == a.n_tok ? kNewRow : kNoRow;
-            return t < t_end ? a.page_table[(size_t)b * a.max_pages + t / a.page_size] : kNoRow;
+            return t < a.max_pages * a.page_size ? a.page_table[(size_t)b * a.max_pages + page_of(a, t)] : kNoRow;
         };
         const auto row_trip = [&](int t, int entry) -> Look {
             Look r{kNoRow, 0, 0.f};
@@ -170,22 +212,22 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && !(kTable && D == 128) ? 3 : 
                     r.mask = __builtin_bit_cast(int, a.tok_norm[(size_t)unit * a.n_tok + t]);
                 }
             } else if (t < t_end && entry >= 0 && entry < a.num_pages) {
-                r.row = (entry * a.kv_heads + head) * a.page_size + t % a.page_size;
+                r.row = (entry * a.kv_heads + head - page_of(a, t)) * a.page_size + t;       // t % page_size rows into the page
                 if (a.pos_pages) r.mask = a.pos_pages[r.row];
             }
             return r;
         };
-        // the batch's rows to LDS; which of them are live.  Dead rows are read as the first live one, which is in bounds
-        // and in the cache already (row 0 where none is live).
-        const auto settle = [&](int t, const Look& k, int buf) -> unsigned long long {
+        // The batch's rows to LDS; which of them are live.  Dead rows are read as the first live one, which is in the cache
+        // already and whose values may meet their zero weights (row 0 where none is live, whose steps are left out).
+        const auto settle = [&](int t, const Look& k, int buf) -> unsigned {
             int row = k.row;
             if constexpr (kTable) {
                 if (t >= t_end) row = kNoRow;
-                factor_of[wave][buf][lane] = row == kNewRow ? 1.f : k.norm > 0.f ? __builtin_bit_cast(float, k.mask) / k.norm : 0.f;
+                if (lane < kLook) factor_of[wave][buf][lane] = row == kNewRow ? 1.f : k.norm > 0.f ? __builtin_bit_cast(float, k.mask) / k.norm : 0.f;
             } else if (k.mask < 0) row = kNoRow;
-            const unsigned long long live = __ballot(row != kNoRow);
-            const int spare = live ? __builtin_amdgcn_readlane(row, __builtin_ctzll(live)) : 0;
-            row_of[wave][buf][lane] = row != kNoRow ? row : spare;
+            const unsigned live = (unsigned)__ballot(row != kNoRow);            // the upper lanes look up what others do
+            const int spare = live ? __builtin_amdgcn_readlane(row, __builtin_ctz(live)) : 0;
+            if (lane < kLook) row_of[wave][buf][lane] = row != kNoRow ? row : spare;
             __builtin_amdgcn_wave_barrier();
             return live;
         };
@@ -218,7 +260,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && !(kTable && D == 128) ? 3 : 
                 }
         };
         // one step on the rows in kf and vf, which the rows of (next_buf, next_at) then take
-        const auto step = [&](unsigned live, int buf, int at, int next_buf, int next_at) {
+        const auto step = [&](unsigned all_live, int buf, int at, int next_buf, int next_at) {
+            unsigned live = uniform((int)(kTiles == 2 ? all_live : all_live & 0xffff));
             f32x4_t s[kTiles];
 #pragma unroll
             for (int i = 0; i < kTiles; ++i) {
@@ -238,6 +281,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && !(kTable && D == 128) ? 3 : 
             __builtin_amdgcn_sched_barrier(0);
             load_keys(next_buf, next_at);
             __builtin_amdgcn_sched_barrier(0);
+            if (live) {                                        // (row 0 may hold anything)
             // logits in units of ln 2, dead rows -inf whatever their products are
             live >>= 4 * quad;
             float top = -INFINITY;
@@ -264,18 +308,6 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && !(kTable && D == 128) ? 3 : 
             for (int i = 0; i < kTiles; ++i)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) { s[i][r] = exp2_fast(s[i][r] - ref); l += s[i][r]; }
-            // what stands in a dead row must not meet its zero weight
-            constexpr unsigned kMine = kTiles == 2 ? 0x000f000f : 0xf;
-            if (!__all((live & kMine) == kMine)) {
-#pragma unroll
-                for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-#pragma unroll
-                        for (int h = 0; h < kParts; ++h)
-#pragma unroll
-                            for (int w = 0; w < kVec; ++w) vf[i][r][h][w] = (live >> (16 * i + r)) & 1 ? vf[i][r][h][w] : 0;
-            }
             if constexpr (sizeof(T) == 2) {
                 bf16x8_t high, rest;
 #pragma unroll
@@ -307,31 +339,52 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && !(kTable && D == 128) ? 3 : 
                                 o[4 * h + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], s[i][r], o[4 * h + e], 0, 0, 0);
                         }
             }
+            }
             __builtin_amdgcn_sched_barrier(0);
             load_values(next_buf, next_at);
             __builtin_amdgcn_sched_barrier(0);
         };
 
-        if (n_batches) {
-            int entry = table_trip(t_first);
-            unsigned long long live = settle(t_first, row_trip(t_first, entry), 0);
+        int entry = table_trip(t_first);
+        if (!a.workers) {
+            len = live_len(a, kTable, b);
+            u_end = units_of(len);
+        }
+        const int seq_units = units_of(len), last = min(u_end - base, seq_units);      // units of this sequence
+        t_end = min(last * kUnit, len);
+        if (t_end > t_first - lane % kLook) {
+            // whole batches, and as many steps of the last one as it has rows
+            const int rows = t_end - (t_first - lane % kLook), whole = (rows - 1) / kUnit;
+            const int n_steps = whole * kSteps + (min(rows - whole * kUnit, kLook) + kStep - 1) / kStep;
+            unsigned live = settle(t_first, row_trip(t_first, entry), 0);
             entry = table_trip(t_first + kUnit);
             load_keys(0, 0);
             load_values(0, 0);
-            for (int j = 0, t = t_first + kUnit; j < n_batches; ++j, t += kUnit) {          // t: the lane's row of batch j + 1
-                const int buf = j & 1;
-                const Look next = row_trip(t, entry);
-                entry = table_trip(t + kUnit);
-#pragma unroll
-                for (int i = 0; i < kSteps - 1; ++i) step((unsigned)(live >> (kStep * i)), buf, i, buf, i + 1);
-                const unsigned rest = (unsigned)(live >> (kLook - kStep));
-                live = settle(t, next, 1 - buf);
-                step(rest, buf, kSteps - 1, 1 - buf, 0);
+            Look next{kNoRow, 0, 0.f};
+#pragma unroll 1
+            for (int i = 0, t = t_first + kUnit; i < n_steps; ++i) {           // t: the lane's row of the next batch
+                const int at = i % kSteps, buf = i / kSteps & 1;
+                if (at == 0) {
+                    next = row_trip(t, entry);
+                    entry = table_trip(t + kUnit);
+                }
+                const bool turn = at == kSteps - 1;
+                const unsigned now = live >> (kStep * at);
+                if (turn) {
+                    live = settle(t, next, 1 - buf);
+                    t += kUnit;
+                }
+                step(now, buf, at, turn ? 1 - buf : buf, turn ? 0 : at + 1);
             }
         }
         l = column_reduce<false>(l);
 
+        {
         // the four waves' results.  Element r of tile e: column kCols (4 quad + r) + e, or 64 h + 4 (4 quad + r) + e % 4.
+        // (The thread's number is taken anew: what is derived from it would hold registers through the loop above.)
+        int tid = threadIdx.x;
+        asm volatile("" : "+v"(tid));
+        const int col = tid % 16, quad = tid % kWave / 16;
         if (quad == 0) { red_ml[wave][col][0] = m; red_ml[wave][col][1] = l; }
         if (col < n_q) {
 #pragma unroll
@@ -345,7 +398,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && !(kTable && D == 128) ? 3 : 
         __syncthreads();
         const bool whole = first == 0 && last == seq_units;
         const size_t part = a.workers ? (((size_t)tile * a.kv_heads + head) * a.workers + worker) * 2 + (first == 0) : 0;
-        for (int i = threadIdx.x; i < n_q * (D / 4); i += 256) {
+        for (int i = tid; i < n_q * (D / 4); i += 256) {
             const int q = i / (D / 4), d = i % (D / 4) * 4;
             float top = red_ml[0][q][0];
 #pragma unroll
@@ -371,66 +424,87 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && !(kTable && D == 128) ? 3 : 
             }
         }
         __syncthreads();
+        }
         base += seq_units;
         u = base;
-        ++b;
-    } while (u < u_end && b < a.batch);
+        if (u >= u_end || ++b >= a.batch) break;
+        len = live_len(a, kTable, b);
+    }
 }
 
-// One block per (sequence, q-head): kGroups groups of D / 4 lanes each take every kGroups-th worker.
+// A block takes join_q q-heads of a sequence; D / 4 lanes take a q-head's columns, and lanes that are left share its workers.
 template <typename T, int D, bool kTable>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a)
 {
-    constexpr int kLanes = D / 4, kGroups = 256 / kLanes;
-    __shared__ float red_ml[kGroups][2];
-    __shared__ __align__(16) float red_o[kGroups][D];
-    const int q_heads = a.kv_heads * a.group;
-    const int b = blockIdx.x / q_heads, qh = blockIdx.x % q_heads, head = qh / a.group, q = qh % a.group;
+    constexpr int kLanes = D / 4, kSlots = 256 / kLanes, kAhead = 4;
+    __shared__ float red_ml[kSlots][2];
+    __shared__ __align__(16) float red_o[kSlots][D];
+    const int b = blockIdx.x, head = blockIdx.y, q0 = blockIdx.z * a.join_q;                   // q0: of the group
     const int len = live_len(a, kTable, b);
-    T* out = reinterpret_cast<T*>(a.out) + (size_t)blockIdx.x * D;
+    const size_t q_head = ((size_t)b * a.kv_heads + head) * a.group + q0;
+    T* out = reinterpret_cast<T*>(a.out) + q_head * D;
     if (len == 0) {
-        if (threadIdx.x < D) out[threadIdx.x] = (T)0.f;
-        if (a.lse && threadIdx.x == 0) a.lse[blockIdx.x] = -INFINITY;
+        for (int i = threadIdx.x; i < a.join_q * D; i += 256) out[i] = (T)0.f;
+        if (a.lse && (int)threadIdx.x < a.join_q) a.lse[q_head + threadIdx.x] = -INFINITY;
         return;
     }
-    const long long total = units_before(a, kTable, a.batch), base = units_before(a, kTable, b);
-    // worker w takes units [w total / workers, (w + 1) total / workers)
-    const long long workers = min((long long)a.workers, total);
-    const auto worker_of = [&](long long unit) { return (int)(((unit + 1) * workers - 1) / total); };
-    const int w0 = worker_of(base), w1 = worker_of(base + units_of(len) - 1);
+    const Units units = count_units(a, kTable, b);
+    const Share share(units.total, a.workers);
+    const int w0 = share.worker_of(units.before), w1 = share.worker_of(units.before + units_of(len) - 1);
     if (w0 == w1) return;                                      // one worker had all of it
 
-    const int grp = threadIdx.x / kLanes, d = threadIdx.x % kLanes * 4;
-    const size_t at = ((size_t)(q / kAttendQ) * a.kv_heads + head) * a.workers;
-    float m = -INFINITY, l = 0.f;
-    f32x4_t x = {0.f, 0.f, 0.f, 0.f};
-    for (int w = w0 + grp; w <= w1; w += kGroups) {
-        const size_t part = ((at + w) * 2 + (w == w0)) * kAttendQ + q % kAttendQ;
-        const float mw = a.part_ml[part * 2], lw = a.part_ml[part * 2 + 1];
-        const f32x4_t xw = *reinterpret_cast<const f32x4_t*>(a.part_o + part * D + d);
-        const float m_new = fmaxf(m, mw), ref = m_new > -INFINITY ? m_new : 0.f;
-        const float f = exp2_fast(m - ref), fw = exp2_fast(mw - ref);
-        l = l * f + lw * fw;
-        x = x * f + xw * fw;
-        m = m_new;
+    const int per = kSlots / a.join_q;                         // lane groups of a q-head
+    const int slot = threadIdx.x / kLanes, d = threadIdx.x % kLanes * 4;
+    const int qi = slot / per, grp = slot % per, q = q0 + qi;
+    if (qi < a.join_q) {
+        const size_t at = ((size_t)(q / kAttendQ) * a.kv_heads + head) * a.workers;
+        float m = -INFINITY, l = 0.f;
+        f32x4_t x = {0.f, 0.f, 0.f, 0.f};
+        for (int w = w0 + grp; w <= w1; w += per * kAhead) {
+            float mw[kAhead], lw[kAhead];
+            f32x4_t xw[kAhead];
+            float top = m;
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int v = w + i * per;
+                const size_t part = ((at + min(v, w1)) * 2 + (v == w0)) * kAttendQ + q % kAttendQ;
+                mw[i] = a.part_ml[part * 2]; lw[i] = a.part_ml[part * 2 + 1];
+                xw[i] = *reinterpret_cast<const f32x4_t*>(a.part_o + part * D + d);
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                if (w + i * per > w1) { mw[i] = -INFINITY; lw[i] = 0.f; xw[i] = f32x4_t{0.f, 0.f, 0.f, 0.f}; }
+                top = fmaxf(top, mw[i]);
+            }
+            const float ref = top > -INFINITY ? top : 0.f, f = exp2_fast(m - ref);
+            l *= f;
+            x *= f;
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const float fw = exp2_fast(mw[i] - ref);
+                l += lw[i] * fw;
+                x += xw[i] * fw;
+            }
+            m = top;
+        }
+        if (d == 0) { red_ml[slot][0] = m; red_ml[slot][1] = l; }
+        *reinterpret_cast<f32x4_t*>(&red_o[slot][d]) = x;
     }
-    if (d == 0) { red_ml[grp][0] = m; red_ml[grp][1] = l; }
-    *reinterpret_cast<f32x4_t*>(&red_o[grp][d]) = x;
     __syncthreads();
-    if (threadIdx.x >= D) return;
-    float top = red_ml[0][0];
-#pragma unroll
-    for (int g = 1; g < kGroups; ++g) top = fmaxf(top, red_ml[g][0]);
-    const float ref = top > -INFINITY ? top : 0.f;
-    float sum = 0.f, y = 0.f;
-#pragma unroll
-    for (int g = 0; g < kGroups; ++g) {
-        const float f = exp2_fast(red_ml[g][0] - ref);
-        sum += f * red_ml[g][1];
-        y += f * red_o[g][threadIdx.x];
+    for (int i = threadIdx.x; i < a.join_q * D; i += 256) {
+        const int s0 = i / D * per, c = i % D;
+        float top = red_ml[s0][0];
+        for (int g = 1; g < per; ++g) top = fmaxf(top, red_ml[s0 + g][0]);
+        const float ref = top > -INFINITY ? top : 0.f;
+        float sum = 0.f, y = 0.f;
+        for (int g = 0; g < per; ++g) {
+            const float f = exp2_fast(red_ml[s0 + g][0] - ref);
+            sum += f * red_ml[s0 + g][1];
+            y += f * red_o[s0 + g][c];
+        }
+        out[i] = (T)(y * (sum == 0.f ? 0.f : 1.f / sum));
+        if (a.lse && c == 0) a.lse[q_head + i / D] = (ref + log2_fast(sum)) * 0.6931471805599453f;
     }
-    out[threadIdx.x] = (T)(y * (sum == 0.f ? 0.f : 1.f / sum));
-    if (a.lse && threadIdx.x == 0) a.lse[blockIdx.x] = (ref + log2_fast(sum)) * 0.6931471805599453f;
 }
 
 // Blocks that share the sequences of a kv-head evenly, or 0: a block per sequence.
@@ -444,13 +518,20 @@ int attend_workers(int batch, int kv_heads, int group, long long max_len)
 
 namespace {
 template <typename T, int D, bool kTable>
-hipError_t launch(const AttendArgs& a, hipStream_t st)
+hipError_t launch(AttendArgs a, hipStream_t st)
 {
+    a.page_shift = 0;
+    while (1 << a.page_shift < a.page_size) ++a.page_shift;
+    a.page_magic = a.page_table ? (unsigned)(((1ull << (31 + a.page_shift)) + a.page_size - 1) / a.page_size) : 0;
+    // q-heads of a join block: as many as it has lanes for, halved (to a divisor of the group) while there are few blocks
+    a.join_q = 1;
+    for (int n = 2; n <= 256 / (D / 4); ++n)
+        if (a.group % n == 0 && (long long)a.batch * a.kv_heads * (a.group / n) >= 512) a.join_q = n;
     const int tiles = (a.group + kAttendQ - 1) / kAttendQ;
-    attend_kernel<T, D, kTable><<<(a.workers ? a.workers : a.batch) * a.kv_heads * tiles, 256, 0, st>>>(a);
+    attend_kernel<T, D, kTable><<<dim3(a.workers ? a.workers : a.batch, a.kv_heads, tiles), 256, 0, st>>>(a);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && a.workers) {
-        attend_join_kernel<T, D, kTable><<<a.batch * a.kv_heads * a.group, 256, 0, st>>>(a);
+        attend_join_kernel<T, D, kTable><<<dim3(a.batch, a.kv_heads, a.group / a.join_q), 256, 0, st>>>(a);
         e = hipGetLastError();
     }
     return e;

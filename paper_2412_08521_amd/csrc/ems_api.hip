@@ -666,7 +666,8 @@ static bool paged_params_ok(const ems_paged_params* p, int* why)
     if (p->head_dim != 64 && p->head_dim != 128) return false;
     if ((long long)p->max_pages * p->page_size > (1ll << 30)) return false;
     if ((long long)p->num_pages * p->page_size > 0x7fffffffll / p->kv_heads) return false;     // 32-bit row numbers
-    if ((long long)p->batch * p->q_heads > (1 << 24)) return false;                            // grid of the attention
+    if ((long long)p->batch * p->q_heads > (1 << 24) || p->q_heads > 65535) return false;      // grid of the attention
+    if ((long long)p->batch * (((long long)p->max_pages * p->page_size + 255) / 256) > (1ll << 30)) return false;     // its units
     return true;
 }
 

@@ -205,6 +205,9 @@ struct AttendArgs {
     int workers;                // per kv-head and tile of q-heads: they share its sequences evenly; 0 = a block per sequence
     bool q_wide;                // q rows start at multiples of 16 bytes
     float scale_log2e;
+    unsigned page_magic;        // division by page_size (set by the launcher)
+    int page_shift;
+    int join_q;                 // q-heads of a join block (set by the launcher)
     float* part_o;              // [kv_heads * tiles, workers, 2, 16, D] what a worker found of a sequence it shares (workspace)
     float* part_ml;             // [.., 16, 2] its maximum and sum
 };

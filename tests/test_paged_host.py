@@ -118,14 +118,20 @@ def test_binding_refuses_host_tensors_and_other_shapes():
     cache = object.__new__(B.PagedCache)                      # a cache, had its tensors been a device's
     cache.k_pages, cache.v_pages, cache.page_table, cache.positions = k, k, table, None
     lens = torch.zeros(2, dtype=torch.int32)
+    q, kn = torch.zeros((2, 4, 128), dtype=torch.bfloat16), torch.zeros((2, 2, 128), dtype=torch.bfloat16)
+    cache.device_index = 77
+    for call in (lambda: B.ems_paged_attention(p, cache, lens, q), lambda: B.ems_paged_append(p, cache, lens, kn, kn)):
+        with pytest.raises(ValueError, match="the cache must be on the current device"):
+            call()
+    cache.device_index = B._current_device()
     with pytest.raises(ValueError, match="q must be a tensor of the current device"):
-        B.ems_paged_attention(p, cache, lens, torch.zeros((2, 4, 128), dtype=torch.bfloat16))
+        B.ems_paged_attention(p, cache, lens, q)
     with pytest.raises(ValueError, match="k must be a tensor of the current device"):
-        B.ems_paged_append(p, cache, lens, k, k)
+        B.ems_paged_append(p, cache, lens, kn, kn)
     for kw in (dict(num_pages=101), dict(page_size=32), dict(max_pages=51), dict(batch=1), dict(dtype=B.EMS_F32),
                dict(kv_heads=4), dict(head_dim=64)):
         with pytest.raises(ValueError, match="does not fit"):
-            cache._check(_paged(**kw))
+            cache._c(_paged(**kw), cache.device_index)
 
 
 # ---- the plain forms themselves
