@@ -132,9 +132,10 @@ __device__ __forceinline__ float column_reduce(float v)
 
 }  // namespace
 
-template <typename T, int D, bool kTable>
-__global__ __launch_bounds__(256, 3) void attend_kernel(AttendArgs a)
+template <typename T, int D, bool kTable, int kW>
+__global__ __launch_bounds__(64 * kW, (kW == 4 ? 3 : kW / 4)) void attend_kernel(AttendArgs a)
 {
+    constexpr int kTurn = kW * kLook;                          // rows of a block's turn
     constexpr int kTiles = kRowBytesOf<T, D> <= 256 ? 2 : 1;    // 16-row tiles of a step: their keys and values wait in registers
     constexpr int kStep = 16 * kTiles, kSteps = kLook / kStep;
     constexpr int kPieces = D * (int)sizeof(T) / 64;           // 16-byte pieces of a key row that a lane reads
@@ -145,18 +146,20 @@ __global__ __launch_bounds__(256, 3) void attend_kernel(AttendArgs a)
     constexpr int kVec = sizeof(T) == 2 ? kCols / 2 : 4;       // dwords
     constexpr int kParts = sizeof(T) == 2 ? 1 : D / 64;
     typedef int vec_t __attribute__((ext_vector_type(kVec)));
-    __shared__ __align__(16) int row_of[kWaves][2][kLook];
-    __shared__ __align__(16) float factor_of[kWaves][2][kTable ? kLook : 4];
-    __shared__ __align__(16) float red_o[kWaves][kAttendQ][D + 4];
-    __shared__ float red_ml[kWaves][kAttendQ][2];
+    __shared__ __align__(16) int row_of[kW][2][kLook];
+    __shared__ __align__(16) float factor_of[kW][2][kTable ? kLook : 4];
+    __shared__ __align__(16) float red_o[kW][kAttendQ][D + 4];
+    __shared__ float red_ml[kW][kAttendQ][2];
 
+    const auto turns_of = [](int n) { return (n + kTurn - 1) / kTurn; };
     const int lane = threadIdx.x % kWave, wave = uniform((int)threadIdx.x / kWave);
     const int col = lane % 16, quad = lane / 16;
 
     // which stretch: units [u, u_end) of the kv-head's sequences, one after the other; base: units of the sequences before b
-    const int head = blockIdx.y, tile = blockIdx.z, worker = a.workers ? blockIdx.x : 0;
+    const bool shared = kW == kWaves && a.workers;             // else a block per sequence
+    const int head = blockIdx.y, tile = blockIdx.z, worker = shared ? blockIdx.x : 0;
     int b = blockIdx.x, u = 0, u_end = 0, base = 0, len = 0;
-    if (a.workers) {
+    if (shared) {
         const Stretch s = stretch_of(a, kTable, worker);
         if (s.b < 0) return;
         b = s.b; base = s.before; len = s.len; u = s.u; u_end = s.u_end;
@@ -195,7 +198,7 @@ __global__ __launch_bounds__(256, 3) void attend_kernel(AttendArgs a)
 
         // Rows are looked up a batch of 64 ahead in two trips (the table; the position, or the norms), keys and values are
         // requested a step ahead, as soon as the registers that take them are free.
-        const int t_first = first * kUnit + wave * kLook + lane % kLook;
+        const int t_first = first * kTurn + wave * kLook + lane % kLook;
         int t_end = 0;                                         // set below: the first trip does not wait for the lengths
         struct Look { int row, mask; float norm; };            // mask: the position; norms of the token and of its row
         const auto table_trip = [&](int t) -> int {
@@ -346,33 +349,33 @@ __global__ __launch_bounds__(256, 3) void attend_kernel(AttendArgs a)
         };
 
         int entry = table_trip(t_first);
-        if (!a.workers) {
+        if (!shared) {
             len = live_len(a, kTable, b);
-            u_end = units_of(len);
+            u_end = turns_of(len);
         }
-        const int seq_units = units_of(len), last = min(u_end - base, seq_units);      // units of this sequence
-        t_end = min(last * kUnit, len);
+        const int seq_units = turns_of(len), last = min(u_end - base, seq_units);      // units of this sequence
+        t_end = min(last * kTurn, len);
         if (t_end > t_first - lane % kLook) {
             // whole batches, and as many steps of the last one as it has rows
-            const int rows = t_end - (t_first - lane % kLook), whole = (rows - 1) / kUnit;
-            const int n_steps = whole * kSteps + (min(rows - whole * kUnit, kLook) + kStep - 1) / kStep;
+            const int rows = t_end - (t_first - lane % kLook), whole = (rows - 1) / kTurn;
+            const int n_steps = whole * kSteps + (min(rows - whole * kTurn, kLook) + kStep - 1) / kStep;
             unsigned live = settle(t_first, row_trip(t_first, entry), 0);
-            entry = table_trip(t_first + kUnit);
+            entry = table_trip(t_first + kTurn);
             load_keys(0, 0);
             load_values(0, 0);
             Look next{kNoRow, 0, 0.f};
 #pragma unroll 1
-            for (int i = 0, t = t_first + kUnit; i < n_steps; ++i) {           // t: the lane's row of the next batch
+            for (int i = 0, t = t_first + kTurn; i < n_steps; ++i) {           // t: the lane's row of the next batch
                 const int at = i % kSteps, buf = i / kSteps & 1;
                 if (at == 0) {
                     next = row_trip(t, entry);
-                    entry = table_trip(t + kUnit);
+                    entry = table_trip(t + kTurn);
                 }
                 const bool turn = at == kSteps - 1;
                 const unsigned now = live >> (kStep * at);
                 if (turn) {
                     live = settle(t, next, 1 - buf);
-                    t += kUnit;
+                    t += kTurn;
                 }
                 step(now, buf, at, turn ? 1 - buf : buf, turn ? 0 : at + 1);
             }
@@ -397,17 +400,17 @@ __global__ __launch_bounds__(256, 3) void attend_kernel(AttendArgs a)
         }
         __syncthreads();
         const bool whole = first == 0 && last == seq_units;
-        const size_t part = a.workers ? (((size_t)tile * a.kv_heads + head) * a.workers + worker) * 2 + (first == 0) : 0;
-        for (int i = tid; i < n_q * (D / 4); i += 256) {
+        const size_t part = shared ? (((size_t)tile * a.kv_heads + head) * a.workers + worker) * 2 + (first == 0) : 0;
+        for (int i = tid; i < n_q * (D / 4); i += 64 * kW) {
             const int q = i / (D / 4), d = i % (D / 4) * 4;
             float top = red_ml[0][q][0];
 #pragma unroll
-            for (int w = 1; w < kWaves; ++w) top = fmaxf(top, red_ml[w][q][0]);
+            for (int w = 1; w < kW; ++w) top = fmaxf(top, red_ml[w][q][0]);
             const float ref = top > -INFINITY ? top : 0.f;
             float sum = 0.f;
             f32x4_t x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) {
+            for (int w = 0; w < kW; ++w) {
                 const float f = exp2_fast(red_ml[w][q][0] - ref);
                 sum += f * red_ml[w][q][1];
                 x += f * *reinterpret_cast<const f32x4_t*>(&red_o[w][q][d]);
@@ -508,12 +511,18 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a)
 }
 
 // Blocks that share the sequences of a kv-head evenly, or 0: a block per sequence.
-int attend_workers(int batch, int kv_heads, int group, long long max_len)
+//
+// Sharing costs the join's launch, 5 us, and a share is a whole number of units; a block of its own has one compute unit's
+// bandwidth, some 50 GB/s against 6.2 TB/s of all.  So a block per sequence while the longest that the table admits is
+// 256 KB of keys and values (us, block per sequence / shared, one sequence of 8 heads, head size 128: 512 rows 10.5 /
+// 11.8, 1024 rows 16.0 / 12.1; 4 heads of 64: 512 rows 8.2 / 10.7, 1024 rows 11.2 / 10.6), and up to 1 MB while there is
+// a block for every compute unit (32 sequences of 8 heads and 1024 rows 26.9 / 34.8, 2048 rows 49.7 / 58.2; 2048 rows at
+// most, lengths spread evenly: 34.6 / 36.1; 64 such sequences 63.3 / 61.0).
+int attend_workers(int batch, int kv_heads, int group, long long max_len, int row_bytes)
 {
-    if (max_len <= 256) return 0;
     const long long columns = (long long)kv_heads * ((group + kAttendQ - 1) / kAttendQ);
-    const long long want = (768 + columns - 1) / columns;      // three blocks a compute unit
-    return (int)want;
+    if (max_len * 2 * row_bytes <= (columns * batch >= 256 ? 1 << 20 : 1 << 18)) return 0;
+    return (int)((768 + columns - 1) / columns);               // three blocks a compute unit
 }
 
 namespace {
@@ -528,7 +537,15 @@ hipError_t launch(AttendArgs a, hipStream_t st)
     for (int n = 2; n <= 256 / (D / 4); ++n)
         if (a.group % n == 0 && (long long)a.batch * a.kv_heads * (a.group / n) >= 512) a.join_q = n;
     const int tiles = (a.group + kAttendQ - 1) / kAttendQ;
-    attend_kernel<T, D, kTable><<<dim3(a.workers ? a.workers : a.batch, a.kv_heads, tiles), 256, 0, st>>>(a);
+    const long long max_len = kTable ? a.n_tok + 1 : (long long)a.max_pages * a.page_size;
+    constexpr int kWide = kRowBytesOf<T, D> <= 128 ? 16 : 8;
+    // A block per sequence has eight waves (or 16, as the registers allow) where it would need several turns of four, and
+    // there is less than two blocks' work for a compute unit (us at 8 heads of 128 and 512 rows, eight waves / four:
+    // 16 sequences 11.5 / 12.4, 32 15.2 / 15.8, 64 29.7 / 27.5, 128 56.6 / 50.4).
+    if (!a.workers && max_len > kUnit && (long long)a.batch * a.kv_heads * tiles < 512)
+        attend_kernel<T, D, kTable, kWide><<<dim3(a.batch, a.kv_heads, tiles), 64 * kWide, 0, st>>>(a);
+    else
+        attend_kernel<T, D, kTable, kWaves><<<dim3(a.workers ? a.workers : a.batch, a.kv_heads, tiles), 256, 0, st>>>(a);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && a.workers) {
         attend_join_kernel<T, D, kTable><<<dim3(a.batch, a.kv_heads, a.group / a.join_q), 256, 0, st>>>(a);

@@ -595,10 +595,10 @@ static bool wide_rows(const void* p, const ems_strides& s, bool f32)
 // Attention workspace: what the workers of a kv-head found of sequences that they share, two of them at most.
 struct AttendPlan { int workers; size_t off_ml, total; };
 
-static AttendPlan plan_attend(int batch, int kv_heads, int group, int head_dim, long long max_len)
+static AttendPlan plan_attend(int batch, int kv_heads, int group, int head_dim, long long max_len, int dtype)
 {
     AttendPlan a{};
-    a.workers = ems::attend_workers(batch, kv_heads, group, max_len);
+    a.workers = ems::attend_workers(batch, kv_heads, group, max_len, head_dim * (dtype == EMS_F32 ? 4 : 2));
     const int tiles = (group + ems::kAttendQ - 1) / ems::kAttendQ;
     const size_t parts = (size_t)kv_heads * tiles * a.workers * 2 * ems::kAttendQ;
     a.off_ml = align_up(sizeof(float) * parts * head_dim);
@@ -620,7 +620,7 @@ static AttendPlan plan_decode_attention(const ems_params* p)
 {
     int n_imp, n_tbm;
     partition_sizes(p, &n_imp, &n_tbm);
-    return plan_attend(p->batch, p->kv_heads, p->q_heads / p->kv_heads, p->head_dim, (long long)n_imp + n_tbm + p->window + 1);
+    return plan_attend(p->batch, p->kv_heads, p->q_heads / p->kv_heads, p->head_dim, (long long)n_imp + n_tbm + p->window + 1, p->dtype);
 }
 
 int ems_decode_attention_workspace_bytes(const ems_params* p, size_t* attention_ws)
@@ -719,7 +719,7 @@ int ems_paged_append(const ems_paged_params* p, const ems_paged_cache* cache, in
 
 static AttendPlan plan_paged(const ems_paged_params* p)
 {
-    return plan_attend(p->batch, p->kv_heads, p->q_heads / p->kv_heads, p->head_dim, (long long)p->max_pages * p->page_size);
+    return plan_attend(p->batch, p->kv_heads, p->q_heads / p->kv_heads, p->head_dim, (long long)p->max_pages * p->page_size, p->dtype);
 }
 
 int ems_paged_workspace_bytes(const ems_paged_params* p, size_t* attention_ws)

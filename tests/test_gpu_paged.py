@@ -233,7 +233,8 @@ def _attend_case(b, hq, hkv, d, ps, lens, mode, masked=None, columns=None, layou
 
 
 ATTEND = [
-    # (b, hq, hkv, d, ps, lens): one block a sequence (tables of up to 256 rows), then shared by several
+    # (b, hq, hkv, d, ps, lens): a block per sequence of one turn, of several turns (eight waves or 16; four where there
+    # are 512 blocks), then sequences that blocks share (test_paged_host holds which is which)
     (1, 1, 1, 64, 16, [1]),
     (4, 4, 4, 64, 16, [0, 1, 16, 17]),
     (3, 8, 2, 128, 16, [256, 255, 65]),
@@ -249,6 +250,9 @@ ATTEND = [
     (5, 2, 2, 128, 16, [0, 2500, 0, 300, 1]),
     (2, 40, 2, 64, 5, [1200, 40]),
     (40, 2, 1, 64, 16, [(37 * i * i) % 700 for i in range(40)]),
+    (130, 8, 4, 64, 16, [(53 * i * i) % 300 for i in range(130)]),
+    (70, 2, 1, 64, 16, [0, 1100] + [(31 * i * i) % 900 for i in range(68)]),
+    (150, 1, 1, 128, 32, [0] * 70 + [1200, 3] + [(7 * i) % 40 for i in range(77)] + [700]),
 ]
 
 

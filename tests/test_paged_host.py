@@ -77,10 +77,20 @@ def test_attention_arguments():
         assert _attend(p, **kw) == WORKSPACE, kw
 
 
-def test_workspace_of_one_block_per_sequence_is_empty():
-    assert B.ems_paged_workspace_bytes(_paged(max_pages=16)) == 0
-    p = B.EmsParams(1, 4, 2, 64, 4096, 16, 100, merge_ratio=0.5)
-    assert B.ems_decode_attention_workspace_bytes(p) == 0
+def test_which_calls_share_sequences_between_blocks():
+    """A workspace is needed where they do: sequences over 256 KB of keys and values, over 1 MB where the blocks of whole
+    sequences are 256 or more."""
+    def shared(rows, **kw):
+        return B.ems_paged_workspace_bytes(_paged(page_size=1, max_pages=rows, **kw)) > 0
+    assert not shared(512) and shared(513)                                               # 512 bytes a row
+    assert not shared(1024, head_dim=64) and shared(1025, head_dim=64)
+    assert not shared(512, head_dim=64, dtype=B.EMS_F32) and shared(513, head_dim=64, dtype=B.EMS_F32)
+    for more in (dict(batch=128), dict(batch=32, q_heads=8, kv_heads=8), dict(batch=64, q_heads=34)):    # the last: two tiles of q-heads
+        assert not shared(2048, **more) and shared(2049, **more)
+    assert shared(2048, batch=127)
+    p = lambda budget, ratio, n=1 << 16: B.EmsParams(1, 4, 2, 64, n, 16, budget, merge_ratio=ratio)  # noqa: E731
+    need = B.ems_decode_attention_workspace_bytes
+    assert need(p(682, 0.5)) == 0 and need(p(683, 0.5)) > 0                              # 1023 and 1024 elements and the new token
 
 
 def test_decode_attention_arguments():
