@@ -11,17 +11,20 @@ namespace ems {
 
 namespace {
 
-// 8 elements of a row as they are; `wide`: the address is a multiple of 16 bytes
+// 8 elements of a row as they are; `wide`: the address is a multiple of 16 bytes; kPast: past the caches (nontemporal)
 template <typename T> struct Piece { frag_t f[8 * sizeof(T) / 16]; };
 template <typename T> struct Elems { T x[8]; };
 
-template <typename T>
+template <typename T, bool kPast>
 __device__ __forceinline__ Piece<T> load_piece(const T* p, bool wide)
 {
     Piece<T> r;
     if (wide) {
 #pragma unroll
-        for (int i = 0; i < (int)(sizeof(r) / 16); ++i) r.f[i] = reinterpret_cast<const frag_t*>(p)[i];
+        for (int i = 0; i < (int)(sizeof(r) / 16); ++i) {
+            const frag_t* at = reinterpret_cast<const frag_t*>(p) + i;
+            r.f[i] = kPast ? __builtin_nontemporal_load(at) : *at;
+        }
     } else {
         Elems<T> e;
 #pragma unroll
@@ -31,12 +34,16 @@ __device__ __forceinline__ Piece<T> load_piece(const T* p, bool wide)
     return r;
 }
 
-template <typename T>
+template <typename T, bool kPast>
 __device__ __forceinline__ void store_piece(T* p, bool wide, const Piece<T>& r)
 {
     if (wide) {
 #pragma unroll
-        for (int i = 0; i < (int)(sizeof(r) / 16); ++i) reinterpret_cast<frag_t*>(p)[i] = r.f[i];
+        for (int i = 0; i < (int)(sizeof(r) / 16); ++i) {
+            frag_t* at = reinterpret_cast<frag_t*>(p) + i;
+            if constexpr (kPast) __builtin_nontemporal_store(r.f[i], at);
+            else *at = r.f[i];
+        }
     } else {
         const Elems<T> e = __builtin_bit_cast(Elems<T>, r);
 #pragma unroll
@@ -83,92 +90,132 @@ __device__ __forceinline__ void rotate(float& u, float& w, float c, float s)
 
 }  // namespace
 
-// A thread takes 16 elements of one row: the two halves of 8 pairs (or 16 elements that only move).  It reads them all
-// before it writes any, so queries may be turned in place.
-template <typename T, int D>
+// A block takes up to 16 tokens and the rows (queries, keys, values) of some kv-heads.  Its angles are formed once, a value a
+// thread, and shared through LDS: formed by every thread for its own row they were what a prompt waited for (four prompts
+// of 8192 tokens, 40 heads to rotate: 187 us, of which ~150 were vector instructions).  Then a lane group of D / 16 lanes
+// takes a row, a lane the two halves of 8 pairs (or 16 elements that only move), kAhead rows requested together; a lane
+// reads all of its elements before it writes any, so queries may be turned in place.
+template <typename T, int D, bool kPast>
 __global__ __launch_bounds__(256) void append_kernel(AppendArgs a)
 {
-    constexpr int kItems = D / 16;
-    const int rows = a.q_heads_used + 2 * a.kv_heads;                          // of one token: queries, keys, values
-    const long long idx = (long long)blockIdx.x * 256 + threadIdx.x;
-    const int item = (int)(idx % kItems);
-    const long long rest = idx / kItems;
-    const int row = (int)(rest % rows);
-    const long long token = rest / rows;
-    if (token >= (long long)a.batch * a.n_new) return;
-    const int b = (int)(token / a.n_new), i = (int)(token % a.n_new);
+    constexpr int kItems = D / 16, kGroups = 256 / kItems, kAhead = 4;
+    __shared__ __align__(16) float cs[kAppendTokens][2][D / 2];
+    const int n_tok = a.tokens;                                // of a block: a power of two
+    const int h0 = blockIdx.y * a.heads, heads = min(a.heads, a.kv_heads - h0);       // its kv-heads
+    const int tok0 = blockIdx.x * n_tok, all = a.batch * a.n_new;
+    const auto place = [&](int token, int& b, int& i) { b = token / a.n_new; i = token - b * a.n_new; };
+    const auto position = [&](int b, int i) -> double {
+        if (a.positions) return a.positions[b * a.pos_sb + h0 * a.pos_sh + i * a.pos_sn];       // (one head where each has its own)
+        return (double)a.start[b] + i;
+    };
+    const int half = a.rot / 2;
+    for (int x = threadIdx.x; x < n_tok * half; x += 256) {
+        const int t = x / half, e = x - t * half;
+        int b, i;
+        place(min(tok0 + t, all - 1), b, i);
+        turn(position(b, i), a.inv_freq[e], cs[t][0][e], cs[t][1][e]);
+    }
+    __syncthreads();
 
+    const int item = threadIdx.x % kItems, group = threadIdx.x / kItems, t = group % n_tok;
+    if (tok0 + t >= all) return;
+    int b, i;
+    place(tok0 + t, b, i);
     const int n = a.new_len ? min(max(a.new_len[b], 0), a.n_new) : a.n_new;
     const long long capacity = (long long)a.max_pages * a.page_size;
     const long long slot = (long long)a.start[b] + i;
-    if (a.len_out && i == 0 && row == 0 && item == 0)
+    if (a.len_out && i == 0 && h0 == 0 && group < n_tok && item == 0)
         a.len_out[b] = (int)min(max((long long)a.start[b] + n, 0ll), capacity);
     if (i >= n) return;
 
-    const bool is_q = row < a.q_heads_used, is_k = !is_q && row < a.q_heads_used + a.kv_heads;
-    const int head = is_q ? row : is_k ? row - a.q_heads_used : row - a.q_heads_used - a.kv_heads;
-    const int kv_head = is_q ? head / a.group : head;
-
-    T* dst;
-    long long at = 0;
-    bool wide_out = true;
-    if (is_q) {
-        dst = reinterpret_cast<T*>(a.q_out) + b * a.qo_sb + head * a.qo_sh + i * a.qo_sn;
-        wide_out = a.qo_wide;
-    } else {
-        if (slot < 0 || slot >= capacity) return;
-        const int page = a.page_table[(size_t)b * a.max_pages + (int)(slot / a.page_size)];
-        if (page < 0 || page >= a.num_pages) return;
-        at = ((long long)page * a.kv_heads + head) * a.page_size + slot % a.page_size;
-        dst = reinterpret_cast<T*>(is_k ? a.k_pages : a.v_pages) + at * D;
+    // the token's row in the cache, of kv-head 0; none: only its queries are turned
+    long long at = -1;
+    if (slot >= 0 && slot < capacity) {
+        const int page = a.page_table[(size_t)b * a.max_pages + (int)slot / a.page_size];
+        if (page >= 0 && page < a.num_pages) at = (long long)page * a.kv_heads * a.page_size + (int)slot % a.page_size;
     }
-    const T* src = is_q   ? reinterpret_cast<const T*>(a.q) + b * a.q_sb + head * a.q_sh + i * a.q_sn
-                   : is_k ? reinterpret_cast<const T*>(a.k) + b * a.k_sb + head * a.k_sh + i * a.k_sn
-                          : reinterpret_cast<const T*>(a.v) + b * a.v_sb + head * a.v_sh + i * a.v_sn;
-    const bool wide_in = is_q ? a.q_wide : is_k ? a.k_wide : a.v_wide;
-
-    const double pos = a.positions ? (double)a.positions[b * a.pos_sb + kv_head * a.pos_sh + i * a.pos_sn] : (double)slot;
-    if (is_k && item == 0 && a.pos_pages) a.pos_pages[at] = (int)pos;
-
     const bool paired = item < a.rot / 16;
-    const bool halves = paired && !a.interleaved;                              // 8 columns of each half, else 16 in a row
-    const int e0 = halves ? 8 * item : 16 * item, e1 = halves ? 8 * item + a.rot / 2 : 16 * item + 8;
-    Piece<T> p0 = load_piece(src + e0, wide_in), p1 = load_piece(src + e1, wide_in);
-    if (paired && (is_q || is_k)) {
-        float x[8], y[8], c[8], s[8];
-        unpack8(p0, x);
-        unpack8(p1, y);
+    const bool halves = paired && !a.interleaved;              // 8 columns of each half, else 16 in a row
+    const int e0 = halves ? 8 * item : 16 * item, e1 = halves ? 8 * item + half : 16 * item + 8;
+    float c[8], s[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) turn(pos, a.inv_freq[8 * item + e], c[e], s[e]);
-        if (halves) {
+    for (int e = 0; e < 8; ++e) { c[e] = paired ? cs[t][0][8 * item + e] : 1.f; s[e] = paired ? cs[t][1][8 * item + e] : 0.f; }
+
+    const int n_q = a.q ? heads * a.group : 0, rows = n_q + 2 * heads;
+    const T* q_in = reinterpret_cast<const T*>(a.q) + b * a.q_sb + (long long)h0 * a.group * a.q_sh + i * a.q_sn;
+    T* q_out = reinterpret_cast<T*>(a.q_out) + b * a.qo_sb + (long long)h0 * a.group * a.qo_sh + i * a.qo_sn;
+    const T* k_in = reinterpret_cast<const T*>(a.k) + b * a.k_sb + h0 * a.k_sh + i * a.k_sn;
+    const T* v_in = reinterpret_cast<const T*>(a.v) + b * a.v_sb + h0 * a.v_sh + i * a.v_sn;
+    const int step = kGroups / n_tok;
+    for (int r0 = group / n_tok; r0 < rows; r0 += kAhead * step) {
+        Piece<T> p0[kAhead], p1[kAhead];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) rotate(x[e], y[e], c[e], s[e]);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                rotate(x[2 * e], x[2 * e + 1], c[e], s[e]);
-                rotate(y[2 * e], y[2 * e + 1], c[e + 4], s[e + 4]);
-            }
+        for (int u = 0; u < kAhead; ++u) {
+            const int r = r0 + u * step, k = r - n_q, v = k - heads;
+            if (r >= rows || (r >= n_q && at < 0)) continue;
+            const T* src = r < n_q ? q_in + r * a.q_sh : v < 0 ? k_in + k * a.k_sh : v_in + v * a.v_sh;
+            const bool wide = r < n_q ? a.q_wide : v < 0 ? a.k_wide : a.v_wide;
+            p0[u] = load_piece<T, kPast>(src + e0, wide);
+            p1[u] = load_piece<T, kPast>(src + e1, wide);
         }
-        p0 = pack8<T>(x);
-        p1 = pack8<T>(y);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int r = r0 + u * step, k = r - n_q, v = k - heads;
+            if (r >= rows || (r >= n_q && at < 0)) continue;
+            if (paired && v < 0) {
+                float x[8], y[8];
+                unpack8(p0[u], x);
+                unpack8(p1[u], y);
+                if (halves) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) rotate(x[e], y[e], c[e], s[e]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        rotate(x[2 * e], x[2 * e + 1], c[e], s[e]);
+                        rotate(y[2 * e], y[2 * e + 1], c[e + 4], s[e + 4]);
+                    }
+                }
+                p0[u] = pack8<T>(x);
+                p1[u] = pack8<T>(y);
+            }
+            const long long row = at + (long long)(h0 + (v < 0 ? k : v)) * a.page_size;
+            T* dst = r < n_q ? q_out + r * a.qo_sh : reinterpret_cast<T*>(v < 0 ? a.k_pages : a.v_pages) + row * D;
+            const bool wide = r >= n_q || a.qo_wide;
+            store_piece<T, kPast>(dst + e0, wide, p0[u]);
+            store_piece<T, kPast>(dst + e1, wide, p1[u]);
+            if (a.pos_pages && r >= n_q && v < 0 && item == 0)
+                a.pos_pages[row] = a.positions ? a.positions[b * a.pos_sb + (h0 + k) * a.pos_sh + i * a.pos_sn] : (int)slot;
+        }
     }
-    store_piece(dst + e0, wide_out, p0);
-    store_piece(dst + e1, wide_out, p1);
 }
+
+namespace {
+template <typename T, int D>
+hipError_t launch(AppendArgs a, hipStream_t st)
+{
+    const long long all = (long long)a.batch * a.n_new;
+    // What the last-level cache (256 MB) cannot hold goes past it: four prompts of 8192 tokens (805 MB) take 156 us instead
+    // of 168, 100 MB 38 instead of 23, whose pages stay for the attention that reads them.
+    const bool past = 2ll * D * (long long)sizeof(T) * all * ((a.q ? a.kv_heads * a.group : 0) + 2 * a.kv_heads) > 256ll << 20;
+    // Tokens and kv-heads of a block: all heads of 16 tokens (of 8 in long prompts, 168 / 182 us), fewer, heads first,
+    // until there are two blocks a compute unit.  Where heads have positions of their own and there is a rotation, a block has one.
+    a.tokens = past ? kAppendTokens / 2 : kAppendTokens;
+    a.heads = a.pos_sh != 0 && a.rot ? 1 : a.kv_heads;
+    const auto blocks = [&] { return (all + a.tokens - 1) / a.tokens * ((a.kv_heads + a.heads - 1) / a.heads); };
+    while (a.heads > 1 && blocks() < 512) a.heads = (a.heads + 1) / 2;
+    while (a.tokens > 1 && blocks() < 512) a.tokens /= 2;
+    const dim3 grid((unsigned)((all + a.tokens - 1) / a.tokens), (a.kv_heads + a.heads - 1) / a.heads);
+    if (past) append_kernel<T, D, true><<<grid, 256, 0, st>>>(a);
+    else append_kernel<T, D, false><<<grid, 256, 0, st>>>(a);
+    return hipGetLastError();
+}
+}  // namespace
 
 hipError_t launch_append(const AppendArgs& a, int head_dim, bool f32, hipStream_t st)
 {
-    const long long threads = (long long)a.batch * a.n_new * (a.q_heads_used + 2 * a.kv_heads) * (head_dim / 16);
-    const dim3 grid((unsigned)((threads + 255) / 256));
-    if (f32) {
-        if (head_dim == 64) append_kernel<float, 64><<<grid, 256, 0, st>>>(a);
-        else append_kernel<float, 128><<<grid, 256, 0, st>>>(a);
-    } else {
-        if (head_dim == 64) append_kernel<bf16_t, 64><<<grid, 256, 0, st>>>(a);
-        else append_kernel<bf16_t, 128><<<grid, 256, 0, st>>>(a);
-    }
-    return hipGetLastError();
+    if (f32) return head_dim == 64 ? launch<float, 64>(a, st) : launch<float, 128>(a, st);
+    return head_dim == 64 ? launch<bf16_t, 64>(a, st) : launch<bf16_t, 128>(a, st);
 }
 
 }  // namespace ems

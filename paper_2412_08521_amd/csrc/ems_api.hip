@@ -704,7 +704,6 @@ int ems_paged_append(const ems_paged_params* p, const ems_paged_cache* cache, in
         a.q_wide = wide_rows(q_opt, *q_strides, f32);
         a.q_out = q_out; a.qo_sb = q_out_strides->batch; a.qo_sh = q_out_strides->head; a.qo_sn = q_out_strides->token;
         a.qo_wide = wide_rows(q_out, *q_out_strides, f32);
-        a.q_heads_used = p->q_heads;
     }
     a.positions = positions_opt;
     if (positions_opt) { a.pos_sb = positions_strides->batch; a.pos_sh = positions_strides->head; a.pos_sn = positions_strides->token; }

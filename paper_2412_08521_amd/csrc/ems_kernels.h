@@ -178,9 +178,11 @@ struct AppendArgs {
     int32_t* pos_pages;         // [num_pages, kv_heads, page_size] or null
     const int32_t* page_table;  // [batch, max_pages]
     int batch, n_new, kv_heads, group, page_size, num_pages, max_pages, rot;
-    int q_heads_used;           // q heads, 0 without queries
+    int tokens, heads;          // tokens and kv-heads of a block (set by the launcher)
     bool interleaved, k_wide, v_wide, q_wide, qo_wide;
 };
+
+constexpr int kAppendTokens = 16;
 
 // Attention of one new token per sequence.  Rows are those of a paged cache (page_table), or of a compact cache whose
 // table elements name them (tok_row; one element more is the new token itself).

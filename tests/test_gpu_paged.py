@@ -102,6 +102,10 @@ def _append_case(b, hq, hkv, d, ps, n, start, rot, mode, layout="packed", interl
     dict(b=2, hq=4, hkv=4, d=64, ps=32, n=50, start=[7, 8], rot=0, layout="packed", store=False),
     dict(b=1, hq=32, hkv=8, d=128, ps=16, n=300, start=[1000], rot=128, new_len=[500]),
     dict(b=1, hq=32, hkv=8, d=128, ps=16, n=9, start=[16], rot=128, new_len=[-3]),
+    # so many tokens that a block takes 16 of them and all heads, two of three heads, and 8 past the caches (over 256 MB)
+    dict(b=3, hq=6, hkv=3, d=64, ps=16, n=3000, start=[0, 5, 16], rot=32, new_len=[3000, 2991, 17]),
+    dict(b=3, hq=9, hkv=3, d=64, ps=32, n=1500, start=[1, 0, 31], rot=64, interleaved=True),
+    dict(b=2, hq=20, hkv=4, d=128, ps=16, n=9700, start=[3, 0], rot=128, new_len=[9700, 9001]),
 ])
 def test_append_matches_64_bits(case, mode):
     _log("append", case, mode)
