@@ -122,6 +122,9 @@ __device__ __forceinline__ Units count_units(const AttendArgs& a, bool table, in
     return {__builtin_amdgcn_readlane(wave_scan(before), 63), __builtin_amdgcn_readlane(wave_scan(total), 63)};
 }
 
+template <bool kPast, typename V>
+__device__ __forceinline__ V read(const V* p) { return kPast ? __builtin_nontemporal_load(p) : *p; }
+
 // Max or sum over the four lanes l % 16 + 16 n that share a column.
 template <bool kMax>
 __device__ __forceinline__ float column_reduce(float v)
@@ -132,7 +135,7 @@ __device__ __forceinline__ float column_reduce(float v)
 
 }  // namespace
 
-template <typename T, int D, bool kTable, int kW>
+template <typename T, int D, bool kTable, int kW, bool kPast>
 __global__ __launch_bounds__(64 * kW, (kW == 4 ? 3 : kW / 4)) void attend_kernel(AttendArgs a)
 {
     constexpr int kTurn = kW * kLook;                          // rows of a block's turn
@@ -248,7 +251,7 @@ __global__ __launch_bounds__(64 * kW, (kW == 4 ? 3 : kW / 4)) void attend_kernel
             for (int i = 0; i < kTiles; ++i) {
                 const char* p = address(a.k, a.k_new, row_of[wave][buf][kStep * at + 16 * i + col]) + 16 * quad;
 #pragma unroll
-                for (int c = 0; c < kPieces; ++c) kf[i][c] = *reinterpret_cast<const frag_t*>(p + 64 * c);
+                for (int c = 0; c < kPieces; ++c) kf[i][c] = read<kPast>(reinterpret_cast<const frag_t*>(p + 64 * c));
             }
         };
         vec_t vf[kTiles][4][kParts];                           // rows 16 i + 4 quad + r
@@ -259,7 +262,7 @@ __global__ __launch_bounds__(64 * kW, (kW == 4 ? 3 : kW / 4)) void attend_kernel
                 for (int r = 0; r < 4; ++r) {
                     const char* p = address(a.v, a.v_new, row_of[wave][buf][kStep * at + 16 * i + 4 * quad + r]) + 4 * kVec * col;
 #pragma unroll
-                    for (int h = 0; h < kParts; ++h) vf[i][r][h] = *reinterpret_cast<const vec_t*>(p + 256 * h);
+                    for (int h = 0; h < kParts; ++h) vf[i][r][h] = read<kPast>(reinterpret_cast<const vec_t*>(p + 256 * h));
                 }
         };
         // one step on the rows in kf and vf, which the rows of (next_buf, next_at) then take
@@ -538,14 +541,22 @@ hipError_t launch(AttendArgs a, hipStream_t st)
         if (a.group % n == 0 && (long long)a.batch * a.kv_heads * (a.group / n) >= 512) a.join_q = n;
     const int tiles = (a.group + kAttendQ - 1) / kAttendQ;
     const long long max_len = kTable ? a.n_tok + 1 : (long long)a.max_pages * a.page_size;
+    const long long blocks = (long long)a.batch * a.kv_heads * tiles;
+    const dim3 grid(a.workers ? a.workers : a.batch, a.kv_heads, tiles);
     constexpr int kWide = kRowBytesOf<T, D> <= 128 ? 16 : 8;
+    // Rows that are read once, and more of them than stay in the caches, go past these (us, plain / past: one sequence of 8
+    // heads of 128 and 16384 rows 16.6 / 16.4, 32768 28.8 / 27.1, 131072 97.8 / 86.9; 64 ragged sequences of up to 32768
+    // 763 / 703).  Two tiles of q-heads share their reads (20 q-heads of a kv-head: 80 / 90), tokens of a compact cache their rows.
+    const bool past = !kTable && tiles == 1 && blocks * max_len * 2 * kRowBytesOf<T, D> > 80 << 20;
     // A block per sequence has eight waves (or 16, as the registers allow) where it would need several turns of four, and
     // there is less than two blocks' work for a compute unit (us at 8 heads of 128 and 512 rows, eight waves / four:
     // 16 sequences 11.5 / 12.4, 32 15.2 / 15.8, 64 29.7 / 27.5, 128 56.6 / 50.4).
-    if (!a.workers && max_len > kUnit && (long long)a.batch * a.kv_heads * tiles < 512)
-        attend_kernel<T, D, kTable, kWide><<<dim3(a.batch, a.kv_heads, tiles), 64 * kWide, 0, st>>>(a);
+    if (!a.workers && max_len > kUnit && blocks < 512)
+        attend_kernel<T, D, kTable, kWide, false><<<grid, 64 * kWide, 0, st>>>(a);
+    else if (past)
+        attend_kernel<T, D, kTable, kWaves, !kTable><<<grid, 256, 0, st>>>(a);
     else
-        attend_kernel<T, D, kTable, kWaves><<<dim3(a.workers ? a.workers : a.batch, a.kv_heads, tiles), 256, 0, st>>>(a);
+        attend_kernel<T, D, kTable, kWaves, false><<<grid, 256, 0, st>>>(a);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && a.workers) {
         attend_join_kernel<T, D, kTable><<<dim3(a.batch, a.kv_heads, a.group / a.join_q), 256, 0, st>>>(a);

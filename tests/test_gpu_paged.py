@@ -285,6 +285,9 @@ def test_attention_layouts_scales_and_long_tables():
         _attend_case(2, 6, 6, 64, 16, [70, 500], mode, scale=0.31, masked=0.2)
         _attend_case(2, 8, 2, 128, 16, [5, 40], mode, columns=600)          # a table much longer than its sequences
         _attend_case(2, 8, 2, 128, 16, [16 * 40, 7], mode, layout="off", columns=41)
+        # tables that admit more than 80 MB: rows are read past the caches, by shared blocks and by a block per sequence
+        _attend_case(3, 8, 2, 128, 16, [5, 1040, 300], mode, columns=6000, masked=0.3)
+        _attend_case(130, 8, 4, 64, 16, [(53 * i * i) % 300 for i in range(130)], mode, columns=128, masked=0.3)
 
 
 def test_attention_clamps_lengths_and_skips_pages_that_do_not_exist():
