@@ -376,7 +376,7 @@ int ems_decode_step(const ems_params* p, const ems_decode_state* state, int32_t 
  *     out = sum_t p_t value_t / sum_t p_t        lse = ln sum_t p_t
  *   state        in : only k_cache, v_cache, row_norm, tok_row and tok_norm are read (the others may be NULL)
  *   q_new        in : device [B, Hq, D] `dtype`;  k_new, v_new in: device [B, Hkv, D] `dtype`, 16-byte aligned
- *   out          out: device [B, Hq, D] `dtype`, 16-byte aligned
+ *   out          out: device [B, Hq, D] `dtype`, 16-byte aligned, apart from the inputs
  *   lse_opt      out: device [B, Hq] f32, or NULL
  *   ws           device scratch of at least ems_decode_attention_workspace_bytes
  * Any Hq / Hkv.  Table elements whose row is outside [0, budget) are taken as free.
@@ -443,7 +443,8 @@ typedef struct {
  *   q_opt, q_out   device [B, Hq, n_new, D] with any strides: queries to rotate (by the positions of their
  *                  kv-head), or both NULL.  q_out may be q itself (same strides); other overlaps are not allowed.
  *   len_out_opt    out: device [B] i32 start[b] + its tokens, clamped to the table: the lengths for
- *                       ems_paged_attention and the next call's `start`; it must not be `start` itself
+ *                       ems_paged_attention and the next call's `start`; it must not overlap `start` or
+ *                       `new_len_opt`
  * Writes the cache (its positions too, where it has them).  No workspace.  Two sequences that write the same page
  * row race.
  */
@@ -462,10 +463,11 @@ int ems_paged_append(const ems_paged_params* p, const ems_paged_cache* cache, in
  * over the live rows t < lens[b] of the kv-head, with p_t = exp(scale q.k_t),
  *     out = sum_t p_t v_t / sum_t p_t        lse = ln sum_t p_t
  * A sequence-head without a live row (length 0, or every row masked) gives zeros and -inf.  What masked rows and
- * rows behind the length hold does not matter; a NaN or an infinity in a live row gives what is not finite.
+ * rows behind the length hold does not matter; a live row whose logit is -inf weighs nothing, other infinities and
+ * NaN in a live row give what is not finite.
  *   lens           in : device [B] i32 rows of every sequence
  *   q              in : device [B, Hq, D] with any strides (batch, head; token is unused)
- *   out            out: device [B, Hq, D] `dtype`, contiguous, 16-byte aligned
+ *   out            out: device [B, Hq, D] `dtype`, contiguous, 16-byte aligned, apart from the inputs
  *   lse_opt        out: device [B, Hq] f32, or NULL
  *   ws             device scratch of at least ems_paged_workspace_bytes
  * The result depends on nothing but the arguments (no atomics); how the work is split depends on the lengths.

@@ -26,7 +26,8 @@ constexpr int kNewRow = -2;      // the row of the new token itself (compact cac
 constexpr int kNoRow = -1;
 
 constexpr int kLook = 32;                 // rows that a wave looks up at a time, a lane each
-constexpr int kUnit = kWaves * kLook;     // rows of a block's turn: what stretches are counted in
+constexpr int kUnit = kAttendUnit;        // what stretches are counted in: a turn of four waves
+static_assert(kUnit == kWaves * kLook, "a turn");
 
 template <typename T, int D> constexpr int kRowBytesOf = D * (int)sizeof(T);
 
@@ -266,8 +267,8 @@ __global__ __launch_bounds__(64 * kW, (kW == 4 ? 3 : kW / 4)) void attend_kernel
                 }
         };
         // one step on the rows in kf and vf, which the rows of (next_buf, next_at) then take
-        const auto step = [&](unsigned all_live, int buf, int at, int next_buf, int next_at) {
-            unsigned live = uniform((int)(kTiles == 2 ? all_live : all_live & 0xffff));
+        const auto step = [&](unsigned live, int buf, int at, int next_buf, int next_at) {
+            live = uniform((int)(kTiles == 2 ? live : live & 0xffff));
             f32x4_t s[kTiles];
 #pragma unroll
             for (int i = 0; i < kTiles; ++i) {
@@ -288,63 +289,63 @@ __global__ __launch_bounds__(64 * kW, (kW == 4 ? 3 : kW / 4)) void attend_kernel
             load_keys(next_buf, next_at);
             __builtin_amdgcn_sched_barrier(0);
             if (live) {                                        // (row 0 may hold anything)
-            // logits in units of ln 2, dead rows -inf whatever their products are
-            live >>= 4 * quad;
-            float top = -INFINITY;
+                // logits in units of ln 2, dead rows -inf whatever their products are
+                live >>= 4 * quad;
+                float top = -INFINITY;
 #pragma unroll
-            for (int i = 0; i < kTiles; ++i) {
-                f32x4_t f = {a.scale_log2e, a.scale_log2e, a.scale_log2e, a.scale_log2e};
-                if constexpr (kTable) f *= *reinterpret_cast<const f32x4_t*>(&factor_of[wave][buf][kStep * at + 16 * i + 4 * quad]);
+                for (int i = 0; i < kTiles; ++i) {
+                    f32x4_t f = {a.scale_log2e, a.scale_log2e, a.scale_log2e, a.scale_log2e};
+                    if constexpr (kTable) f *= *reinterpret_cast<const f32x4_t*>(&factor_of[wave][buf][kStep * at + 16 * i + 4 * quad]);
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    s[i][r] = (live >> (16 * i + r)) & 1 ? s[i][r] * f[r] : -INFINITY;
-                    top = fmaxf(top, s[i][r]);
+                    for (int r = 0; r < 4; ++r) {
+                        s[i][r] = (live >> (16 * i + r)) & 1 ? s[i][r] * f[r] : -INFINITY;
+                        top = fmaxf(top, s[i][r]);
+                    }
                 }
-            }
-            const float m_new = fmaxf(m, column_reduce<true>(top));
-            const float ref = m_new > -INFINITY ? m_new : 0.f;
-            if (__any(m_new > m)) {
-                const float shrink = exp2_fast(m - ref);
-                l *= shrink;
+                const float m_new = fmaxf(m, column_reduce<true>(top));
+                const float ref = m_new > -INFINITY ? m_new : 0.f;
+                if (__any(m_new > m)) {
+                    const float shrink = exp2_fast(m - ref);
+                    l *= shrink;
 #pragma unroll
-                for (int i = 0; i < kOut; ++i) o[i] *= shrink;
-                m = m_new;
-            }
-#pragma unroll
-            for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) { s[i][r] = exp2_fast(s[i][r] - ref); l += s[i][r]; }
-            if constexpr (sizeof(T) == 2) {
-                bf16x8_t high, rest;
-#pragma unroll
-                for (int r = 0; r < 8; ++r) {
-                    const float p = s[r / 4][r % 4];
-                    high[r] = (bf16_t)p;
-                    rest[r] = (bf16_t)(p - (float)high[r]);
+                    for (int i = 0; i < kOut; ++i) o[i] *= shrink;
+                    m = m_new;
                 }
-#pragma unroll
-                for (int e = 0; e < kCols; ++e) {
-                    frag_t x;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        x[j] = __builtin_amdgcn_perm(vf[(2 * j + 1) / 4][(2 * j + 1) % 4][0][e / 2], vf[2 * j / 4][2 * j % 4][0][e / 2],
-                                                     e % 2 ? 0x07060302 : 0x05040100);
-                    o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, x), high, o[e], 0, 0, 0);
-                    o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, x), rest, o[e], 0, 0, 0);
-                }
-            } else {
 #pragma unroll
                 for (int i = 0; i < kTiles; ++i)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r)
+                    for (int r = 0; r < 4; ++r) { s[i][r] = exp2_fast(s[i][r] - ref); l += s[i][r]; }
+                if constexpr (sizeof(T) == 2) {
+                    bf16x8_t high, rest;
 #pragma unroll
-                        for (int h = 0; h < kParts; ++h) {
-                            const f32x4_t x = __builtin_bit_cast(f32x4_t, vf[i][r][h]);
+                    for (int r = 0; r < 8; ++r) {
+                        const float p = s[r / 4][r % 4];
+                        high[r] = (bf16_t)p;
+                        rest[r] = (bf16_t)(p - (float)high[r]);
+                    }
 #pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                o[4 * h + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], s[i][r], o[4 * h + e], 0, 0, 0);
-                        }
-            }
+                    for (int e = 0; e < kCols; ++e) {
+                        frag_t x;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            x[j] = __builtin_amdgcn_perm(vf[(2 * j + 1) / 4][(2 * j + 1) % 4][0][e / 2], vf[2 * j / 4][2 * j % 4][0][e / 2],
+                                                         e % 2 ? 0x07060302 : 0x05040100);
+                        o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, x), high, o[e], 0, 0, 0);
+                        o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, x), rest, o[e], 0, 0, 0);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r)
+#pragma unroll
+                            for (int h = 0; h < kParts; ++h) {
+                                const f32x4_t x = __builtin_bit_cast(f32x4_t, vf[i][r][h]);
+#pragma unroll
+                                for (int e = 0; e < 4; ++e)
+                                    o[4 * h + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], s[i][r], o[4 * h + e], 0, 0, 0);
+                            }
+                }
             }
             __builtin_amdgcn_sched_barrier(0);
             load_values(next_buf, next_at);

@@ -583,6 +583,13 @@ static float scale_log2e(float softmax_scale, int head_dim)
     return (float)(scale * 1.4426950408889634074);
 }
 
+// grid dimensions, and units of work as 32-bit numbers
+static bool attend_grid_ok(int batch, int q_heads, long long max_len)
+{
+    return (long long)batch * q_heads <= (1 << 24) && q_heads <= 65535 &&
+           batch * ((max_len + ems::kAttendUnit - 1) / ems::kAttendUnit) <= (1ll << 30);
+}
+
 static bool aligned16(const void* p) { return ((uintptr_t)p % 16) == 0; }
 
 // rows of `dtype` that start at multiples of 16 bytes, whatever the index
@@ -616,17 +623,29 @@ static int attend(ems::AttendArgs& a, const AttendPlan& plan, bool f32, void* ws
     return e == hipSuccess ? EMS_OK : EMS_ERR_LAUNCH;
 }
 
-static AttendPlan plan_decode_attention(const ems_params* p)
+static int decode_table(const ems_params* p)
 {
     int n_imp, n_tbm;
     partition_sizes(p, &n_imp, &n_tbm);
-    return plan_attend(p->batch, p->kv_heads, p->q_heads / p->kv_heads, p->head_dim, (long long)n_imp + n_tbm + p->window + 1, p->dtype);
+    return n_imp + n_tbm + p->window;
+}
+
+static bool decode_attention_params_ok(const ems_params* p, int* why)
+{
+    if (!full_params_ok(p, why)) return false;
+    *why = EMS_ERR_UNSUPPORTED;
+    return attend_grid_ok(p->batch, p->q_heads, decode_table(p) + 1ll);
+}
+
+static AttendPlan plan_decode_attention(const ems_params* p)
+{
+    return plan_attend(p->batch, p->kv_heads, p->q_heads / p->kv_heads, p->head_dim, decode_table(p) + 1ll, p->dtype);
 }
 
 int ems_decode_attention_workspace_bytes(const ems_params* p, size_t* attention_ws)
 {
     int why;
-    if (!full_params_ok(p, &why)) return why;
+    if (!decode_attention_params_ok(p, &why)) return why;
     if (attention_ws) *attention_ws = plan_decode_attention(p).total;
     return EMS_OK;
 }
@@ -636,18 +655,16 @@ int ems_decode_attention(const ems_params* p, const ems_decode_state* state,
                          void* out, float* lse_opt, void* ws, size_t ws_bytes, void* hip_stream)
 {
     int why;
-    if (!full_params_ok(p, &why)) return why;
+    if (!decode_attention_params_ok(p, &why)) return why;
     if (!state || !state->k_cache || !state->v_cache || !state->row_norm || !state->tok_row || !state->tok_norm) return EMS_ERR_INVALID_ARG;
     if (!q_new || !k_new || !v_new || !out) return EMS_ERR_INVALID_ARG;
     if (!aligned16(state->k_cache) || !aligned16(state->v_cache) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(out))
         return EMS_ERR_INVALID_ARG;
-    int n_imp, n_tbm;
-    partition_sizes(p, &n_imp, &n_tbm);
     ems::AttendArgs a{};
     a.q = q_new; a.q_sh = p->head_dim; a.q_sb = (long long)p->q_heads * p->head_dim; a.q_wide = aligned16(q_new);
     a.k = state->k_cache; a.v = state->v_cache; a.out = out; a.lse = lse_opt;
     a.tok_row = state->tok_row; a.tok_norm = state->tok_norm; a.row_norm = state->row_norm;
-    a.k_new = k_new; a.v_new = v_new; a.n_tok = n_imp + n_tbm + p->window; a.budget = p->budget;
+    a.k_new = k_new; a.v_new = v_new; a.n_tok = decode_table(p); a.budget = p->budget;
     a.batch = p->batch; a.kv_heads = p->kv_heads; a.group = p->q_heads / p->kv_heads; a.head_dim = p->head_dim;
     a.scale_log2e = scale_log2e(p->softmax_scale, p->head_dim);
     return attend(a, plan_decode_attention(p), p->dtype == EMS_F32, ws, ws_bytes, hip_stream);
@@ -666,9 +683,7 @@ static bool paged_params_ok(const ems_paged_params* p, int* why)
     if (p->head_dim != 64 && p->head_dim != 128) return false;
     if ((long long)p->max_pages * p->page_size > (1ll << 30)) return false;
     if ((long long)p->num_pages * p->page_size > 0x7fffffffll / p->kv_heads) return false;     // 32-bit row numbers
-    if ((long long)p->batch * p->q_heads > (1 << 24) || p->q_heads > 65535) return false;      // grid of the attention
-    if ((long long)p->batch * (((long long)p->max_pages * p->page_size + 255) / 256) > (1ll << 30)) return false;     // its units
-    return true;
+    return attend_grid_ok(p->batch, p->q_heads, (long long)p->max_pages * p->page_size);
 }
 
 static bool paged_cache_ok(const ems_paged_cache* c)
@@ -692,7 +707,9 @@ int ems_paged_append(const ems_paged_params* p, const ems_paged_cache* cache, in
     if (positions_opt && !positions_strides) return EMS_ERR_INVALID_ARG;
     if (rot_dim < 0 || rot_dim > p->head_dim || (rot_dim > 0) != (inv_freq_opt != nullptr)) return EMS_ERR_INVALID_ARG;
     if ((q_opt != nullptr) != (q_out != nullptr) || (q_opt && (!q_strides || !q_out_strides))) return EMS_ERR_INVALID_ARG;
-    if (len_out_opt && len_out_opt == start) return EMS_ERR_INVALID_ARG;
+    // the lengths that go in are read while those that come out are written
+    const auto apart = [&](const int32_t* in) { return !in || !len_out_opt || len_out_opt + p->batch <= in || in + p->batch <= len_out_opt; };
+    if (!apart(start) || !apart(new_len_opt)) return EMS_ERR_INVALID_ARG;
     if (rot_dim % 16) return EMS_ERR_UNSUPPORTED;
     if ((long long)p->batch * n_new > 0x7fffffffll / (p->q_heads + 2 * p->kv_heads)) return EMS_ERR_UNSUPPORTED;
     const bool f32 = p->dtype == EMS_F32;

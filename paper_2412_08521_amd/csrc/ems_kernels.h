@@ -214,6 +214,7 @@ struct AttendArgs {
     float* part_ml;             // [.., 16, 2] its maximum and sum
 };
 constexpr int kAttendQ = 16;    // q-heads of a group that a block takes: the columns of a matrix product
+constexpr int kAttendUnit = 128;        // rows that work is counted in
 int attend_workers(int batch, int kv_heads, int group, long long max_len, int row_bytes);      // AttendArgs::workers
 hipError_t launch_append(const AppendArgs& a, int head_dim, bool f32, hipStream_t st);
 hipError_t launch_attend(const AttendArgs& a, bool f32, hipStream_t st);

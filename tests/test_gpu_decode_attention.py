@@ -99,6 +99,20 @@ def test_decode_attention_of_an_empty_table_is_the_new_value(mode):
 
 
 @pytest.mark.parametrize("mode", [BF16, F32])
+def test_decode_attention_of_queries_off_a_boundary(mode):
+    p, st, gen = _made_up(2, 4, 2, 128, 700, 16, 0.5, mode, seed=3)
+    q, k, v = _token(p, gen)
+    flat = torch.zeros(q.numel() + 1, dtype=q.dtype).cuda()
+    flat[1:] = q.flatten().cuda()
+    off = flat[1:].view(q.shape)
+    assert off.data_ptr() % 16
+    out = B.ems_decode_attention(p, st, off, k.cuda(), v.cuda())
+    assert torch.equal(out, B.ems_decode_attention(p, st, q.cuda(), k.cuda(), v.cuda()))
+    with pytest.raises(B.EmsError, match="invalid argument"):
+        B.ems_decode_attention(p, st, off, off[:, :2].contiguous(), off.flatten()[:v.numel()].view(v.shape))
+
+
+@pytest.mark.parametrize("mode", [BF16, F32])
 def test_generation_over_the_compact_cache(mode):
     """Prompt to generation: attention, then the step that changes the state, token after token; the output agrees with
     64 bits, and with the weights of the step itself."""

@@ -41,7 +41,8 @@ def _attend(p, **kw):
     (dict(page_size=0), INVALID), (dict(num_pages=0), INVALID), (dict(max_pages=-1), INVALID), (dict(dtype=2), INVALID),
     (dict(softmax_scale=float("nan")), INVALID), (dict(softmax_scale=float("inf")), INVALID),
     (dict(head_dim=96), UNSUPPORTED), (dict(num_pages=1 << 26), UNSUPPORTED), (dict(max_pages=(1 << 26) + 1), UNSUPPORTED),
-    (dict(batch=1 << 23), UNSUPPORTED)])
+    (dict(batch=1 << 23), UNSUPPORTED), (dict(q_heads=65538), UNSUPPORTED),
+    (dict(batch=1 << 20, max_pages=1 << 20), UNSUPPORTED)])
 def test_paged_parameters(kw, code):
     p = _paged(**kw)
     assert _append(p) == code and _attend(p) == code
@@ -57,7 +58,8 @@ def test_append_arguments():
                dict(cache=B.ems_paged_cache(D, D, None, None)), dict(cache=B.ems_paged_cache(D + 8, D, None, D)),
                dict(cache=B.ems_paged_cache(D, D + 2, None, D)), dict(n_new=0), dict(n_new=-1), dict(start=None), dict(k=None),
                dict(ks=None), dict(v=None), dict(vs=None), dict(pos=D), dict(freq=None), dict(rot=0), dict(rot=-16), dict(rot=144),
-               dict(q=None), dict(q_out=None), dict(qs=None), dict(qos=None), dict(len_out=D)):
+               dict(q=None), dict(q_out=None), dict(qs=None), dict(qos=None), dict(len_out=D), dict(len_out=D + 4), dict(len_out=D - 4),
+               dict(start=D + 64, new_len=D, len_out=D + 4)):
         assert _append(p, **kw) == INVALID, kw
     assert _append(None) == INVALID
     assert _append(p, rot=24) == UNSUPPORTED and _append(p, rot=2) == UNSUPPORTED
@@ -109,6 +111,7 @@ def test_decode_attention_arguments():
                dict(tok_norm=None), dict(cp=B.EmsParams(1, 6, 2, 64, 4096, 16, 16).c())):
         assert call(**kw) == INVALID, kw
     assert call(cp=B.EmsParams(1, 6, 2, 80, 4096, 16, 1000).c()) == UNSUPPORTED
+    assert call(cp=B.EmsParams(1, 65536, 2, 64, 4096, 16, 1000).c()) == UNSUPPORTED
     for kw in (dict(ws=None), dict(ws=D + 16), dict(n=need - 1)):
         assert call(**kw) == WORKSPACE, kw
     assert lib.ems_decode_attention(C.byref(cp), None, D, D, D, D, None, D, 1 << 40, None) == INVALID
