@@ -11,61 +11,34 @@ namespace ems {
 
 namespace {
 
-// 8 elements of a row as they are; `wide`: the address is a multiple of 16 bytes; kPast: past the caches (nontemporal)
-template <typename T> struct Piece { frag_t f[8 * sizeof(T) / 16]; };
-template <typename T> struct Elems { T x[8]; };
+// 16 bytes of a row as they are; `wide`: the address is a multiple of 16 bytes; kPast: past the caches (nontemporal)
+template <typename T> struct Elems { T x[16 / sizeof(T)]; };
 
 template <typename T, bool kPast>
-__device__ __forceinline__ Piece<T> load_piece(const T* p, bool wide)
-{
-    Piece<T> r;
-    if (wide) {
-#pragma unroll
-        for (int i = 0; i < (int)(sizeof(r) / 16); ++i) {
-            const frag_t* at = reinterpret_cast<const frag_t*>(p) + i;
-            r.f[i] = kPast ? __builtin_nontemporal_load(at) : *at;
-        }
-    } else {
-        Elems<T> e;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) e.x[i] = p[i];
-        r = __builtin_bit_cast(Piece<T>, e);
-    }
-    return r;
-}
-
-template <typename T, bool kPast>
-__device__ __forceinline__ void store_piece(T* p, bool wide, const Piece<T>& r)
+__device__ __forceinline__ frag_t load_piece(const T* p, bool wide)
 {
     if (wide) {
-#pragma unroll
-        for (int i = 0; i < (int)(sizeof(r) / 16); ++i) {
-            frag_t* at = reinterpret_cast<frag_t*>(p) + i;
-            if constexpr (kPast) __builtin_nontemporal_store(r.f[i], at);
-            else *at = r.f[i];
-        }
-    } else {
-        const Elems<T> e = __builtin_bit_cast(Elems<T>, r);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) p[i] = e.x[i];
+        const frag_t* at = reinterpret_cast<const frag_t*>(p);
+        return kPast ? __builtin_nontemporal_load(at) : *at;
     }
-}
-
-template <typename T>
-__device__ __forceinline__ void unpack8(const Piece<T>& r, float (&x)[8])
-{
-    const Elems<T> e = __builtin_bit_cast(Elems<T>, r);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = to_float(e.x[i]);
-}
-
-template <typename T>
-__device__ __forceinline__ Piece<T> pack8(const float (&x)[8])
-{
     Elems<T> e;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) e.x[i] = (T)x[i];              // round to nearest even
-    return __builtin_bit_cast(Piece<T>, e);
+    for (int i = 0; i < (int)(16 / sizeof(T)); ++i) e.x[i] = p[i];
+    return __builtin_bit_cast(frag_t, e);
+}
+
+template <typename T, bool kPast>
+__device__ __forceinline__ void store_piece(T* p, bool wide, const frag_t& f)
+{
+    if (wide) {
+        frag_t* at = reinterpret_cast<frag_t*>(p);
+        if constexpr (kPast) __builtin_nontemporal_store(f, at);
+        else *at = f;
+    } else {
+        const Elems<T> e = __builtin_bit_cast(Elems<T>, f);
+#pragma unroll
+        for (int i = 0; i < (int)(16 / sizeof(T)); ++i) p[i] = e.x[i];
+    }
 }
 
 // cos and sin of t f
@@ -92,13 +65,14 @@ __device__ __forceinline__ void rotate(float& u, float& w, float c, float s)
 
 // A block takes up to 16 tokens and the rows (queries, keys, values) of some kv-heads.  Its angles are formed once, a value a
 // thread, and shared through LDS: formed by every thread for its own row they were what a prompt waited for (four prompts
-// of 8192 tokens, 40 heads to rotate: 187 us, of which ~150 were vector instructions).  Then a lane group of D / 16 lanes
-// takes a row, a lane the two halves of 8 pairs (or 16 elements that only move), kAhead rows requested together; a lane
+// of 8192 tokens, 40 heads to rotate: 187 us, of which ~150 were vector instructions).  Then a lane group
+// takes a row, a lane two pieces of 16 bytes that hold both halves of its pairs, kAhead rows requested together; a lane
 // reads all of its elements before it writes any, so queries may be turned in place.
 template <typename T, int D, bool kPast>
 __global__ __launch_bounds__(256) void append_kernel(AppendArgs a)
 {
-    constexpr int kItems = D / 16, kGroups = 256 / kItems, kAhead = 4;
+    constexpr int kPer = 16 / (int)sizeof(T);                  // elements of a piece: a lane takes two pieces of a row
+    constexpr int kItems = D / (2 * kPer), kGroups = 256 / kItems, kAhead = 4;
     __shared__ __align__(16) float cs[kAppendTokens][2][D / 2];
     const int n_tok = a.tokens;                                // of a block: a power of two
     const int h0 = blockIdx.y * a.heads, heads = min(a.heads, a.kv_heads - h0);       // its kv-heads
@@ -134,12 +108,19 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a)
         const int page = a.page_table[(size_t)b * a.max_pages + (int)slot / a.page_size];
         if (page >= 0 && page < a.num_pages) at = (long long)page * a.kv_heads * a.page_size + (int)slot % a.page_size;
     }
-    const bool paired = item < a.rot / 16;
-    const bool halves = paired && !a.interleaved;              // 8 columns of each half, else 16 in a row
-    const int e0 = halves ? 8 * item : 16 * item, e1 = halves ? 8 * item + half : 16 * item + 8;
-    float c[8], s[8];
+    // Neighbouring lanes take neighbouring pieces: of the two halves of the rotated columns (paired across the halves, or
+    // within each piece), of the two halves of those behind them, and of a row that only moves.
+    const int n_paired = a.rot / (2 * kPer);
+    const bool paired = item < n_paired;
+    const int e0 = paired ? kPer * item : a.rot + kPer * (item - n_paired), e1 = e0 + (paired ? half : (D - a.rot) / 2);
+    const int m0 = kPer * item, m1 = m0 + D / 2;
+    float c[kPer], s[kPer];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) { c[e] = paired ? cs[t][0][8 * item + e] : 1.f; s[e] = paired ? cs[t][1][8 * item + e] : 0.f; }
+    for (int e = 0; e < kPer; ++e) {
+        const int f = !a.interleaved ? kPer * item + e : kPer / 2 * item + e % (kPer / 2) + (e < kPer / 2 ? 0 : half / 2);
+        c[e] = paired ? cs[t][0][f] : 1.f;
+        s[e] = paired ? cs[t][1][f] : 0.f;
+    }
 
     const int n_q = a.q ? heads * a.group : 0, rows = n_q + 2 * heads;
     const T* q_in = reinterpret_cast<const T*>(a.q) + b * a.q_sb + (long long)h0 * a.group * a.q_sh + i * a.q_sn;
@@ -148,42 +129,42 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a)
     const T* v_in = reinterpret_cast<const T*>(a.v) + b * a.v_sb + h0 * a.v_sh + i * a.v_sn;
     const int step = kGroups / n_tok;
     for (int r0 = group / n_tok; r0 < rows; r0 += kAhead * step) {
-        Piece<T> p0[kAhead], p1[kAhead];
+        frag_t p0[kAhead], p1[kAhead];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             const int r = r0 + u * step, k = r - n_q, v = k - heads;
             if (r >= rows || (r >= n_q && at < 0)) continue;
             const T* src = r < n_q ? q_in + r * a.q_sh : v < 0 ? k_in + k * a.k_sh : v_in + v * a.v_sh;
             const bool wide = r < n_q ? a.q_wide : v < 0 ? a.k_wide : a.v_wide;
-            p0[u] = load_piece<T, kPast>(src + e0, wide);
-            p1[u] = load_piece<T, kPast>(src + e1, wide);
+            p0[u] = load_piece<T, kPast>(src + (v < 0 ? e0 : m0), wide);
+            p1[u] = load_piece<T, kPast>(src + (v < 0 ? e1 : m1), wide);
         }
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             const int r = r0 + u * step, k = r - n_q, v = k - heads;
             if (r >= rows || (r >= n_q && at < 0)) continue;
             if (paired && v < 0) {
-                float x[8], y[8];
-                unpack8(p0[u], x);
-                unpack8(p1[u], y);
-                if (halves) {
+                float x[kPer], y[kPer];
+                Pack<T>::unpack(p0[u], x);
+                Pack<T>::unpack(p1[u], y);
+                if (!a.interleaved) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) rotate(x[e], y[e], c[e], s[e]);
+                    for (int e = 0; e < kPer; ++e) rotate(x[e], y[e], c[e], s[e]);
                 } else {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
+                    for (int e = 0; e < kPer / 2; ++e) {
                         rotate(x[2 * e], x[2 * e + 1], c[e], s[e]);
-                        rotate(y[2 * e], y[2 * e + 1], c[e + 4], s[e + 4]);
+                        rotate(y[2 * e], y[2 * e + 1], c[kPer / 2 + e], s[kPer / 2 + e]);
                     }
                 }
-                p0[u] = pack8<T>(x);
-                p1[u] = pack8<T>(y);
+                p0[u] = Pack<T>::pack(x);
+                p1[u] = Pack<T>::pack(y);
             }
             const long long row = at + (long long)(h0 + (v < 0 ? k : v)) * a.page_size;
             T* dst = r < n_q ? q_out + r * a.qo_sh : reinterpret_cast<T*>(v < 0 ? a.k_pages : a.v_pages) + row * D;
             const bool wide = r >= n_q || a.qo_wide;
-            store_piece<T, kPast>(dst + e0, wide, p0[u]);
-            store_piece<T, kPast>(dst + e1, wide, p1[u]);
+            store_piece<T, kPast>(dst + (v < 0 ? e0 : m0), wide, p0[u]);
+            store_piece<T, kPast>(dst + (v < 0 ? e1 : m1), wide, p1[u]);
             if (a.pos_pages && r >= n_q && v < 0 && item == 0)
                 a.pos_pages[row] = a.positions ? a.positions[b * a.pos_sb + (h0 + k) * a.pos_sh + i * a.pos_sn] : (int)slot;
         }

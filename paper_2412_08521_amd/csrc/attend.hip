@@ -136,8 +136,8 @@ __device__ __forceinline__ float column_reduce(float v)
 
 }  // namespace
 
-template <typename T, int D, bool kTable, int kW, bool kPast>
-__global__ __launch_bounds__(64 * kW, (kW == 4 ? 3 : kW / 4)) void attend_kernel(AttendArgs a)
+template <typename T, int D, bool kTable, int kW, bool kPast, int kQt>
+__global__ __launch_bounds__(64 * kW, (kQt == 2 ? 2 : kW == 4 ? 3 : kW / 4)) void attend_kernel(AttendArgs a)
 {
     constexpr int kTurn = kW * kLook;                          // rows of a block's turn
     constexpr int kTiles = kRowBytesOf<T, D> <= 256 ? 2 : 1;    // 16-row tiles of a step: their keys and values wait in registers
@@ -152,8 +152,8 @@ __global__ __launch_bounds__(64 * kW, (kW == 4 ? 3 : kW / 4)) void attend_kernel
     typedef int vec_t __attribute__((ext_vector_type(kVec)));
     __shared__ __align__(16) int row_of[kW][2][kLook];
     __shared__ __align__(16) float factor_of[kW][2][kTable ? kLook : 4];
-    __shared__ __align__(16) float red_o[kW][kAttendQ][D + 4];
-    __shared__ float red_ml[kW][kAttendQ][2];
+    __shared__ __align__(16) float red_o[kW][kQt * kAttendQ][D + 4];
+    __shared__ float red_ml[kW][kQt * kAttendQ][2];
 
     const auto turns_of = [](int n) { return (n + kTurn - 1) / kTurn; };
     const int lane = threadIdx.x % kWave, wave = uniform((int)threadIdx.x / kWave);
@@ -168,7 +168,7 @@ __global__ __launch_bounds__(64 * kW, (kW == 4 ? 3 : kW / 4)) void attend_kernel
         if (s.b < 0) return;
         b = s.b; base = s.before; len = s.len; u = s.u; u_end = s.u_end;
     }
-    const int q0 = tile * kAttendQ, n_q = min(a.group - q0, kAttendQ);
+    const int q0 = tile * kQt * kAttendQ, n_q = min(a.group - q0, kQt * kAttendQ);
 
     for (;;) {
         const int first = u - base;
@@ -176,29 +176,35 @@ __global__ __launch_bounds__(64 * kW, (kW == 4 ? 3 : kW / 4)) void attend_kernel
         const size_t q_head = (size_t)unit * a.group + q0;                          // = b * Hq + head * group + q0
 
         // queries: the right operand of the first product
-        frag_t qf[kPieces];
-        {
-            const T* q = reinterpret_cast<const T*>(a.q) + b * a.q_sb + (long long)(head * a.group + q0 + col) * a.q_sh;
+        frag_t qf[kQt][kPieces];
+#pragma unroll
+        for (int j = 0; j < kQt; ++j) {
+            const int qi = kAttendQ * j + col;
+            const T* q = reinterpret_cast<const T*>(a.q) + b * a.q_sb + (long long)(head * a.group + q0 + qi) * a.q_sh;
 #pragma unroll
             for (int c = 0; c < kPieces; ++c) {
-                qf[c] = zero_frag();
-                if (col < n_q) {
+                qf[j][c] = zero_frag();
+                if (qi < n_q) {
                     const T* at = q + (4 * c + quad) * (16 / (int)sizeof(T));
-                    if (a.q_wide) qf[c] = *reinterpret_cast<const frag_t*>(at);
+                    if (a.q_wide) qf[j][c] = *reinterpret_cast<const frag_t*>(at);
                     else {
                         struct Elems { T x[16 / sizeof(T)]; } e;
 #pragma unroll
                         for (int i = 0; i < (int)(16 / sizeof(T)); ++i) e.x[i] = at[i];
-                        qf[c] = __builtin_bit_cast(frag_t, e);
+                        qf[j][c] = __builtin_bit_cast(frag_t, e);
                     }
                 }
             }
         }
 
-        f32x4_t o[kOut];
+        f32x4_t o[kQt][kOut];
+        float m[kQt], l[kQt];                                  // of column `col`; l: this lane's rows only
 #pragma unroll
-        for (int i = 0; i < kOut; ++i) o[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        float m = -INFINITY, l = 0.f;                          // of column `col`; l: this lane's rows only
+        for (int j = 0; j < kQt; ++j) {
+            m[j] = -INFINITY; l[j] = 0.f;
+#pragma unroll
+            for (int i = 0; i < kOut; ++i) o[j][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        }
 
         // Rows are looked up a batch of 64 ahead in two trips (the table; the position, or the norms), keys and values are
         // requested a step ahead, as soon as the registers that take them are free.
@@ -269,69 +275,82 @@ __global__ __launch_bounds__(64 * kW, (kW == 4 ? 3 : kW / 4)) void attend_kernel
         // one step on the rows in kf and vf, which the rows of (next_buf, next_at) then take
         const auto step = [&](unsigned live, int buf, int at, int next_buf, int next_at) {
             live = uniform((int)(kTiles == 2 ? live : live & 0xffff));
-            f32x4_t s[kTiles];
+            f32x4_t s[kQt][kTiles];
 #pragma unroll
-            for (int i = 0; i < kTiles; ++i) {
-                s[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            for (int j = 0; j < kQt; ++j)
 #pragma unroll
-                for (int c = 0; c < kPieces; ++c) {
-                    if constexpr (sizeof(T) == 2) {
-                        s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf[i][c]),
-                                                                       __builtin_bit_cast(bf16x8_t, qf[c]), s[i], 0, 0, 0);
-                    } else {
-                        const f32x4_t x = __builtin_bit_cast(f32x4_t, kf[i][c]), y = __builtin_bit_cast(f32x4_t, qf[c]);
+                for (int i = 0; i < kTiles; ++i) {
+                    s[j][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) s[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], y[e], s[i], 0, 0, 0);
+                    for (int c = 0; c < kPieces; ++c) {
+                        if constexpr (sizeof(T) == 2) {
+                            s[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf[i][c]),
+                                                                              __builtin_bit_cast(bf16x8_t, qf[j][c]), s[j][i], 0, 0, 0);
+                        } else {
+                            const f32x4_t x = __builtin_bit_cast(f32x4_t, kf[i][c]), y = __builtin_bit_cast(f32x4_t, qf[j][c]);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) s[j][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], y[e], s[j][i], 0, 0, 0);
+                        }
                     }
                 }
-            }
             __builtin_amdgcn_sched_barrier(0);
             load_keys(next_buf, next_at);
             __builtin_amdgcn_sched_barrier(0);
             if (live) {                                        // (row 0 may hold anything)
                 // logits in units of ln 2, dead rows -inf whatever their products are
                 live >>= 4 * quad;
-                float top = -INFINITY;
+                f32x4_t f[kTiles];
 #pragma unroll
                 for (int i = 0; i < kTiles; ++i) {
-                    f32x4_t f = {a.scale_log2e, a.scale_log2e, a.scale_log2e, a.scale_log2e};
-                    if constexpr (kTable) f *= *reinterpret_cast<const f32x4_t*>(&factor_of[wave][buf][kStep * at + 16 * i + 4 * quad]);
+                    f[i] = f32x4_t{a.scale_log2e, a.scale_log2e, a.scale_log2e, a.scale_log2e};
+                    if constexpr (kTable) f[i] *= *reinterpret_cast<const f32x4_t*>(&factor_of[wave][buf][kStep * at + 16 * i + 4 * quad]);
+                }
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        s[i][r] = (live >> (16 * i + r)) & 1 ? s[i][r] * f[r] : -INFINITY;
-                        top = fmaxf(top, s[i][r]);
+                for (int j = 0; j < kQt; ++j) {
+                    float top = -INFINITY;
+#pragma unroll
+                    for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            s[j][i][r] = (live >> (16 * i + r)) & 1 ? s[j][i][r] * f[i][r] : -INFINITY;
+                            top = fmaxf(top, s[j][i][r]);
+                        }
+                    const float m_new = fmaxf(m[j], column_reduce<true>(top));
+                    const float ref = m_new > -INFINITY ? m_new : 0.f;
+                    if (__any(m_new > m[j])) {
+                        const float shrink = exp2_fast(m[j] - ref);
+                        l[j] *= shrink;
+#pragma unroll
+                        for (int i = 0; i < kOut; ++i) o[j][i] *= shrink;
+                        m[j] = m_new;
                     }
+#pragma unroll
+                    for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) { s[j][i][r] = exp2_fast(s[j][i][r] - ref); l[j] += s[j][i][r]; }
                 }
-                const float m_new = fmaxf(m, column_reduce<true>(top));
-                const float ref = m_new > -INFINITY ? m_new : 0.f;
-                if (__any(m_new > m)) {
-                    const float shrink = exp2_fast(m - ref);
-                    l *= shrink;
-#pragma unroll
-                    for (int i = 0; i < kOut; ++i) o[i] *= shrink;
-                    m = m_new;
-                }
-#pragma unroll
-                for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) { s[i][r] = exp2_fast(s[i][r] - ref); l += s[i][r]; }
                 if constexpr (sizeof(T) == 2) {
-                    bf16x8_t high, rest;
+                    bf16x8_t high[kQt], rest[kQt];
 #pragma unroll
-                    for (int r = 0; r < 8; ++r) {
-                        const float p = s[r / 4][r % 4];
-                        high[r] = (bf16_t)p;
-                        rest[r] = (bf16_t)(p - (float)high[r]);
-                    }
+                    for (int j = 0; j < kQt; ++j)
+#pragma unroll
+                        for (int r = 0; r < 8; ++r) {
+                            const float p = s[j][r / 4][r % 4];
+                            high[j][r] = (bf16_t)p;
+                            rest[j][r] = (bf16_t)(p - (float)high[j][r]);
+                        }
 #pragma unroll
                     for (int e = 0; e < kCols; ++e) {
                         frag_t x;
 #pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            x[j] = __builtin_amdgcn_perm(vf[(2 * j + 1) / 4][(2 * j + 1) % 4][0][e / 2], vf[2 * j / 4][2 * j % 4][0][e / 2],
+                        for (int d = 0; d < 4; ++d)
+                            x[d] = __builtin_amdgcn_perm(vf[(2 * d + 1) / 4][(2 * d + 1) % 4][0][e / 2], vf[2 * d / 4][2 * d % 4][0][e / 2],
                                                          e % 2 ? 0x07060302 : 0x05040100);
-                        o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, x), high, o[e], 0, 0, 0);
-                        o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, x), rest, o[e], 0, 0, 0);
+#pragma unroll
+                        for (int j = 0; j < kQt; ++j) {
+                            o[j][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, x), high[j], o[j][e], 0, 0, 0);
+                            o[j][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, x), rest[j], o[j][e], 0, 0, 0);
+                        }
                     }
                 } else {
 #pragma unroll
@@ -342,8 +361,10 @@ __global__ __launch_bounds__(64 * kW, (kW == 4 ? 3 : kW / 4)) void attend_kernel
                             for (int h = 0; h < kParts; ++h) {
                                 const f32x4_t x = __builtin_bit_cast(f32x4_t, vf[i][r][h]);
 #pragma unroll
-                                for (int e = 0; e < 4; ++e)
-                                    o[4 * h + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], s[i][r], o[4 * h + e], 0, 0, 0);
+                                for (int j = 0; j < kQt; ++j)
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e)
+                                        o[j][4 * h + e] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], s[j][i][r], o[j][4 * h + e], 0, 0, 0);
                             }
                 }
             }
@@ -384,7 +405,8 @@ __global__ __launch_bounds__(64 * kW, (kW == 4 ? 3 : kW / 4)) void attend_kernel
                 step(now, buf, at, turn ? 1 - buf : buf, turn ? 0 : at + 1);
             }
         }
-        l = column_reduce<false>(l);
+#pragma unroll
+        for (int j = 0; j < kQt; ++j) l[j] = column_reduce<false>(l[j]);
 
         {
         // the four waves' results.  Element r of tile e: column kCols (4 quad + r) + e, or 64 h + 4 (4 quad + r) + e % 4.
@@ -392,19 +414,22 @@ __global__ __launch_bounds__(64 * kW, (kW == 4 ? 3 : kW / 4)) void attend_kernel
         int tid = threadIdx.x;
         asm volatile("" : "+v"(tid));
         const int col = tid % 16, quad = tid % kWave / 16;
-        if (quad == 0) { red_ml[wave][col][0] = m; red_ml[wave][col][1] = l; }
-        if (col < n_q) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
+        for (int j = 0; j < kQt; ++j) {
+            const int q = kAttendQ * j + col;
+            if (quad == 0) { red_ml[wave][q][0] = m[j]; red_ml[wave][q][1] = l[j]; }
+            if (q < n_q) {
 #pragma unroll
-                for (int e = 0; e < kOut; e += 4) {
-                    const int d = sizeof(T) == 2 ? kCols * (4 * quad + r) + e : 64 * (e / 4) + 4 * (4 * quad + r);
-                    *reinterpret_cast<f32x4_t*>(&red_o[wave][col][d]) = f32x4_t{o[e][r], o[e + 1][r], o[e + 2][r], o[e + 3][r]};
-                }
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int e = 0; e < kOut; e += 4) {
+                        const int d = sizeof(T) == 2 ? kCols * (4 * quad + r) + e : 64 * (e / 4) + 4 * (4 * quad + r);
+                        *reinterpret_cast<f32x4_t*>(&red_o[wave][q][d]) = f32x4_t{o[j][e][r], o[j][e + 1][r], o[j][e + 2][r], o[j][e + 3][r]};
+                    }
+            }
         }
         __syncthreads();
         const bool whole = first == 0 && last == seq_units;
-        const size_t part = shared ? (((size_t)tile * a.kv_heads + head) * a.workers + worker) * 2 + (first == 0) : 0;
         for (int i = tid; i < n_q * (D / 4); i += 64 * kW) {
             const int q = i / (D / 4), d = i % (D / 4) * 4;
             float top = red_ml[0][q][0];
@@ -426,8 +451,9 @@ __global__ __launch_bounds__(64 * kW, (kW == 4 ? 3 : kW / 4)) void attend_kernel
                 for (int e = 0; e < 4; ++e) out[e] = (T)(x[e] * inv);
                 if (a.lse && d == 0) a.lse[q_head + q] = (ref + log2_fast(sum)) * 0.6931471805599453f;
             } else {
-                *reinterpret_cast<f32x4_t*>(a.part_o + (part * kAttendQ + q) * D + d) = x;
-                if (d == 0) { a.part_ml[(part * kAttendQ + q) * 2] = top; a.part_ml[(part * kAttendQ + q) * 2 + 1] = sum; }
+                const size_t at = ((((size_t)(q0 + q) / kAttendQ * a.kv_heads + head) * a.workers + worker) * 2 + (first == 0)) * kAttendQ + q % kAttendQ;
+                *reinterpret_cast<f32x4_t*>(a.part_o + at * D + d) = x;
+                if (d == 0) { a.part_ml[at * 2] = top; a.part_ml[at * 2 + 1] = sum; }
             }
         }
         __syncthreads();
@@ -514,6 +540,10 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a)
     }
 }
 
+// Tiles of q-heads that blocks take: one of 16, or two where there are more, which share the rows' registers (20 q-heads of
+// a kv-head read twice, by blocks of one tile each: PLACEHOLDER).
+static int tiles_of(int group) { return group <= kAttendQ ? 1 : (group + 2 * kAttendQ - 1) / (2 * kAttendQ); }
+
 // Blocks that share the sequences of a kv-head evenly, or 0: a block per sequence.
 //
 // Sharing costs the join's launch, 5 us, and a share is a whole number of units; a block of its own has one compute unit's
@@ -524,7 +554,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a)
 // most, lengths spread evenly: 34.6 / 36.1; 64 such sequences 63.3 / 61.0).
 int attend_workers(int batch, int kv_heads, int group, long long max_len, int row_bytes)
 {
-    const long long columns = (long long)kv_heads * ((group + kAttendQ - 1) / kAttendQ);
+    const long long columns = (long long)kv_heads * tiles_of(group);
     if (max_len * 2 * row_bytes <= (columns * batch >= 256 ? 1 << 20 : 1 << 18)) return 0;
     return (int)((768 + columns - 1) / columns);               // three blocks a compute unit
 }
@@ -540,7 +570,7 @@ hipError_t launch(AttendArgs a, hipStream_t st)
     a.join_q = 1;
     for (int n = 2; n <= 256 / (D / 4); ++n)
         if (a.group % n == 0 && (long long)a.batch * a.kv_heads * (a.group / n) >= 512) a.join_q = n;
-    const int tiles = (a.group + kAttendQ - 1) / kAttendQ;
+    const int tiles = tiles_of(a.group);
     const long long max_len = kTable ? a.n_tok + 1 : (long long)a.max_pages * a.page_size;
     const long long blocks = (long long)a.batch * a.kv_heads * tiles;
     const dim3 grid(a.workers ? a.workers : a.batch, a.kv_heads, tiles);
@@ -552,12 +582,16 @@ hipError_t launch(AttendArgs a, hipStream_t st)
     // A block per sequence has eight waves (or 16, as the registers allow) where it would need several turns of four, and
     // there is less than two blocks' work for a compute unit (us at 8 heads of 128 and 512 rows, eight waves / four:
     // 16 sequences 11.5 / 12.4, 32 15.2 / 15.8, 64 29.7 / 27.5, 128 56.6 / 50.4).
-    if (!a.workers && max_len > kUnit && blocks < 512)
-        attend_kernel<T, D, kTable, kWide, false><<<grid, 64 * kWide, 0, st>>>(a);
-    else if (past)
-        attend_kernel<T, D, kTable, kWaves, !kTable><<<grid, 256, 0, st>>>(a);
-    else
-        attend_kernel<T, D, kTable, kWaves, false><<<grid, 256, 0, st>>>(a);
+    if (a.group > kAttendQ) {
+        if (past) attend_kernel<T, D, kTable, kWaves, !kTable, 2><<<grid, 256, 0, st>>>(a);
+        else attend_kernel<T, D, kTable, kWaves, false, 2><<<grid, 256, 0, st>>>(a);
+    } else if (!a.workers && max_len > kUnit && blocks < 512) {
+        attend_kernel<T, D, kTable, kWide, false, 1><<<grid, 64 * kWide, 0, st>>>(a);
+    } else if (past) {
+        attend_kernel<T, D, kTable, kWaves, !kTable, 1><<<grid, 256, 0, st>>>(a);
+    } else {
+        attend_kernel<T, D, kTable, kWaves, false, 1><<<grid, 256, 0, st>>>(a);
+    }
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && a.workers) {
         attend_join_kernel<T, D, kTable><<<dim3(a.batch, a.kv_heads, a.group / a.join_q), 256, 0, st>>>(a);

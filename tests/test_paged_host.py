@@ -87,7 +87,7 @@ def test_which_calls_share_sequences_between_blocks():
     assert not shared(512) and shared(513)                                               # 512 bytes a row
     assert not shared(1024, head_dim=64) and shared(1025, head_dim=64)
     assert not shared(512, head_dim=64, dtype=B.EMS_F32) and shared(513, head_dim=64, dtype=B.EMS_F32)
-    for more in (dict(batch=128), dict(batch=32, q_heads=8, kv_heads=8), dict(batch=64, q_heads=34)):    # the last: two tiles of q-heads
+    for more in (dict(batch=128), dict(batch=32, q_heads=8, kv_heads=8), dict(batch=64, q_heads=66)):    # the last: two blocks' q-heads
         assert not shared(2048, **more) and shared(2049, **more)
     assert shared(2048, batch=127)
     p = lambda budget, ratio, n=1 << 16: B.EmsParams(1, 4, 2, 64, n, 16, budget, merge_ratio=ratio)  # noqa: E731
