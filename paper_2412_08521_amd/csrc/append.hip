@@ -63,7 +63,7 @@ __device__ __forceinline__ void rotate(float& u, float& w, float c, float s)
 
 }  // namespace
 
-// A block takes up to 16 tokens and the rows (queries, keys, values) of some kv-heads.  Its angles are formed once, a value a
+// A block takes some tokens and the rows (queries, keys, values) of some kv-heads.  Its angles are formed once, a value a
 // thread, and shared through LDS: formed by every thread for its own row they were what a prompt waited for (four prompts
 // of 8192 tokens, 40 heads to rotate: 187 us, of which ~150 were vector instructions).  Then a lane group
 // takes a row, a lane two pieces of 16 bytes that hold both halves of its pairs, kAhead rows requested together; a lane
@@ -73,7 +73,7 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a)
 {
     constexpr int kPer = 16 / (int)sizeof(T);                  // elements of a piece: a lane takes two pieces of a row
     constexpr int kItems = D / (2 * kPer), kGroups = 256 / kItems, kAhead = 4;
-    __shared__ __align__(16) float cs[kAppendTokens][2][D / 2];
+    __shared__ __align__(16) float cs[kGroups][2][D / 2];
     const int n_tok = a.tokens;                                // of a block: a power of two
     const int h0 = blockIdx.y * a.heads, heads = min(a.heads, a.kv_heads - h0);       // its kv-heads
     const int tok0 = blockIdx.x * n_tok, all = a.batch * a.n_new;
@@ -176,12 +176,16 @@ template <typename T, int D>
 hipError_t launch(AppendArgs a, hipStream_t st)
 {
     const long long all = (long long)a.batch * a.n_new;
+    const int rows = (a.q ? a.kv_heads * a.group : 0) + 2 * a.kv_heads;
     // What the last-level cache (256 MB) cannot hold goes past it: four prompts of 8192 tokens (805 MB) take 156 us instead
     // of 168, 100 MB 38 instead of 23, whose pages stay for the attention that reads them.
-    const bool past = 2ll * D * (long long)sizeof(T) * all * ((a.q ? a.kv_heads * a.group : 0) + 2 * a.kv_heads) > 256ll << 20;
-    // Tokens and kv-heads of a block: all heads of 16 tokens (of 8 in long prompts, 168 / 182 us), fewer, heads first,
-    // until there are two blocks a compute unit.  Where heads have positions of their own and there is a rotation, a block has one.
-    a.tokens = past ? kAppendTokens / 2 : kAppendTokens;
+    const bool past = 2ll * D * (long long)sizeof(T) * all * rows > 256ll << 20;
+    // Tokens and kv-heads of a block: all heads, and eight rows for a lane group if there are that few (four prompts of 8192
+    // tokens of 48 rows by 16 tokens a block, where eight give it 12 rows: 182 us, by 8: 168); less, heads first, until
+    // there are two blocks a compute unit.  Where heads have positions of their own and there is a rotation, a block has one.
+    constexpr int kGroups = 256 / (D * (int)sizeof(T) / 32);
+    a.tokens = 1;
+    while (a.tokens < kGroups && a.tokens * rows < 8 * kGroups) a.tokens *= 2;
     a.heads = a.pos_sh != 0 && a.rot ? 1 : a.kv_heads;
     const auto blocks = [&] { return (all + a.tokens - 1) / a.tokens * ((a.kv_heads + a.heads - 1) / a.heads); };
     while (a.heads > 1 && blocks() < 512) a.heads = (a.heads + 1) / 2;

@@ -540,8 +540,8 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a)
     }
 }
 
-// Tiles of q-heads that blocks take: one of 16, or two where there are more, which share the rows' registers (20 q-heads of
-// a kv-head read twice, by blocks of one tile each: PLACEHOLDER).
+// Blocks that share a kv-head's q-heads: one takes a tile of 16, or two where there are more, on the same rows (32 kv-heads
+// of 20 q-heads, 605 MB: 109 us, and 172 by blocks of one tile each).
 static int tiles_of(int group) { return group <= kAttendQ ? 1 : (group + 2 * kAttendQ - 1) / (2 * kAttendQ); }
 
 // Blocks that share the sequences of a kv-head evenly, or 0: a block per sequence.
@@ -577,7 +577,8 @@ hipError_t launch(AttendArgs a, hipStream_t st)
     constexpr int kWide = kRowBytesOf<T, D> <= 128 ? 16 : 8;
     // Rows that are read once, and more of them than stay in the caches, go past these (us, plain / past: one sequence of 8
     // heads of 128 and 16384 rows 16.6 / 16.4, 32768 28.8 / 27.1, 131072 97.8 / 86.9; 64 ragged sequences of up to 32768
-    // 763 / 703).  Two tiles of q-heads share their reads (20 q-heads of a kv-head: 80 / 90), tokens of a compact cache their rows.
+    // 763 / 703).  More than 32 q-heads of a kv-head are several blocks', tokens of a compact cache share rows: these profit from
+    // the caches (64 q-heads 62 / 83, a compact cache of 32 x 8 heads and 2048 rows 66 / 70).
     const bool past = !kTable && tiles == 1 && blocks * max_len * 2 * kRowBytesOf<T, D> > 80 << 20;
     // A block per sequence has eight waves (or 16, as the registers allow) where it would need several turns of four, and
     // there is less than two blocks' work for a compute unit (us at 8 heads of 128 and 512 rows, eight waves / four:

@@ -182,8 +182,6 @@ struct AppendArgs {
     bool interleaved, k_wide, v_wide, q_wide, qo_wide;
 };
 
-constexpr int kAppendTokens = 16;
-
 // Attention of one new token per sequence.  Rows are those of a paged cache (page_table), or of a compact cache whose
 // table elements name them (tok_row; one element more is the new token itself).
 struct AttendArgs {
