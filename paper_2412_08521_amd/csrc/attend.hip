@@ -209,7 +209,7 @@ __global__ __launch_bounds__(64 * kW, (kQt == 2 ? 2 : kW == 4 ? 3 : kW / 4)) voi
             for (int i = 0; i < kOut; ++i) o[j][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         }
 
-        // Rows are looked up a batch of 64 ahead in two trips (the table; the position, or the norms), keys and values are
+        // Rows are looked up a batch of 32 ahead in two trips (the table; the position, or the norms), keys and values are
         // requested a step ahead, as soon as the registers that take them are free.
         const int t_first = first * kTurn + wave * kLook + lane % kLook;
         int t_end = 0;                                         // set below: the first trip does not wait for the lengths
