@@ -9,11 +9,12 @@
  *     ems_global_local_score  ->  ems_select  ->  ems_evict_merge
  *
  * and, for the generation that follows, ems_expand (run-time keys/values of the compact
- * cache) and ems_decode_init -> ems_decode_step per generated token.
+ * cache) and ems_decode_init -> ems_decode_attention, ems_decode_step per generated token;
+ * or, over a paged cache, ems_paged_append, ems_paged_attention per generated token.
  *
  * Conventions shared by every entry point
- *   - Every tensor pointer is a DEVICE pointer, contiguous and row-major, owned by the
- *     caller.  The library never allocates, frees or synchronises: work is enqueued on
+ *   - Every tensor pointer is a DEVICE pointer, contiguous and row-major (where no strides
+ *     come with it), owned by the caller.  The library never allocates, frees or synchronises: work is enqueued on
  *     the caller's stream (`hip_stream` is a hipStream_t, NULL = the default stream) and
  *     scratch space comes in through `ws` (sizes from ems_workspace_bytes; 256-byte
  *     aligned; its contents need no initialisation and mean nothing between calls).
@@ -437,7 +438,8 @@ typedef struct {
  *                       What stands behind them is not read, the rows behind them are left as they are.
  *   k, v           in : device [B, Hkv, n_new, D] with any strides (token-major projections, views)
  *   positions_opt  in : device [B, Hkv, n_new] i32 with any strides (head stride 0: shared by the heads), or NULL:
- *                       the position is the row, start[b] + i
+ *                       the position is the row, start[b] + i.  (Negative ones rotate like any other; only a
+ *                       cache with `positions` remembers them and masks their rows.)
  *   inv_freq_opt   in : device [rot_dim / 2] f32; NULL iff rot_dim == 0 (no rotation)
  *   rot_dim        multiple of 16, at most D
  *   q_opt, q_out   device [B, Hq, n_new, D] with any strides: queries to rotate (by the positions of their

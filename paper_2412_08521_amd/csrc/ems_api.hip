@@ -183,7 +183,7 @@ bool ws_ok(const void* ws, size_t have, size_t need)
 
 extern "C" {
 
-int ems_version(void) { return 200; }
+int ems_version(void) { return 300; }
 
 const char* ems_strerror(int status)
 {
