@@ -139,7 +139,7 @@ __device__ __forceinline__ float column_reduce(float v)
 
 }  // namespace
 
-template <typename T, int D, bool kTable, int kW, bool kPast, int kQt>
+template <typename T, int D, bool kTable, int kW, bool kPast, int kQt, bool kSparse>
 __global__ __launch_bounds__(64 * kW, (kQt == 2 ? 2 : kW == 4 ? 3 : kW / 4)) void attend_kernel(AttendArgs a)
 {
     constexpr int kTurn = kW * kLook;                          // rows of a block's turn
@@ -153,7 +153,8 @@ __global__ __launch_bounds__(64 * kW, (kQt == 2 ? 2 : kW == 4 ? 3 : kW / 4)) voi
     constexpr int kVec = sizeof(T) == 2 ? kCols / 2 : 4;       // dwords
     constexpr int kParts = sizeof(T) == 2 ? 1 : D / 64;
     typedef int vec_t __attribute__((ext_vector_type(kVec)));
-    __shared__ __align__(16) int row_of[kW][2][kLook];
+    constexpr int kRing = 128;
+    __shared__ __align__(16) int row_of[kW][kSparse ? kRing : 2 * kLook];       // two batches, or a ring of live rows
     __shared__ __align__(16) float factor_of[kW][2][kTable ? kLook : 4];
     __shared__ __align__(16) float red_o[kW][kQt * kAttendQ][D + 4];
     __shared__ float red_ml[kW][kQt * kAttendQ][2];
@@ -211,7 +212,7 @@ __global__ __launch_bounds__(64 * kW, (kQt == 2 ? 2 : kW == 4 ? 3 : kW / 4)) voi
 
         // Rows are looked up a batch of 32 ahead in two trips (the table; the position, or the norms), keys and values are
         // requested a step ahead, as soon as the registers that take them are free.
-        const int t_first = first * kTurn + wave * kLook + lane % kLook;
+        const int t_first = first * kTurn + wave * kLook + lane % kLook + (kSparse ? lane / kLook * kTurn : 0);
         int t_end = 0;                                         // set below: the first trip does not wait for the lengths
         struct Look { int row, mask; float norm; };            // mask: the position; norms of the token and of its row
         const auto table_trip = [&](int t) -> int {
@@ -243,7 +244,7 @@ __global__ __launch_bounds__(64 * kW, (kQt == 2 ? 2 : kW == 4 ? 3 : kW / 4)) voi
             } else if (k.mask < 0) row = kNoRow;
             const unsigned live = (unsigned)__ballot(row != kNoRow);            // the upper lanes look up what others do
             const int spare = live ? __builtin_amdgcn_readlane(row, __builtin_ctz(live)) : 0;
-            if (lane < kLook) row_of[wave][buf][lane] = row != kNoRow ? row : spare;
+            if (lane < kLook) row_of[wave][kLook * buf + lane] = row != kNoRow ? row : spare;
             __builtin_amdgcn_wave_barrier();
             return live;
         };
@@ -259,7 +260,7 @@ __global__ __launch_bounds__(64 * kW, (kQt == 2 ? 2 : kW == 4 ? 3 : kW / 4)) voi
         const auto load_keys = [&](int buf, int at) {
 #pragma unroll
             for (int i = 0; i < kTiles; ++i) {
-                const char* p = address(a.k, a.k_new, row_of[wave][buf][kStep * at + 16 * i + col]) + 16 * quad;
+                const char* p = address(a.k, a.k_new, row_of[wave][kSparse ? (buf + 16 * i + col) % kRing : kLook * buf + kStep * at + 16 * i + col]) + 16 * quad;
 #pragma unroll
                 for (int c = 0; c < kPieces; ++c) kf[i][c] = read<kPast>(reinterpret_cast<const frag_t*>(p + 64 * c));
             }
@@ -270,7 +271,7 @@ __global__ __launch_bounds__(64 * kW, (kQt == 2 ? 2 : kW == 4 ? 3 : kW / 4)) voi
             for (int i = 0; i < kTiles; ++i)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const char* p = address(a.v, a.v_new, row_of[wave][buf][kStep * at + 16 * i + 4 * quad + r]) + 4 * kVec * col;
+                    const char* p = address(a.v, a.v_new, row_of[wave][kSparse ? (buf + 16 * i + 4 * quad) % kRing + r : kLook * buf + kStep * at + 16 * i + 4 * quad + r]) + 4 * kVec * col;
 #pragma unroll
                     for (int h = 0; h < kParts; ++h) vf[i][r][h] = read<kPast>(reinterpret_cast<const vec_t*>(p + 256 * h));
                 }
@@ -383,7 +384,44 @@ __global__ __launch_bounds__(64 * kW, (kQt == 2 ? 2 : kW == 4 ? 3 : kW / 4)) voi
         }
         const int seq_units = turns_of(len), last = min(u_end - base, seq_units);      // units of this sequence
         t_end = min(last * kTurn, len);
-        if (t_end > t_first - lane % kLook) {
+        if constexpr (kSparse) {
+            // Live rows only, packed: 64 lanes look up two turns, what is live goes to a ring in LDS, which the steps empty.
+            // Behind the last live row stand kStep copies of it, for steps that are not full.
+            const int t0 = first * kTurn + wave * kLook, n_batches = t_end > t0 ? (t_end - t0 + 2 * kTurn - 1) / (2 * kTurn) : 0;
+            Look next = row_trip(t_first, entry);
+            entry = table_trip(t_first + 2 * kTurn);
+            int found = 0, batch = 0;
+            const auto find = [&](int need) {                  // rows until there are `need`, or no more
+                while (found < need && batch < n_batches) {
+                    const bool on = next.row != kNoRow && next.mask >= 0;
+                    const unsigned long long live = __ballot(on);
+                    if (live) {
+                        const int at = found + __builtin_amdgcn_mbcnt_hi((unsigned)(live >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)live, 0));
+                        const int last = __builtin_amdgcn_readlane(next.row, 63 - __builtin_clzll(live));
+                        if (on) row_of[wave][at % kRing] = next.row;
+                        found += __builtin_popcountll(live);
+                        if (lane < kStep) row_of[wave][(found + lane) % kRing] = last;
+                    }
+                    ++batch;
+                    const int t = t_first + 2 * kTurn * batch;
+                    next = row_trip(t, entry);
+                    entry = table_trip(t + 2 * kTurn);
+                }
+                __builtin_amdgcn_wave_barrier();
+            };
+            find(kStep);
+            if (found) {
+                load_keys(0, 0);
+                load_values(0, 0);
+#pragma unroll 1
+                for (int at = 0; at < found;) {
+                    const int n = min(kStep, found - at);
+                    at += n;
+                    find(at + kStep);
+                    step(n == 32 ? ~0u : (1u << n) - 1, 0, 0, min(at, (found - 1) / kStep * kStep), 0);       // (after the last step, its own rows again)
+                }
+            }
+        } else if (t_end > t_first - lane % kLook) {
             // whole batches, and as many steps of the last one as it has rows
             const int rows = t_end - (t_first - lane % kLook), whole = (rows - 1) / kTurn;
             const int n_steps = whole * kSteps + (min(rows - whole * kTurn, kLook) + kStep - 1) / kStep;
@@ -586,15 +624,22 @@ hipError_t launch(AttendArgs a, hipStream_t st)
     // A block per sequence has eight waves (or 16, as the registers allow) where it would need several turns of four, and
     // there is less than two blocks' work for a compute unit (us at 8 heads of 128 and 512 rows, eight waves / four:
     // 16 sequences 11.5 / 12.4, 32 15.2 / 15.8, 64 29.7 / 27.5, 128 56.6 / 50.4).
+    // Where such a cache has positions its live rows are packed into full steps.  That costs a little where all are live and
+    // saves the steps' loads of nothing where few are (us, packed / not: 128 sequences of 1500 rows, 8 heads, 1 % masked 135
+    // / 130, 30 % 97 / 99; 157 of 6451, 60 % 300 / 342; float32, 14 of 109374, 20 q-heads a kv-head, 60 % 328 / 604), and
+    // a microsecond of a short call.
     if (a.group > kAttendQ) {
-        if (past) attend_kernel<T, D, kTable, kWaves, !kTable, 2><<<grid, 256, 0, st>>>(a);
-        else attend_kernel<T, D, kTable, kWaves, false, 2><<<grid, 256, 0, st>>>(a);
+        if (past && a.pos_pages) attend_kernel<T, D, kTable, kWaves, !kTable, 2, !kTable><<<grid, 256, 0, st>>>(a);
+        else if (past) attend_kernel<T, D, kTable, kWaves, !kTable, 2, false><<<grid, 256, 0, st>>>(a);
+        else attend_kernel<T, D, kTable, kWaves, false, 2, false><<<grid, 256, 0, st>>>(a);
     } else if (!a.workers && max_len > kUnit && blocks < 512) {
-        attend_kernel<T, D, kTable, kWide, false, 1><<<grid, 64 * kWide, 0, st>>>(a);
+        attend_kernel<T, D, kTable, kWide, false, 1, false><<<grid, 64 * kWide, 0, st>>>(a);
+    } else if (past && a.pos_pages) {
+        attend_kernel<T, D, kTable, kWaves, !kTable, 1, !kTable><<<grid, 256, 0, st>>>(a);
     } else if (past) {
-        attend_kernel<T, D, kTable, kWaves, !kTable, 1><<<grid, 256, 0, st>>>(a);
+        attend_kernel<T, D, kTable, kWaves, !kTable, 1, false><<<grid, 256, 0, st>>>(a);
     } else {
-        attend_kernel<T, D, kTable, kWaves, false, 1><<<grid, 256, 0, st>>>(a);
+        attend_kernel<T, D, kTable, kWaves, false, 1, false><<<grid, 256, 0, st>>>(a);
     }
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && a.workers) {

@@ -290,6 +290,21 @@ def test_attention_layouts_scales_and_long_tables():
         _attend_case(130, 8, 4, 64, 16, [(53 * i * i) % 300 for i in range(130)], mode, columns=128, masked=0.3)
 
 
+@pytest.mark.parametrize("mode", [BF16, F32])
+@pytest.mark.parametrize("masked", [None, 0.0, 0.02, 0.6, 0.97, 1.0])
+@pytest.mark.parametrize("shape,columns", [
+    ((2, 8, 2, 128, 16, [31, 2050]), 6000),
+    ((3, 3, 3, 64, 7, [900, 0, 64]), 24000),
+    ((2, 40, 2, 64, 5, [1200, 40]), 40000),
+    ((1, 17, 1, 128, 32, [3001]), 6000),
+    ((300, 8, 4, 64, 16, [(53 * i * i) % 260 for i in range(300)]), 64),
+])
+def test_attention_past_the_caches_packs_live_rows(shape, columns, masked, mode):
+    """Tables that admit more than 80 MB, with and without positions; rings of live rows that fill, wrap and run dry."""
+    _log("attend", shape[:5], columns, masked, mode)
+    _attend_case(*shape, mode, masked=masked, columns=columns, seed=len(shape[5]))
+
+
 def test_attention_clamps_lengths_and_skips_pages_that_do_not_exist():
     gen = torch.Generator().manual_seed(5)
     p = B.PagedParams(2, 2, 1, 64, 16, 8, 4)
