@@ -450,54 +450,54 @@ __global__ __launch_bounds__(64 * kW, (kQt == 2 ? 2 : kW == 4 ? 3 : kW / 4)) voi
         for (int j = 0; j < kQt; ++j) l[j] = column_reduce<false>(l[j]);
 
         {
-        // the four waves' results.  Element r of tile e: column kCols (4 quad + r) + e, or 64 h + 4 (4 quad + r) + e % 4.
-        // (The thread's number is taken anew: what is derived from it would hold registers through the loop above.)
-        int tid = threadIdx.x;
-        asm volatile("" : "+v"(tid));
-        const int col = tid % 16, quad = tid % kWave / 16;
+            // the waves' results.  Element r of tile e: column kCols (4 quad + r) + e, or 64 h + 4 (4 quad + r) + e % 4.
+            // (The thread's number is taken anew: what is derived from it would hold registers through the loop above.)
+            int tid = threadIdx.x;
+            asm volatile("" : "+v"(tid));
+            const int col = tid % 16, quad = tid % kWave / 16;
 #pragma unroll
-        for (int j = 0; j < kQt; ++j) {
-            const int q = kAttendQ * j + col;
-            if (quad == 0) { red_ml[wave][q][0] = m[j]; red_ml[wave][q][1] = l[j]; }
-            if (q < n_q) {
+            for (int j = 0; j < kQt; ++j) {
+                const int q = kAttendQ * j + col;
+                if (quad == 0) { red_ml[wave][q][0] = m[j]; red_ml[wave][q][1] = l[j]; }
+                if (q < n_q) {
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
+                    for (int r = 0; r < 4; ++r)
 #pragma unroll
-                    for (int e = 0; e < kOut; e += 4) {
-                        const int d = sizeof(T) == 2 ? kCols * (4 * quad + r) + e : 64 * (e / 4) + 4 * (4 * quad + r);
-                        *reinterpret_cast<f32x4_t*>(&red_o[wave][q][d]) = f32x4_t{o[j][e][r], o[j][e + 1][r], o[j][e + 2][r], o[j][e + 3][r]};
-                    }
+                        for (int e = 0; e < kOut; e += 4) {
+                            const int d = sizeof(T) == 2 ? kCols * (4 * quad + r) + e : 64 * (e / 4) + 4 * (4 * quad + r);
+                            *reinterpret_cast<f32x4_t*>(&red_o[wave][q][d]) = f32x4_t{o[j][e][r], o[j][e + 1][r], o[j][e + 2][r], o[j][e + 3][r]};
+                        }
+                }
             }
-        }
-        __syncthreads();
-        const bool whole = first == 0 && last == seq_units;
-        for (int i = tid; i < n_q * (D / 4); i += 64 * kW) {
-            const int q = i / (D / 4), d = i % (D / 4) * 4;
-            float top = red_ml[0][q][0];
+            __syncthreads();
+            const bool whole = first == 0 && last == seq_units;
+            for (int i = tid; i < n_q * (D / 4); i += 64 * kW) {
+                const int q = i / (D / 4), d = i % (D / 4) * 4;
+                float top = red_ml[0][q][0];
 #pragma unroll
-            for (int w = 1; w < kW; ++w) top = fmaxf(top, red_ml[w][q][0]);
-            const float ref = top > -INFINITY ? top : 0.f;
-            float sum = 0.f;
-            f32x4_t x = {0.f, 0.f, 0.f, 0.f};
+                for (int w = 1; w < kW; ++w) top = fmaxf(top, red_ml[w][q][0]);
+                const float ref = top > -INFINITY ? top : 0.f;
+                float sum = 0.f;
+                f32x4_t x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int w = 0; w < kW; ++w) {
-                const float f = exp2_fast(red_ml[w][q][0] - ref);
-                sum += f * red_ml[w][q][1];
-                x += f * *reinterpret_cast<const f32x4_t*>(&red_o[w][q][d]);
+                for (int w = 0; w < kW; ++w) {
+                    const float f = exp2_fast(red_ml[w][q][0] - ref);
+                    sum += f * red_ml[w][q][1];
+                    x += f * *reinterpret_cast<const f32x4_t*>(&red_o[w][q][d]);
+                }
+                if (whole) {
+                    const float inv = sum == 0.f ? 0.f : 1.f / sum;                     // (NaN stays)
+                    T* out = reinterpret_cast<T*>(a.out) + (q_head + q) * D + d;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) out[e] = (T)(x[e] * inv);
+                    if (a.lse && d == 0) a.lse[q_head + q] = (ref + log2_fast(sum)) * 0.6931471805599453f;
+                } else {
+                    const size_t at = ((((size_t)(q0 + q) / kAttendQ * a.kv_heads + head) * a.workers + worker) * 2 + (first == 0)) * kAttendQ + q % kAttendQ;
+                    *reinterpret_cast<f32x4_t*>(a.part_o + at * D + d) = x;
+                    if (d == 0) { a.part_ml[at * 2] = top; a.part_ml[at * 2 + 1] = sum; }
+                }
             }
-            if (whole) {
-                const float inv = sum == 0.f ? 0.f : 1.f / sum;                     // (NaN stays)
-                T* out = reinterpret_cast<T*>(a.out) + (q_head + q) * D + d;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) out[e] = (T)(x[e] * inv);
-                if (a.lse && d == 0) a.lse[q_head + q] = (ref + log2_fast(sum)) * 0.6931471805599453f;
-            } else {
-                const size_t at = ((((size_t)(q0 + q) / kAttendQ * a.kv_heads + head) * a.workers + worker) * 2 + (first == 0)) * kAttendQ + q % kAttendQ;
-                *reinterpret_cast<f32x4_t*>(a.part_o + at * D + d) = x;
-                if (d == 0) { a.part_ml[at * 2] = top; a.part_ml[at * 2 + 1] = sum; }
-            }
-        }
-        __syncthreads();
+            __syncthreads();
         }
         base += seq_units;
         u = base;
@@ -607,7 +607,7 @@ hipError_t launch(AttendArgs a, hipStream_t st)
     a.page_shift = 0;
     while (1 << a.page_shift < a.page_size) ++a.page_shift;
     a.page_magic = a.page_table ? (unsigned)(((1ull << (31 + a.page_shift)) + a.page_size - 1) / a.page_size) : 0;
-    // q-heads of a join block: as many as it has lanes for, halved (to a divisor of the group) while there are few blocks
+    // q-heads of a join block: as many as it has lanes for, of the divisors of the group that leave two blocks a compute unit
     a.join_q = 1;
     for (int n = 2; n <= 256 / (D / 4); ++n)
         if (a.group % n == 0 && (long long)a.batch * a.kv_heads * (a.group / n) >= 512) a.join_q = n;
@@ -621,13 +621,15 @@ hipError_t launch(AttendArgs a, hipStream_t st)
     // 763 / 703).  More than 32 q-heads of a kv-head are several blocks', tokens of a compact cache share rows: these profit from
     // the caches (64 q-heads 62 / 83, a compact cache of 32 x 8 heads and 2048 rows 66 / 70).
     const bool past = !kTable && tiles == 1 && blocks * max_len * 2 * kRowBytesOf<T, D> > 80 << 20;
-    // A block per sequence has eight waves (or 16, as the registers allow) where it would need several turns of four, and
-    // there is less than two blocks' work for a compute unit (us at 8 heads of 128 and 512 rows, eight waves / four:
-    // 16 sequences 11.5 / 12.4, 32 15.2 / 15.8, 64 29.7 / 27.5, 128 56.6 / 50.4).
+    //
     // Where such a cache has positions its live rows are packed into full steps.  That costs a little where all are live and
     // saves the steps' loads of nothing where few are (us, packed / not: 128 sequences of 1500 rows, 8 heads, 1 % masked 135
     // / 130, 30 % 97 / 99; 157 of 6451, 60 % 300 / 342; float32, 14 of 109374, 20 q-heads a kv-head, 60 % 328 / 604), and
     // a microsecond of a short call.
+    //
+    // A block per sequence has eight waves (or 16, as the registers allow) where it would need several turns of four, and
+    // there is less than two blocks' work for a compute unit (us at 8 heads of 128 and 512 rows, eight waves / four:
+    // 16 sequences 11.5 / 12.4, 32 15.2 / 15.8, 64 29.7 / 27.5, 128 56.6 / 50.4).
     if (a.group > kAttendQ) {
         if (past && a.pos_pages) attend_kernel<T, D, kTable, kWaves, !kTable, 2, !kTable><<<grid, 256, 0, st>>>(a);
         else if (past) attend_kernel<T, D, kTable, kWaves, !kTable, 2, false><<<grid, 256, 0, st>>>(a);
