@@ -49,6 +49,14 @@ __device__ __forceinline__ int page_of(const AttendArgs& a, int t) { return (int
 // a value that is the same in every lane, for the scalar registers
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
+// What lanes of a wave wrote to LDS is for its other lanes, and may be written anew once those have read it.  A wave's LDS
+// accesses are carried out in their order; the fence holds the compiler to it and is no instruction.
+__device__ __forceinline__ void wave_handover()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // Inclusive sums over the lanes of a wave.
 template <int kCtrl, int kRowMask>
 __device__ __forceinline__ int dpp_or_zero(int v) { return __builtin_amdgcn_update_dpp(0, v, kCtrl, kRowMask, 0xf, false); }
@@ -238,6 +246,7 @@ __global__ __launch_bounds__(64 * kW, (kQt == 2 ? 2 : kW == 4 ? 3 : kW / 4)) voi
         // already and whose values may meet their zero weights (row 0 where none is live, whose steps are left out).
         const auto settle = [&](int t, const Look& k, int buf) -> unsigned {
             int row = k.row;
+            wave_handover();
             if constexpr (kTable) {
                 if (t >= t_end) row = kNoRow;
                 if (lane < kLook) factor_of[wave][buf][lane] = row == kNewRow ? 1.f : k.norm > 0.f ? __builtin_bit_cast(float, k.mask) / k.norm : 0.f;
@@ -245,7 +254,7 @@ __global__ __launch_bounds__(64 * kW, (kQt == 2 ? 2 : kW == 4 ? 3 : kW / 4)) voi
             const unsigned live = (unsigned)__ballot(row != kNoRow);            // the upper lanes look up what others do
             const int spare = live ? __builtin_amdgcn_readlane(row, __builtin_ctz(live)) : 0;
             if (lane < kLook) row_of[wave][kLook * buf + lane] = row != kNoRow ? row : spare;
-            __builtin_amdgcn_wave_barrier();
+            wave_handover();
             return live;
         };
         const auto address = [&](const void* rows, const void* fresh, int r) -> const char* {
@@ -392,6 +401,7 @@ __global__ __launch_bounds__(64 * kW, (kQt == 2 ? 2 : kW == 4 ? 3 : kW / 4)) voi
             entry = table_trip(t_first + 2 * kTurn);
             int found = 0, batch = 0;
             const auto find = [&](int need) {                  // rows until there are `need`, or no more
+                wave_handover();
                 while (found < need && batch < n_batches) {
                     const bool on = next.row != kNoRow && next.mask >= 0;
                     const unsigned long long live = __ballot(on);
@@ -407,7 +417,7 @@ __global__ __launch_bounds__(64 * kW, (kQt == 2 ? 2 : kW == 4 ? 3 : kW / 4)) voi
                     next = row_trip(t, entry);
                     entry = table_trip(t + 2 * kTurn);
                 }
-                __builtin_amdgcn_wave_barrier();
+                wave_handover();
             };
             find(kStep);
             if (found) {
