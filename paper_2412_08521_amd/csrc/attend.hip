@@ -10,8 +10,10 @@
 //                       O^T = V^T P^T lane l: its S^T elements are the right operand as they are (rows 4 (l / 16) + r of
 //                                     a tile); the left one is a 16-byte piece of each of those rows, transposed between
 //                                     registers (two 16-bit elements a v_perm; float32 needs none)
-//                     Probabilities go into the products as two bf16 pieces, high and rest (2^-17 of a probability is
-//                     left out; one piece would leave 2^-9, as much as the output's own rounding).
+//                     Probabilities go into the products as the exact sum of three bf16 pieces (a float's 24 digits are three
+//                     times eight): the numerator's weights are the denominator's.  Two would leave 2^-17 of a probability,
+//                     one 2^-8, as much as the output's own rounding; the third takes at most 1 % of a call's time (us, two /
+//                     three: the ragged sequences below 675 / 672, 32 x 8 compact heads of 2048 rows 65.8 / 66.0).
 //                     Memory bounds it: the products fill 6 % of the matrix pipes.  12 waves a compute unit keep 16 KB
 //                     each in flight; 64 sequences of up to 32768 rows, 8 heads of 128 (4.5 GB): 677 us, 6.6 TB/s.
 // attend_join_kernel  a sequence that several blocks share: their outputs, weighted by their maxima and sums (5 us, a
@@ -343,14 +345,17 @@ __global__ __launch_bounds__(64 * kW, (kQt == 2 ? 2 : kW == 4 ? 3 : kW / 4)) voi
                         for (int r = 0; r < 4; ++r) { s[j][i][r] = exp2_fast(s[j][i][r] - ref); l[j] += s[j][i][r]; }
                 }
                 if constexpr (sizeof(T) == 2) {
-                    bf16x8_t high[kQt], rest[kQt];
+                    bf16x8_t piece[kQt][3];
 #pragma unroll
                     for (int j = 0; j < kQt; ++j)
 #pragma unroll
                         for (int r = 0; r < 8; ++r) {
-                            const float p = s[j][r / 4][r % 4];
-                            high[j][r] = (bf16_t)p;
-                            rest[j][r] = (bf16_t)(p - (float)high[j][r]);
+                            float p = s[j][r / 4][r % 4];
+#pragma unroll
+                            for (int n = 0; n < 3; ++n) {
+                                piece[j][n][r] = (bf16_t)p;
+                                p -= (float)piece[j][n][r];
+                            }
                         }
 #pragma unroll
                     for (int e = 0; e < kCols; ++e) {
@@ -360,10 +365,10 @@ __global__ __launch_bounds__(64 * kW, (kQt == 2 ? 2 : kW == 4 ? 3 : kW / 4)) voi
                             x[d] = __builtin_amdgcn_perm(vf[(2 * d + 1) / 4][(2 * d + 1) % 4][0][e / 2], vf[2 * d / 4][2 * d % 4][0][e / 2],
                                                          e % 2 ? 0x07060302 : 0x05040100);
 #pragma unroll
-                        for (int j = 0; j < kQt; ++j) {
-                            o[j][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, x), high[j], o[j][e], 0, 0, 0);
-                            o[j][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, x), rest[j], o[j][e], 0, 0, 0);
-                        }
+                        for (int j = 0; j < kQt; ++j)
+#pragma unroll
+                            for (int n = 0; n < 3; ++n)
+                                o[j][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, x), piece[j][n], o[j][e], 0, 0, 0);
                     }
                 } else {
 #pragma unroll
