@@ -226,14 +226,14 @@ __global__ __launch_bounds__(64 * kW, (kQt == 2 ? 2 : kW == 4 ? 3 : kW / 4)) voi
         int t_end = 0;                                         // set below: the first trip does not wait for the lengths
         struct Look { int row, mask; float norm; };            // mask: the position; norms of the token and of its row
         const auto table_trip = [&](int t) -> int {
-            if constexpr (kTable) return t < a.n_tok ? a.tok_row[(size_t)unit * a.n_tok + t] : t == a.n_tok ? kNewRow : kNoRow;
+            if constexpr (kTable) return t < a.n_tok ? a.tok_row[(size_t)unit * a.n_tok + t] : kNoRow;
             return t < a.max_pages * a.page_size ? a.page_table[(size_t)b * a.max_pages + page_of(a, t)] : kNoRow;
         };
         const auto row_trip = [&](int t, int entry) -> Look {
             Look r{kNoRow, 0, 0.f};
             if constexpr (kTable) {
-                r.row = entry;
-                if (entry >= a.budget || entry < kNewRow) r.row = kNoRow;
+                // (the index says which is the new token: a caller's element may hold any number)
+                r.row = t == a.n_tok ? kNewRow : (unsigned)entry < (unsigned)a.budget ? entry : kNoRow;
                 if (r.row >= 0) {
                     r.norm = a.row_norm[(size_t)unit * a.budget + entry];
                     r.mask = __builtin_bit_cast(int, a.tok_norm[(size_t)unit * a.n_tok + t]);
