@@ -115,6 +115,7 @@ class PagedParams:
         put("torch_dtype", torch.float32 if self.dtype == EMS_F32 else torch.bfloat16)
         put("_q_row", (self.batch, self.q_heads, self.head_dim))
         put("_pages", (self.num_pages, self.kv_heads, self.page_size, self.head_dim))
+        put("_positions", self._pages[:3])
         put("_table", (self.batch, self.max_pages))
 
     def c(self) -> ems_paged_params:
@@ -462,8 +463,15 @@ class DecodeState:
         self.tok_pos.fill_(-1)
         self.tok_row.fill_(-1)
 
+    def __setattr__(self, name, x):
+        old = self.__dict__.get(name) if name in STATE_FIELDS else None
+        if old is not None:                                  # a tensor in another's place has to be like it; its address is taken anew
+            _check_dense(x, old.get_device(), old.dtype, old.shape, name)
+            self.__dict__["_c"] = None
+        self.__dict__[name] = x
+
     def c(self) -> ems_decode_state:
-        if getattr(self, "_c", None) is None:                # the tensors never move
+        if getattr(self, "_c", None) is None:                # made once: the tensors do not move
             self._c = ems_decode_state(*[getattr(self, name).data_ptr() for name in STATE_FIELDS])
         return self._c
 
@@ -612,7 +620,7 @@ def ems_decode_attention(p: EmsParams, st: DecodeState, q_new, k_new, v_new, wan
     _check_dense(v_new, dev, dt, shape, "v_new")
     table = (p.batch, p.kv_heads, _table_length(p.seq_len, p.window, p.budget, p.merge_ratio))
     _check_dense(st.k_cache, dev, dt, (p.batch, p.kv_heads, p.budget + 1, p.head_dim), "k_cache")
-    _check_dense(st.tok_row, dev, torch.int32, table, "tok_row")
+    _check_dense(st.tok_row, dev, torch.int32, table, "tok_row")        # (the state's other tensors go with these two)
     ws = _check_ws(ws, dev, ems_decode_attention_workspace_bytes, p)
     o, lse = _attention_out(out, dev, want_lse, heads + shape[2:], dt)
     cs = st.c()
@@ -648,18 +656,26 @@ class PagedCache:
         _check_dense(v_pages, dev, p.torch_dtype, p._pages, "v_pages")
         _check_dense(page_table, dev, torch.int32, p._table, "page_table")
         if positions is not None:
-            _check_dense(positions, dev, torch.int32, p._pages[:3], "positions")
+            _check_dense(positions, dev, torch.int32, p._positions, "positions")
         self.k_pages, self.v_pages, self.page_table, self.positions = k_pages, v_pages, page_table, positions
         self.device_index = dev
 
+    def __setattr__(self, name, t):
+        # a tensor in another's place (a longer table, a larger pool) is checked here, its shape by the next call
+        if name in self.__dict__ and name in ("k_pages", "v_pages", "page_table", "positions") and (t is not None or name != "positions"):
+            dtype = self.k_pages.dtype if name in ("k_pages", "v_pages") else torch.int32
+            _check_dense(t, self.device_index, dtype, t.shape, name)
+        self.__dict__[name] = t
+
     def _c(self, p: PagedParams, dev):
         """The cache for a call on device `dev` with parameters that have to be those of its tensors."""
-        k = self.k_pages
-        if k.shape != p._pages or self.page_table.shape != p._table or k.dtype != p.torch_dtype:
+        k, pos = self.k_pages, self.positions
+        if (k.shape != p._pages or self.v_pages.shape != p._pages or self.page_table.shape != p._table or k.dtype != p.torch_dtype or
+                (pos is not None and pos.shape != p._positions)):
             raise ValueError(f"a cache of {tuple(k.shape)} rows with a table of {tuple(self.page_table.shape)} does not fit {p}")
         if self.device_index != dev:
             raise ValueError("the cache must be on the current device")
-        return C.byref(ems_paged_cache(k.data_ptr(), self.v_pages.data_ptr(), _ptr(self.positions), self.page_table.data_ptr()))
+        return C.byref(ems_paged_cache(k.data_ptr(), self.v_pages.data_ptr(), _ptr(pos), self.page_table.data_ptr()))
 
 
 def alloc_paged_cache(p: PagedParams, page_table, positions: bool = False) -> PagedCache:
@@ -667,7 +683,7 @@ def alloc_paged_cache(p: PagedParams, page_table, positions: bool = False) -> Pa
     dev = page_table.device
     return PagedCache(p, torch.zeros(p._pages, dtype=p.torch_dtype, device=dev),
                       torch.zeros(p._pages, dtype=p.torch_dtype, device=dev), page_table,
-                      torch.full(p._pages[:3], -1, dtype=torch.int32, device=dev) if positions else None)
+                      torch.full(p._positions, -1, dtype=torch.int32, device=dev) if positions else None)
 
 
 def _rows(t, dev, dtype, shape, name):
