@@ -401,8 +401,8 @@ int ems_decode_attention(const ems_params* p, const ems_decode_state* state,
  * [0, num_pages) are neither written nor attended, lengths are clamped to [0, max_pages * page_size].
  */
 typedef struct {
-    int32_t batch;         /* B >= 1 sequences */
-    int32_t q_heads;       /* Hq >= 1 */
+    int32_t batch;         /* B >= 1 sequences, < 2^24 (B * Hq <= 2^24) */
+    int32_t q_heads;       /* Hq >= 1, <= 65535 */
     int32_t kv_heads;      /* Hkv >= 1, divides Hq */
     int32_t head_dim;      /* D in {64, 128} */
     int32_t page_size;     /* rows of a page, >= 1, any */
@@ -431,7 +431,8 @@ typedef struct {
  * (x[2e], x[2e+1]), becomes
  *     (x1 cos a - x2 sin a, x2 cos a + x1 sin a),   a = position * f[e]
  * with the angle formed in 64 bits and one rounding to `dtype`; other elements, and values, are copied bit for bit.
- *   n_new          tokens per sequence in k, v and q, >= 1
+ *   n_new          tokens per sequence in k, v and q, >= 1 (B * n_new * (Hq + 2 Hkv) < 2^31, and B * n_new at most
+ *                       16 (2^24 - 1) for float32 rows of 128, twice that for rows of half the bytes)
  *   start          in : device [B] i32 rows the sequence holds already.  Tokens whose row falls outside the table
  *                       are not stored.
  *   new_len_opt    in : device [B] i32 how many of the n_new tokens there are (a padded batch), or NULL = all.

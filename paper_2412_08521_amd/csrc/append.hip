@@ -171,6 +171,16 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a)
     }
 }
 
+// Tokens of a block: eight rows for a lane group if there are that few (four prompts of 8192 tokens of 48 rows by 16 tokens a
+// block, where eight give it 12 rows: 182 us, by 8: 168).
+int append_tokens(int rows, int row_bytes)
+{
+    const int groups = 256 / (row_bytes / 32);
+    int n = 1;
+    while (n < groups && n * rows < 8 * groups) n *= 2;
+    return n;
+}
+
 namespace {
 template <typename T, int D>
 hipError_t launch(AppendArgs a, hipStream_t st)
@@ -180,12 +190,9 @@ hipError_t launch(AppendArgs a, hipStream_t st)
     // What the last-level cache (256 MB) cannot hold goes past it: four prompts of 8192 tokens (805 MB) take 156 us instead
     // of 168, 100 MB 38 instead of 23, whose pages stay for the attention that reads them.
     const bool past = 2ll * D * (long long)sizeof(T) * all * rows > 256ll << 20;
-    // Tokens and kv-heads of a block: all heads, and eight rows for a lane group if there are that few (four prompts of 8192
-    // tokens of 48 rows by 16 tokens a block, where eight give it 12 rows: 182 us, by 8: 168); less, heads first, until
-    // there are two blocks a compute unit.  Where heads have positions of their own and there is a rotation, a block has one.
-    constexpr int kGroups = 256 / (D * (int)sizeof(T) / 32);
-    a.tokens = 1;
-    while (a.tokens < kGroups && a.tokens * rows < 8 * kGroups) a.tokens *= 2;
+    // Tokens and kv-heads of a block: all heads, and tokens for eight rows a lane group; less, heads first, until there are
+    // two blocks a compute unit.  Where heads have positions of their own and there is a rotation, a block has one.
+    a.tokens = append_tokens(rows, D * (int)sizeof(T));
     a.heads = a.pos_sh != 0 && a.rot ? 1 : a.kv_heads;
     const auto blocks = [&] { return (all + a.tokens - 1) / a.tokens * ((a.kv_heads + a.heads - 1) / a.heads); };
     while (a.heads > 1 && blocks() < 512) a.heads = (a.heads + 1) / 2;

@@ -583,10 +583,13 @@ static float scale_log2e(float softmax_scale, int head_dim)
     return (float)(scale * 1.4426950408889634074);
 }
 
+// a launch has less than 2^32 threads in x, 256 a block at most where blocks are many
+constexpr int kMostBlocks = 1 << 24;
+
 // grid dimensions, and units of work as 32-bit numbers
 static bool attend_grid_ok(int batch, int q_heads, long long max_len)
 {
-    return (long long)batch * q_heads <= (1 << 24) && q_heads <= 65535 &&
+    return batch < kMostBlocks && (long long)batch * q_heads <= (1 << 24) && q_heads <= 65535 &&
            batch * ((max_len + ems::kAttendUnit - 1) / ems::kAttendUnit) <= (1ll << 30);
 }
 
@@ -713,6 +716,8 @@ int ems_paged_append(const ems_paged_params* p, const ems_paged_cache* cache, in
     if (rot_dim % 16) return EMS_ERR_UNSUPPORTED;
     if ((long long)p->batch * n_new > 0x7fffffffll / (p->q_heads + 2 * p->kv_heads)) return EMS_ERR_UNSUPPORTED;
     const bool f32 = p->dtype == EMS_F32;
+    const int tokens = ems::append_tokens((q_opt ? p->q_heads : 0) + 2 * p->kv_heads, p->head_dim * (f32 ? 4 : 2));
+    if ((long long)p->batch * n_new > (kMostBlocks - 1ll) * tokens) return EMS_ERR_UNSUPPORTED;
     ems::AppendArgs a{};
     a.k = k; a.k_sb = k_strides->batch; a.k_sh = k_strides->head; a.k_sn = k_strides->token; a.k_wide = wide_rows(k, *k_strides, f32);
     a.v = v; a.v_sb = v_strides->batch; a.v_sh = v_strides->head; a.v_sn = v_strides->token; a.v_wide = wide_rows(v, *v_strides, f32);

@@ -214,6 +214,7 @@ struct AttendArgs {
 constexpr int kAttendQ = 16;    // q-heads of a group that a block takes: the columns of a matrix product
 constexpr int kAttendUnit = 128;        // rows that work is counted in
 int attend_workers(int batch, int kv_heads, int group, long long max_len, int row_bytes);      // AttendArgs::workers
+int append_tokens(int rows, int row_bytes);    // tokens of a block where there are many, `rows` (queries, keys, values) each
 hipError_t launch_append(const AppendArgs& a, int head_dim, bool f32, hipStream_t st);
 hipError_t launch_attend(const AttendArgs& a, bool f32, hipStream_t st);
 
