@@ -436,7 +436,7 @@ typedef struct {
  *   start          in : device [B] i32 rows the sequence holds already.  Tokens whose row falls outside the table
  *                       are not stored.
  *   new_len_opt    in : device [B] i32 how many of the n_new tokens there are (a padded batch), or NULL = all.
- *                       What stands behind them is not read, the rows behind them are left as they are.
+ *                       What k, v and q hold behind them is not read, the rows behind them are left as they are.
  *   k, v           in : device [B, Hkv, n_new, D] with any strides (token-major projections, views)
  *   positions_opt  in : device [B, Hkv, n_new] i32 with any strides (head stride 0: shared by the heads), or NULL:
  *                       the position is the row, start[b] + i.  (Negative ones rotate like any other; only a
@@ -466,8 +466,8 @@ int ems_paged_append(const ems_paged_params* p, const ems_paged_cache* cache, in
  * over the live rows t < lens[b] of the kv-head, with p_t = exp(scale q.k_t),
  *     out = sum_t p_t v_t / sum_t p_t        lse = ln sum_t p_t
  * A sequence-head without a live row (length 0, or every row masked) gives zeros and -inf.  What masked rows and
- * rows behind the length hold does not matter; a live row whose logit is -inf weighs nothing, other infinities and
- * NaN in a live row give what is not finite.
+ * rows behind the length hold does not matter; a live row whose logit is -inf weighs nothing (its value counts 0
+ * times, so it has to be finite), other infinities and NaN in a live row give what is not finite.
  *   lens           in : device [B] i32 rows of every sequence
  *   q              in : device [B, Hq, D] with any strides (batch, head; token is unused)
  *   out            out: device [B, Hq, D] `dtype`, contiguous, 16-byte aligned, apart from the inputs

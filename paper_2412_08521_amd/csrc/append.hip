@@ -188,7 +188,8 @@ hipError_t launch(AppendArgs a, hipStream_t st)
     const long long all = (long long)a.batch * a.n_new;
     const int rows = (a.q ? a.kv_heads * a.group : 0) + 2 * a.kv_heads;
     // What the last-level cache (256 MB) cannot hold goes past it: four prompts of 8192 tokens (805 MB) take 156 us instead
-    // of 168, 100 MB 38 instead of 23, whose pages stay for the attention that reads them.
+    // of 168, 100 MB 38 instead of 23, whose pages stay for the attention that reads them.  (Between them nothing was compared; 149 MB
+    // take 44 us, staying.)
     const bool past = 2ll * D * (long long)sizeof(T) * all * rows > 256ll << 20;
     // Tokens and kv-heads of a block: all heads, and tokens for eight rows a lane group; less, heads first, until there are
     // two blocks a compute unit.  Where heads have positions of their own and there is a rotation, a block has one.

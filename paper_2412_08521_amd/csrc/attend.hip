@@ -14,7 +14,7 @@
 //                     times eight): the numerator's weights are the denominator's.  Two would leave 2^-17 of a probability,
 //                     one 2^-8, as much as the output's own rounding; the third takes at most 1 % of a call's time (us, two /
 //                     three: the ragged sequences below 675 / 672, 32 x 8 compact heads of 2048 rows 65.8 / 66.0).
-//                     Memory bounds it: the products fill 6 % of the matrix pipes.  12 waves a compute unit keep 16 KB
+//                     Memory bounds it: the products fill 9 % of the matrix pipes.  12 waves a compute unit keep 16 KB
 //                     each in flight; 64 sequences of up to 32768 rows, 8 heads of 128 (4.5 GB): 677 us, 6.6 TB/s.
 // attend_join_kernel  a sequence that several blocks share: their outputs, weighted by their maxima and sums (5 us, a
 //                     launch and three trips).
@@ -607,12 +607,14 @@ static int tiles_of(int group) { return group <= kAttendQ ? 1 : (group + 2 * kAt
 // 256 KB of keys and values (us, block per sequence / shared, one sequence of 8 heads, head size 128: 512 rows 10.5 /
 // 11.8, 1024 rows 16.0 / 12.1; 4 heads of 64: 512 rows 8.2 / 10.7, 1024 rows 11.2 / 10.6), and up to 1 MB while there is
 // a block for every compute unit (32 sequences of 8 heads and 1024 rows 26.9 / 34.8, 2048 rows 49.7 / 58.2; 2048 rows at
-// most, lengths spread evenly: 34.6 / 36.1; 64 such sequences 63.3 / 61.0).
+// most, lengths spread evenly: 34.6 / 36.1; 64 such sequences 63.3 / 61.0).  At the bounds themselves the two are near each other.
 int attend_workers(int batch, int kv_heads, int group, long long max_len, int row_bytes)
 {
     const long long columns = (long long)kv_heads * tiles_of(group);
     if (max_len * 2 * row_bytes <= (columns * batch >= 256 ? 1 << 20 : 1 << 18)) return 0;
-    return (int)((768 + columns - 1) / columns);               // three blocks a compute unit
+    // 768 blocks, rounded up: three a compute unit.  (Where there are two tiles of q-heads in a block, in float32 or at head size
+    // 128, two fit: a third of the blocks starts after the others.)
+    return (int)((768 + columns - 1) / columns);
 }
 
 namespace {
@@ -631,10 +633,12 @@ hipError_t launch(AttendArgs a, hipStream_t st)
     const long long blocks = (long long)a.batch * a.kv_heads * tiles;
     const dim3 grid(a.workers ? a.workers : a.batch, a.kv_heads, tiles);
     constexpr int kWide = kRowBytesOf<T, D> <= 128 ? 16 : 8;
-    // Rows that are read once, and more of them than stay in the caches, go past these (us, plain / past: one sequence of 8
+    // Rows that a block alone reads, and more of them than stay in the caches, go past these (us, plain / past: one sequence of 8
     // heads of 128 and 16384 rows 16.6 / 16.4, 32768 28.8 / 27.1, 131072 97.8 / 86.9; 64 ragged sequences of up to 32768
     // 763 / 703).  More than 32 q-heads of a kv-head are several blocks', tokens of a compact cache share rows: these profit from
-    // the caches (64 q-heads 62 / 83, a compact cache of 32 x 8 heads and 2048 rows 66 / 70).
+    // the caches (64 q-heads 62 / 83, a compact cache of 32 x 8 heads and 2048 rows 66 / 70).  The lengths are on the device: what
+    // the table admits decides, and a table wider than its sequences costs what it would not have to (32 sequences of 1024
+    // rows, 8 heads, 26.3 us by a table of 1024 rows, 31.7 by one of 4096 or 16384).
     const bool past = !kTable && tiles == 1 && blocks * max_len * 2 * kRowBytesOf<T, D> > 80 << 20;
     //
     // Where such a cache has positions its live rows are packed into full steps.  That costs a little where all are live and
