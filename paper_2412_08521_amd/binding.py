@@ -464,11 +464,15 @@ class DecodeState:
         self.tok_row.fill_(-1)
 
     def __setattr__(self, name, x):
-        old = self.__dict__.get(name) if name in STATE_FIELDS else None
-        if old is not None:                                  # a tensor in another's place has to be like it; its address is taken anew
-            _check_dense(x, old.get_device(), old.dtype, old.shape, name)
-            self.__dict__["_c"] = None
+        if name in STATE_FIELDS and x is not None:           # a tensor in another's place has to be like the first one there
+            like = self.__dict__.setdefault("_like", {})
+            if name in like:
+                _check_dense(x, *like[name], name)
+            else:
+                like[name] = (x.get_device(), x.dtype, x.shape)
         self.__dict__[name] = x
+        if name in STATE_FIELDS:
+            self.__dict__["_c"] = None                       # its address is taken anew
 
     def c(self) -> ems_decode_state:
         if getattr(self, "_c", None) is None:                # made once: the tensors do not move
@@ -658,12 +662,12 @@ class PagedCache:
         if positions is not None:
             _check_dense(positions, dev, torch.int32, p._positions, "positions")
         self.k_pages, self.v_pages, self.page_table, self.positions = k_pages, v_pages, page_table, positions
-        self.device_index = dev
+        self.device_index, self.dtype = dev, p.torch_dtype
 
     def __setattr__(self, name, t):
         # a tensor in another's place (a longer table, a larger pool) is checked here, its shape by the next call
-        if name in self.__dict__ and name in ("k_pages", "v_pages", "page_table", "positions") and (t is not None or name != "positions"):
-            dtype = self.k_pages.dtype if name in ("k_pages", "v_pages") else torch.int32
+        if t is not None and name in self.__dict__ and name in ("k_pages", "v_pages", "page_table", "positions"):
+            dtype = self.dtype if name in ("k_pages", "v_pages") else torch.int32
             _check_dense(t, self.device_index, dtype, t.shape, name)
         self.__dict__[name] = t
 

@@ -88,3 +88,27 @@ def test_paged_cache_refuses_replaced_tensors(host_device):
     c.page_table, c.positions = wide, None
     got = c._c(B.PagedParams(2, 4, 2, 64, 16, 10, 9), -1)._obj
     assert got.page_table == wide.data_ptr() and got.positions is None
+
+
+def test_tensors_that_are_let_go(host_device):
+    """None frees a tensor's memory; a call has nothing to run on then, old addresses least of all."""
+    p = B.EmsParams(2, 4, 2, 64, 400, 16, 100, merge_ratio=0.5)
+    st = _state(p)
+    st.c()
+    st.v_cache = None
+    with pytest.raises(AttributeError):
+        st.c()
+    with pytest.raises(ValueError, match="v_cache"):
+        st.v_cache = st.k_cache[:1].clone()
+    st.v_cache = st.k_cache.clone()
+    assert st.c().v_cache == st.v_cache.data_ptr()
+    pp = B.PagedParams(2, 4, 2, 64, 16, 10, 5)
+    rows = [torch.zeros((10, 2, 16, 64), dtype=torch.bfloat16) for _ in range(2)]
+    cache = B.PagedCache(pp, *rows, torch.zeros((2, 5), dtype=torch.int32))
+    cache.k_pages = None
+    with pytest.raises(AttributeError):
+        cache._c(pp, -1)
+    with pytest.raises(ValueError, match="k_pages"):
+        cache.k_pages = rows[0].float()
+    cache.k_pages = rows[0]
+    assert cache._c(pp, -1)._obj.k_pages == rows[0].data_ptr()
