@@ -3,9 +3,9 @@
   prompt    ems_prompt_attention: causal attention of whole prompts with grouped heads, the sequences of a batch side by
             side or packed one after the other; the log-sum-exp of its rows is what the score of a prompt starts from
   chunk     ems_paged_chunk_attention: the newest tokens of every sequence against its pages, theirs among them
-  store8    ems_paged8_append, ems_paged8_read: new keys and values are rotated and go into a paged cache as 8-bit numbers
+  store8    ems_quant_append, ems_quant_read: new keys and values are rotated and go into a paged cache as 8-bit numbers
             (e4m3, a power of two for every row), and the sequences' rows are read back for the attention of a chunk
-  attend8   ems_paged8_attention: one new token per sequence against its 8-bit pages
+  attend8   ems_quant_attention: one new token per sequence against its 8-bit pages
 
 With `own` false `run` computes each in elementary torch operations, in 32 bits (rotation angles in 64), rounded once.
 `exact` does it in 64 bits, one sequence at a time.
@@ -327,8 +327,8 @@ def _prepare_paged(c, s, u, gen):
             s["cache"] = B.PagedCache(p, s["k_pages"], s["v_pages"], s["table"], positions=s["pos_pages"])
             ws = B.ems_paged_chunk_workspace_bytes(p, c["new"])
         else:
-            s["cache"] = B.Paged8Cache(p, s["k_pages"], s["v_pages"], s["k_scale"], s["v_scale"], s["table"], positions=s["pos_pages"])
-            ws = B.ems_paged8_workspace_bytes(p)
+            s["cache"] = B.QuantCache(p, s["k_pages"], s["v_pages"], s["k_scale"], s["v_scale"], s["table"], positions=s["pos_pages"])
+            ws = B.ems_quant_workspace_bytes(p)
         s["ws"] = torch.empty(max(ws, 256), dtype=torch.uint8, device="cuda")
 
 
@@ -351,12 +351,12 @@ def _run_own(c, s):
         return B.ems_paged_chunk_attention(s["p"], s["cache"], s["lens"], s["q"], new_len=s["new_len"], want_lse=c["lse"],
                                            ws=s["ws"], out=(s["out"], s["lse"]))
     if c["kind"] == "store8":
-        q_out = B.ems_paged8_append(s["p"], s["cache"], s["start"], s["k"], s["v"], new_len=s["new_len"],
+        q_out = B.ems_quant_append(s["p"], s["cache"], s["start"], s["k"], s["v"], new_len=s["new_len"],
                                     inv_freq=s["inv_freq"], interleaved=c["interleaved"], q=s["q"], q_out=s["q_out"],
                                     len_out=s["len_out"])
-        k, v = B.ems_paged8_read(s["p"], s["cache"], s["len_out"], out=(s["k_out"], s["v_out"]))
+        k, v = B.ems_quant_read(s["p"], s["cache"], s["len_out"], out=(s["k_out"], s["v_out"]))
         return k, v, q_out, s["len_out"]
-    return B.ems_paged8_attention(s["p"], s["cache"], s["lens"], s["q"], want_lse=c["lse"], ws=s["ws"],
+    return B.ems_quant_attention(s["p"], s["cache"], s["lens"], s["q"], want_lse=c["lse"], ws=s["ws"],
                                   out=(s["out"], s["lse"]))
 
 
