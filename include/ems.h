@@ -10,7 +10,10 @@
  *
  * and, for the generation that follows, ems_expand (run-time keys/values of the compact
  * cache) and ems_decode_init -> ems_decode_attention, ems_decode_step per generated token;
- * or, over a paged cache, ems_paged_append, ems_paged_attention per generated token.
+ * or, over a paged cache, ems_paged_append, ems_paged_attention per generated token
+ * (ems_paged_chunk_attention for several at once), or the ems_quant calls over one in 8 bits.
+ * ems_prompt_attention is the attention of the prompt itself, whose log-sum-exp
+ * ems_global_local_score_from_lse takes.
  *
  * Conventions shared by every entry point
  *   - Every tensor pointer is a DEVICE pointer, contiguous and row-major (where no strides
@@ -479,6 +482,116 @@ int ems_paged_workspace_bytes(const ems_paged_params* p, size_t* attention_ws);
 int ems_paged_attention(const ems_paged_params* p, const ems_paged_cache* cache, const int32_t* lens,
                         const void* q, const ems_strides* q_strides, void* out, float* lse_opt,
                         void* ws, size_t ws_bytes, void* hip_stream);
+
+/*
+ * Attention of several new tokens per sequence over its pages: a chunk of a prompt, drafted tokens to be checked.
+ * Their own keys and values have been appended before (ems_paged_append).  Token i of the n_b new ones of
+ * sequence b is row lens[b] - n_b + i of the sequence; it sees the live rows up to its own, and none after it:
+ *     out = sum_t p_t v_t / sum_t p_t        lse = ln sum_t p_t        p_t = exp(scale q.k_t), t <= lens[b] - n_b + i
+ * A token-head that sees no live row gives zeros and -inf.  What masked rows, rows behind the length and rows that a
+ * token does not see hold does not matter to it; infinities and NaN as in ems_paged_attention.
+ *   n_new          tokens per sequence in q, >= 1 (B * n_new * Hq < 2^31)
+ *   lens           in : device [B] i32 rows of every sequence, its new tokens' among them (ems_paged_append's len_out)
+ *   new_len_opt    in : device [B] i32 how many of the n_new tokens there are, or NULL = all.  What q holds behind
+ *                       them is not read; what out and lse hold there is left as it is.
+ *   q, out         device [B, Hq, n_new, D] with any strides; out: every row in a place of its own, apart from the
+ *                  inputs
+ *   lse_opt        out: device [B, Hq, n_new] f32, or NULL
+ *   ws             device scratch of at least ems_paged_chunk_workspace_bytes (of the same n_new)
+ * 16-bit products take the weights p_t rounded to bf16, relative to the largest so far (the sum in the denominator
+ * is of the weights themselves).  The result depends on nothing but the arguments.
+ */
+int ems_paged_chunk_workspace_bytes(const ems_paged_params* p, int32_t n_new, size_t* chunk_ws);
+int ems_paged_chunk_attention(const ems_paged_params* p, const ems_paged_cache* cache, int32_t n_new,
+                              const int32_t* lens, const int32_t* new_len_opt,
+                              const void* q, const ems_strides* q_strides,
+                              void* out, const ems_strides* out_strides, float* lse_opt,
+                              void* ws, size_t ws_bytes, void* hip_stream);
+
+/*
+ * Attention of whole prompts: causal, with grouped heads, sequences of one length side by side or of different
+ * lengths one after the other.  Of a sequence with n queries and m rows of keys and values, query i sees rows
+ * t <= i + m - n (so with n = m the usual causal mask, with n < m the queries are the last tokens of m):
+ *     out = sum_t p_t v_t / sum_t p_t        lse = ln sum_t p_t        p_t = exp(scale q.k_t)
+ * A query that sees no row gives zeros and -inf; what rows hold that a query does not see does not matter to it.
+ * lse is what ems_global_local_score_from_lse takes.  Weights in 16-bit products as in ems_paged_chunk_attention.
+ *   q, out         device [B, Hq, q_rows, D] with any strides, or with q_start [Hq, q_rows, D] (the batch stride is
+ *                  not used); out: every row in a place of its own, apart from the inputs
+ *   k, v           in : device [B, Hkv, k_rows, D], or with q_start [Hkv, k_rows, D], any strides
+ *   q_start_opt    in : device [B + 1] i32: sequence b's queries are rows q_start[b] .. q_start[b + 1] - 1 of q, or
+ *                       NULL: all q_rows of batch entry b.  Rows before the first and behind the last one are
+ *                       neither read nor written.
+ *   k_start_opt    in : device [B + 1] i32, the same for k and v; NULL iff q_start is
+ *   lse_opt        out: device [B, Hq, q_rows] f32, with q_start [Hq, q_rows], or NULL
+ *   ws             device scratch of at least ems_prompt_workspace_bytes
+ * Starts are device data and cannot be checked on the host: they are clamped to [0, rows], an end to its start.
+ */
+typedef struct {
+    int32_t batch;         /* B >= 1 sequences */
+    int32_t q_heads;       /* Hq >= 1 */
+    int32_t kv_heads;      /* Hkv >= 1, divides Hq */
+    int32_t head_dim;      /* D in {64, 128} */
+    int32_t q_rows;        /* queries of every sequence, or of all of them together, >= 1 (B * Hq * q_rows < 2^31; */
+                           /*   together: (B + q_rows) * Hq < 2^31) */
+    int32_t k_rows;        /* rows of keys and values, the same way, 0 .. 2^30 (0: k and v may be NULL) */
+    float   softmax_scale; /* <= 0 means 1/sqrt(D) */
+    int32_t dtype;         /* ems_dtype of q, k, v and out */
+} ems_prompt_params;
+
+int ems_prompt_workspace_bytes(const ems_prompt_params* p, size_t* prompt_ws);
+int ems_prompt_attention(const ems_prompt_params* p,
+                         const void* q, const ems_strides* q_strides,
+                         const void* k, const ems_strides* k_strides,
+                         const void* v, const ems_strides* v_strides,
+                         const int32_t* q_start_opt, const int32_t* k_start_opt,
+                         void* out, const ems_strides* out_strides, float* lse_opt,
+                         void* ws, size_t ws_bytes, void* hip_stream);
+
+/*
+ * A paged cache in 8 bits: half the bytes of a bf16 one, for generations that memory bounds.  A row x of keys or
+ * values is held as e4m3 numbers (OCP FP8: 1, 4 and 3 bits, largest 448, one NaN and no infinity) and one power of
+ * two 2^s, s the smallest (not below -126) with max |x_e| <= 448 2^s over its finite elements:
+ *     code_e = x_e 2^-s to the nearest e4m3 (ties to even; NaN where x_e is not finite)      value = code_e 2^s
+ *   k_pages, v_pages [num_pages, Hkv, page_size, D] e4m3, 16-byte aligned
+ *   k_scale, v_scale [num_pages, Hkv, page_size] u8: s + 127, 1 .. 254
+ *   positions, page_table  as in ems_paged_cache
+ * ems_paged_params describes it; its dtype is that of keys, values, queries and outputs, EMS_BF16.
+ */
+typedef struct {
+    void* k_pages;
+    void* v_pages;
+    uint8_t* k_scale;
+    uint8_t* v_scale;
+    int32_t* positions;          /* or NULL */
+    const int32_t* page_table;
+} ems_quant_cache;
+
+/* ems_paged_append to such a cache: keys are rotated in 32 bits and rounded once, to their codes. */
+int ems_quant_append(const ems_paged_params* p, const ems_quant_cache* cache, int32_t n_new,
+                      const int32_t* start, const int32_t* new_len_opt,
+                      const void* k, const ems_strides* k_strides,
+                      const void* v, const ems_strides* v_strides,
+                      const int32_t* positions_opt, const ems_strides* positions_strides,
+                      const float* inv_freq_opt, int32_t rot_dim, int32_t interleaved,
+                      const void* q_opt, const ems_strides* q_strides,
+                      void* q_out, const ems_strides* q_out_strides,
+                      int32_t* len_out_opt, void* hip_stream);
+
+/*
+ * The values that the cache stands for, of the first min(lens[b], n_rows) rows of every sequence, to k_out and v_out
+ * [B, Hkv, n_rows, D] `dtype` with any strides (every row in a place of its own, apart from the cache).  A bf16 holds
+ * them exactly (from 2^-126 up).  Rows whose page is outside the pool give zeros, masked rows what they hold; output
+ * rows behind the length are left as they are.  n_rows >= 1, B * Hkv * n_rows < 2^31.
+ */
+int ems_quant_read(const ems_paged_params* p, const ems_quant_cache* cache, int32_t n_rows, const int32_t* lens,
+                    void* k_out, const ems_strides* k_out_strides,
+                    void* v_out, const ems_strides* v_out_strides, void* hip_stream);
+
+/* ems_paged_attention over such a cache: the same of the values that it stands for. */
+int ems_quant_workspace_bytes(const ems_paged_params* p, size_t* attention_ws);
+int ems_quant_attention(const ems_paged_params* p, const ems_quant_cache* cache, const int32_t* lens,
+                         const void* q, const ems_strides* q_strides, void* out, float* lse_opt,
+                         void* ws, size_t ws_bytes, void* hip_stream);
 
 #ifdef __cplusplus
 }

@@ -34,7 +34,10 @@ EXPORTS = ("ems_version", "ems_strerror", "ems_partition_sizes", "ems_workspace_
            "ems_decode_workspace_bytes", "ems_decode_init", "ems_decode_step",
            "ems_sparsity_rate", "ems_redundancy_rate",
            "ems_decode_attention_workspace_bytes", "ems_decode_attention",
-           "ems_paged_workspace_bytes", "ems_paged_append", "ems_paged_attention")
+           "ems_paged_workspace_bytes", "ems_paged_append", "ems_paged_attention",
+           "ems_paged_chunk_workspace_bytes", "ems_paged_chunk_attention",
+           "ems_prompt_workspace_bytes", "ems_prompt_attention",
+           "ems_quant_append", "ems_quant_read", "ems_quant_workspace_bytes", "ems_quant_attention")
 
 
 class ems_params(C.Structure):
@@ -59,6 +62,15 @@ class ems_paged_params(C.Structure):
 
 class ems_paged_cache(C.Structure):
     _fields_ = [(name, C.c_void_p) for name in ("k_pages", "v_pages", "positions", "page_table")]
+
+
+class ems_quant_cache(C.Structure):
+    _fields_ = [(name, C.c_void_p) for name in ("k_pages", "v_pages", "k_scale", "v_scale", "positions", "page_table")]
+
+
+class ems_prompt_params(C.Structure):
+    _fields_ = [(name, C.c_int32) for name in ("batch", "q_heads", "kv_heads", "head_dim", "q_rows", "k_rows")] + [
+        ("softmax_scale", C.c_float), ("dtype", C.c_int32)]
 
 
 class ems_strides(C.Structure):
@@ -122,6 +134,28 @@ class PagedParams:
         return self._c
 
 
+@dataclass(frozen=True)
+class PromptParams:
+    """q_rows, k_rows: of every sequence, or of all of them together where they are packed."""
+    batch: int
+    q_heads: int
+    kv_heads: int
+    head_dim: int
+    q_rows: int
+    k_rows: int
+    softmax_scale: float = 0.0
+    dtype: int = EMS_BF16
+
+    def __post_init__(self):                       # made once, as those of PagedParams
+        put = lambda name, x: object.__setattr__(self, name, x)  # noqa: E731
+        put("_c", ems_prompt_params(self.batch, self.q_heads, self.kv_heads, self.head_dim, self.q_rows, self.k_rows,
+                                    self.softmax_scale, self.dtype))
+        put("torch_dtype", torch.float32 if self.dtype == EMS_F32 else torch.bfloat16)
+
+    def c(self) -> ems_prompt_params:
+        return self._c
+
+
 _lib = None
 
 
@@ -160,6 +194,16 @@ def lib():
                                         C.c_void_p, ST, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, ST, C.c_void_p, ST,
                                         C.c_void_p, C.c_void_p])
         l.ems_paged_attention.argtypes = [PP, PC, C.c_void_p, C.c_void_p, ST] + [C.c_void_p] * 3 + [C.c_size_t, C.c_void_p]
+        PP8, PR = C.POINTER(ems_quant_cache), C.POINTER(ems_prompt_params)
+        l.ems_paged_chunk_workspace_bytes.argtypes = [PP, C.c_int32, C.POINTER(C.c_size_t)]
+        l.ems_paged_chunk_attention.argtypes = ([PP, PC, C.c_int32] + [C.c_void_p] * 3 + [ST, C.c_void_p, ST] + [C.c_void_p] * 2 +
+                                                [C.c_size_t, C.c_void_p])
+        l.ems_prompt_workspace_bytes.argtypes = [PR, C.POINTER(C.c_size_t)]
+        l.ems_prompt_attention.argtypes = [PR] + [C.c_void_p, ST] * 3 + [C.c_void_p] * 3 + [ST] + [C.c_void_p] * 2 + [C.c_size_t, C.c_void_p]
+        l.ems_quant_append.argtypes = [PP, PP8] + l.ems_paged_append.argtypes[2:]
+        l.ems_quant_read.argtypes = [PP, PP8, C.c_int32, C.c_void_p, C.c_void_p, ST, C.c_void_p, ST, C.c_void_p]
+        l.ems_quant_workspace_bytes.argtypes = [PP, C.POINTER(C.c_size_t)]
+        l.ems_quant_attention.argtypes = [PP, PP8] + l.ems_paged_attention.argtypes[2:]
         for name in EXPORTS[2:]:
             getattr(l, name).restype = C.c_int
         _lib = l
@@ -653,11 +697,12 @@ class PagedCache:
     """Device tensors of a paged cache (see ems_paged_cache in include/ems.h): k_pages, v_pages
     [num_pages, Hkv, page_size, D], page_table [B, max_pages] int32, and with `positions` [num_pages, Hkv, page_size]
     int32 the position of every row, negative = masked."""
+    _dtypes = dict(k_pages=None, v_pages=None, page_table=torch.int32, positions=torch.int32)      # None: that of the parameters
 
     def __init__(self, p: PagedParams, k_pages, v_pages, page_table, positions=None):
-        dev = _current_device()
-        _check_dense(k_pages, dev, p.torch_dtype, p._pages, "k_pages")
-        _check_dense(v_pages, dev, p.torch_dtype, p._pages, "v_pages")
+        dev, dt = _current_device(), self._dtypes["k_pages"] or p.torch_dtype
+        _check_dense(k_pages, dev, dt, p._pages, "k_pages")
+        _check_dense(v_pages, dev, dt, p._pages, "v_pages")
         _check_dense(page_table, dev, torch.int32, p._table, "page_table")
         if positions is not None:
             _check_dense(positions, dev, torch.int32, p._positions, "positions")
@@ -666,9 +711,8 @@ class PagedCache:
 
     def __setattr__(self, name, t):
         # a tensor in another's place (a longer table, a larger pool) is checked here, its shape by the next call
-        if t is not None and name in self.__dict__ and name in ("k_pages", "v_pages", "page_table", "positions"):
-            dtype = self.dtype if name in ("k_pages", "v_pages") else torch.int32
-            _check_dense(t, self.device_index, dtype, t.shape, name)
+        if t is not None and name in self.__dict__ and name in self._dtypes:
+            _check_dense(t, self.device_index, self._dtypes[name] or self.dtype, t.shape, name)
         self.__dict__[name] = t
 
     def _c(self, p: PagedParams, dev):
@@ -680,6 +724,41 @@ class PagedCache:
         if self.device_index != dev:
             raise ValueError("the cache must be on the current device")
         return C.byref(ems_paged_cache(k.data_ptr(), self.v_pages.data_ptr(), _ptr(pos), self.page_table.data_ptr()))
+
+
+class QuantCache(PagedCache):
+    """Device tensors of a paged cache in 8 bits (see ems_quant_cache in include/ems.h): k_pages, v_pages
+    [num_pages, Hkv, page_size, D] float8_e4m3fn, k_scale, v_scale [num_pages, Hkv, page_size] uint8 (s + 127 of a row's
+    2^s), page_table and positions as in a PagedCache."""
+    _dtypes = dict(PagedCache._dtypes, k_pages=torch.float8_e4m3fn, v_pages=torch.float8_e4m3fn, k_scale=torch.uint8,
+                   v_scale=torch.uint8)
+
+    def __init__(self, p: PagedParams, k_pages, v_pages, k_scale, v_scale, page_table, positions=None):
+        dev = _current_device()
+        for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
+            _check_dense(t, dev, torch.uint8, p._positions, name)
+        self.k_scale, self.v_scale = k_scale, v_scale
+        super().__init__(p, k_pages, v_pages, page_table, positions)
+
+    def _c(self, p: PagedParams, dev):
+        k, pos = self.k_pages, self.positions
+        if (k.shape != p._pages or self.v_pages.shape != p._pages or self.page_table.shape != p._table or
+                self.k_scale.shape != p._positions or self.v_scale.shape != p._positions or
+                (pos is not None and pos.shape != p._positions)):
+            raise ValueError(f"a cache of {tuple(k.shape)} rows with a table of {tuple(self.page_table.shape)} does not fit {p}")
+        if self.device_index != dev:
+            raise ValueError("the cache must be on the current device")
+        return C.byref(ems_quant_cache(k.data_ptr(), self.v_pages.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr(),
+                                        _ptr(pos), self.page_table.data_ptr()))
+
+
+def alloc_quant_cache(p: PagedParams, page_table, positions: bool = False) -> QuantCache:
+    """alloc_paged_cache in 8 bits: every row stands for zeros."""
+    dev = page_table.device
+    pages = lambda: torch.zeros(p._pages, dtype=torch.uint8, device=dev).view(torch.float8_e4m3fn)  # noqa: E731
+    scale = lambda: torch.ones(p._positions, dtype=torch.uint8, device=dev)  # noqa: E731
+    return QuantCache(p, pages(), pages(), scale(), scale(), page_table,
+                       torch.full(p._positions, -1, dtype=torch.int32, device=dev) if positions else None)
 
 
 def alloc_paged_cache(p: PagedParams, page_table, positions: bool = False) -> PagedCache:
@@ -706,6 +785,30 @@ def ems_paged_append(p: PagedParams, cache: PagedCache, start, k, v, positions=N
     queries q [B,Hq,N,D] are rotated by inv_freq [rot/2] f32 at their positions ([B,N] or [B,Hkv,N] int32, default
     the row).  new_len [B] int32: tokens there are of the N.  -> q_out (q's shape; pass q to rotate in place), None
     without q.  len_out [B] int32 is written start + new tokens."""
+    return _append(lib().ems_paged_append, "ems_paged_append", p, _in_full(cache), start, k, v, positions, new_len, inv_freq, interleaved, q,
+                   q_out, len_out)
+
+
+def ems_quant_append(p: PagedParams, cache: QuantCache, start, k, v, positions=None, new_len=None, inv_freq=None,
+                      interleaved=False, q=None, q_out=None, len_out=None):
+    """ems_paged_append to a cache in 8 bits."""
+    return _append(lib().ems_quant_append, "ems_quant_append", p, _in_8_bits(cache), start, k, v, positions, new_len, inv_freq,
+                   interleaved, q, q_out, len_out)
+
+
+def _in_8_bits(cache):
+    if not isinstance(cache, QuantCache):
+        raise ValueError("cache: a QuantCache")
+    return cache
+
+
+def _in_full(cache):
+    if isinstance(cache, QuantCache):
+        raise ValueError("cache: a PagedCache (the ems_quant calls take one in 8 bits)")
+    return cache
+
+
+def _append(call, name, p, cache, start, k, v, positions, new_len, inv_freq, interleaved, q, q_out, len_out):
     dev, dt, b = _current_device(), p.torch_dtype, p.batch
     cc = cache._c(p, dev)
     single = k.dim() == 3
@@ -741,11 +844,11 @@ def ems_paged_append(p: PagedParams, cache: PagedCache, start, k, v, positions=N
             raise ValueError("q_out: every row in a place of its own")
     elif q_out is not None:
         raise ValueError("q_out without q")
-    rc = lib().ems_paged_append(C.byref(p._c), cc, n, start.data_ptr(), _ptr(new_len), k.data_ptr(), ks, v.data_ptr(), vs,
-                                _ptr(positions), ps, _ptr(inv_freq), rot, 1 if interleaved else 0, _ptr(q), qs,
-                                _ptr(q_out), qos, _ptr(len_out), _stream_of(dev))
+    rc = call(C.byref(p._c), cc, n, start.data_ptr(), _ptr(new_len), k.data_ptr(), ks, v.data_ptr(), vs,
+              _ptr(positions), ps, _ptr(inv_freq), rot, 1 if interleaved else 0, _ptr(q), qs,
+              _ptr(q_out), qos, _ptr(len_out), _stream_of(dev))
     if rc != EMS_OK:
-        raise EmsError(rc, "ems_paged_append")
+        raise EmsError(rc, name)
     return q_out
 
 
@@ -760,14 +863,176 @@ def ems_paged_workspace_bytes(p: PagedParams) -> int:
 def ems_paged_attention(p: PagedParams, cache: PagedCache, lens, q, want_lse=False, ws=None, out=None):
     """Attention of one new token per sequence, q [B,Hq,D], over the first lens [B] int32 rows of its pages
     -> out [B,Hq,D] (or (out, lse [B,Hq] f32) with want_lse).  `out`: (out, lse or None) to write to."""
+    return _attend(lib().ems_paged_attention, "ems_paged_attention", ems_paged_workspace_bytes, p, _in_full(cache), lens, q, want_lse, ws, out)
+
+
+def ems_quant_workspace_bytes(p: PagedParams) -> int:
+    n = C.c_size_t(0)
+    rc = lib().ems_quant_workspace_bytes(C.byref(p._c), C.byref(n))
+    if rc != EMS_OK:
+        raise EmsError(rc, "ems_quant_workspace_bytes")
+    return int(n.value)
+
+
+def ems_quant_attention(p: PagedParams, cache: QuantCache, lens, q, want_lse=False, ws=None, out=None):
+    """ems_paged_attention over a cache in 8 bits."""
+    return _attend(lib().ems_quant_attention, "ems_quant_attention", ems_quant_workspace_bytes, p, _in_8_bits(cache), lens, q, want_lse, ws, out)
+
+
+def _attend(call, name, need, p, cache, lens, q, want_lse, ws, out):
     dev = _current_device()
     cc = cache._c(p, dev)
     qs = _rows(q, dev, p.torch_dtype, p._q_row, "q")
     _check_dense(lens, dev, torch.int32, (p.batch,), "lens")
-    ws = _check_ws(ws, dev, ems_paged_workspace_bytes, p)
+    ws = _check_ws(ws, dev, need, p)
     o, lse = _attention_out(out, dev, want_lse, p._q_row, p.torch_dtype)
-    rc = lib().ems_paged_attention(C.byref(p._c), cc, lens.data_ptr(), q.data_ptr(), qs, o.data_ptr(), _ptr(lse),
-                                   ws.data_ptr(), ws.numel(), _stream_of(dev))
+    rc = call(C.byref(p._c), cc, lens.data_ptr(), q.data_ptr(), qs, o.data_ptr(), _ptr(lse), ws.data_ptr(), ws.numel(), _stream_of(dev))
     if rc != EMS_OK:
-        raise EmsError(rc, "ems_paged_attention")
+        raise EmsError(rc, name)
     return (o, lse) if want_lse else o
+
+
+def ems_quant_read(p: PagedParams, cache: QuantCache, lens, rows=None, out=None):
+    """The values that the first lens [B] int32 rows of every sequence stand for -> k, v [B,Hkv,rows,D], rows: all that the
+    table has, or fewer; what is behind a length is left as it is (zeros in new tensors).  `out`: (k, v) to write to, of
+    any strides."""
+    dev = _current_device()
+    cc = _in_8_bits(cache)._c(p, dev)
+    _check_dense(lens, dev, torch.int32, (p.batch,), "lens")
+    if out is None:
+        n = p.max_pages * p.page_size if rows is None else rows
+        shape = (p.batch, p.kv_heads, n, p.head_dim)
+        out = tuple(torch.zeros(shape, dtype=p.torch_dtype, device="cuda") for _ in range(2))
+    k, v = out
+    if k.dim() != 4 or (rows is not None and k.shape[2] != rows):
+        raise ValueError("out: k and v [B, Hkv, rows, D]")
+    shape = (p.batch, p.kv_heads, k.shape[2], p.head_dim)
+    ks, vs = (_out_rows(t, dev, p.torch_dtype, shape, name) for t, name in ((k, "k"), (v, "v")))
+    rc = lib().ems_quant_read(C.byref(p._c), cc, k.shape[2], lens.data_ptr(), k.data_ptr(), ks, v.data_ptr(), vs, _stream_of(dev))
+    if rc != EMS_OK:
+        raise EmsError(rc, "ems_quant_read")
+    return k, v
+
+
+def _out_rows(t, dev, dtype, shape, name):
+    """Rows to write to: with strides like those of _rows, but no row in two places."""
+    s = _rows(t, dev, dtype, shape, name)
+    if not t.is_contiguous() and any(m > 1 and step == 0 for m, step in zip(t.shape, t.stride())):
+        raise ValueError(f"{name}: every row in a place of its own")
+    return s
+
+
+def _out_like(q):
+    """A new tensor of q's shape, heads and tokens in the order that q has them in."""
+    d = q.dim() - 3
+    swap = q.shape[d + 1] > 1 and q.shape[d] > 1 and q.stride(d + 1) > q.stride(d)
+    if not swap:
+        return torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    shape = list(q.shape)
+    shape[d], shape[d + 1] = shape[d + 1], shape[d]
+    return torch.empty(shape, dtype=q.dtype, device=q.device).transpose(d, d + 1)
+
+
+def ems_paged_chunk_workspace_bytes(p: PagedParams, n_new: int) -> int:
+    n = C.c_size_t(0)
+    rc = lib().ems_paged_chunk_workspace_bytes(C.byref(p._c), n_new, C.byref(n))
+    if rc != EMS_OK:
+        raise EmsError(rc, "ems_paged_chunk_workspace_bytes")
+    return int(n.value)
+
+
+def ems_paged_chunk_attention(p: PagedParams, cache: PagedCache, lens, q, new_len=None, want_lse=False, ws=None, out=None):
+    """Attention of the newest tokens of every sequence, q [B,Hq,N,D] of any strides, over the first lens [B] int32 rows of
+    its pages, theirs the last of them: each sees the rows up to its own.  new_len [B] int32: tokens there are of the N.
+    -> out [B,Hq,N,D], heads and tokens in q's order (or (out, lse [B,Hq,N] f32) with want_lse); what is behind new_len is left
+    as it is.  `out`: (out of any strides, lse or None) to write to."""
+    dev = _current_device()
+    cc = _in_full(cache)._c(p, dev)
+    if q.dim() != 4:
+        raise ValueError("q: [B, Hq, N, D]")
+    n = q.shape[2]
+    shape = (p.batch, p.q_heads, n, p.head_dim)
+    qs = _rows(q, dev, p.torch_dtype, shape, "q")
+    _check_dense(lens, dev, torch.int32, (p.batch,), "lens")
+    if new_len is not None:
+        _check_dense(new_len, dev, torch.int32, (p.batch,), "new_len")
+    if ws is None:
+        ws = torch.empty(max(ems_paged_chunk_workspace_bytes(p, n), 256), dtype=torch.uint8, device="cuda")
+    else:
+        _check_ws(ws, dev, None, p)
+    o, lse = _many_out(out, q, dev, want_lse, shape, p.torch_dtype)
+    rc = lib().ems_paged_chunk_attention(C.byref(p._c), cc, n, lens.data_ptr(), _ptr(new_len), q.data_ptr(), qs, o.data_ptr(),
+                                         _out_rows(o, dev, p.torch_dtype, shape, "out"), _ptr(lse), ws.data_ptr(), ws.numel(), _stream_of(dev))
+    if rc != EMS_OK:
+        raise EmsError(rc, "ems_paged_chunk_attention")
+    return (o, lse) if want_lse else o
+
+
+def _many_out(out, q, dev, want_lse, shape, dtype):
+    if out is None:
+        return _out_like(q), torch.empty(shape[:-1], dtype=torch.float32, device="cuda") if want_lse else None
+    o, lse = out
+    if not want_lse:
+        return o, None
+    if lse is None:
+        raise ValueError("out: a tensor for the log-sum-exp is wanted")
+    _check_dense(lse, dev, torch.float32, shape[:-1], "lse")
+    return o, lse
+
+
+def ems_prompt_workspace_bytes(p: PromptParams) -> int:
+    n = C.c_size_t(0)
+    rc = lib().ems_prompt_workspace_bytes(C.byref(p._c), C.byref(n))
+    if rc != EMS_OK:
+        raise EmsError(rc, "ems_prompt_workspace_bytes")
+    return int(n.value)
+
+
+def ems_prompt_attention(p: PromptParams, q, k, v, q_start=None, k_start=None, want_lse=False, ws=None, out=None):
+    """Causal attention of whole prompts, q [B,Hq,N,D], k, v [B,Hkv,M,D] of any strides -> out [B,Hq,N,D], heads and tokens in
+    q's order (or (out, lse [B,Hq,N] f32) with want_lse).  Packed, with q_start [B + 1] int32 (first rows of the sequences):
+    q, out [N,Hq,D], k, v [M,Hkv,D], lse [Hq,N]; k_start: theirs, None = q_start.  Queries are the last tokens of their
+    sequence's rows.  `out`: (out of any strides, lse or None) to write to."""
+    dev, dt, h, hq, d = _current_device(), p.torch_dtype, p.kv_heads, p.q_heads, p.head_dim
+    if q_start is not None:
+        if k_start is None:
+            k_start = q_start
+        _check_dense(q_start, dev, torch.int32, (p.batch + 1,), "q_start")
+        _check_dense(k_start, dev, torch.int32, (p.batch + 1,), "k_start")
+        shape, rows, lse_shape = (p.q_rows, hq, d), (p.k_rows, h, d), (hq, p.q_rows)
+        strides, checked = _token_rows, _token_out_rows
+    else:
+        if k_start is not None:
+            raise ValueError("k_start without q_start")
+        shape, rows, lse_shape = (p.batch, hq, p.q_rows, d), (p.batch, h, p.k_rows, d), (p.batch, hq, p.q_rows)
+        strides, checked = _rows, _out_rows
+    qs, ks, vs = strides(q, dev, dt, shape, "q"), strides(k, dev, dt, rows, "k"), strides(v, dev, dt, rows, "v")
+    if ws is None:
+        ws = torch.empty(max(ems_prompt_workspace_bytes(p), 256), dtype=torch.uint8, device="cuda")
+    else:
+        _check_ws(ws, dev, None, p)
+    if out is None and q_start is not None:
+        out = torch.empty(shape, dtype=dt, device="cuda"), torch.empty(lse_shape, dtype=torch.float32, device="cuda") if want_lse else None
+    o, lse = _many_out(out, q, dev, want_lse, lse_shape + (d,), dt)
+    rc = lib().ems_prompt_attention(C.byref(p._c), q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, _ptr(q_start), _ptr(k_start),
+                                    o.data_ptr(), checked(o, dev, dt, shape, "out"), _ptr(lse), ws.data_ptr(), ws.numel(), _stream_of(dev))
+    if rc != EMS_OK:
+        raise EmsError(rc, "ems_prompt_attention")
+    return (o, lse) if want_lse else o
+
+
+def _token_rows(t, dev, dtype, shape, name):
+    """Rows [tokens, heads, D] with any strides but the last -> their strides."""
+    s = t.stride()
+    if t.shape != shape or t.dtype != dtype or t.get_device() != dev:
+        _refuse(t, dev, dtype, shape, name)
+    if s[-1] != 1:
+        raise ValueError(f"{name}: the elements of a row must be adjacent")
+    return _strides(0, s[1], s[0])
+
+
+def _token_out_rows(t, dev, dtype, shape, name):
+    s = _token_rows(t, dev, dtype, shape, name)
+    if not t.is_contiguous() and any(m > 1 and step == 0 for m, step in zip(t.shape, t.stride())):
+        raise ValueError(f"{name}: every row in a place of its own")
+    return s

@@ -61,6 +61,46 @@ __device__ __forceinline__ void rotate(float& u, float& w, float c, float s)
     w = w * c + x * s;
 }
 
+// Largest modulus of the finite among x, over the kItems lanes that hold a row.
+template <int kItems, int kN>
+__device__ __forceinline__ float row_top(const float (&x)[kN], const float (&y)[kN])
+{
+    float top = 0.f;
+#pragma unroll
+    for (int e = 0; e < kN; ++e) {
+        const float a = fabsf(x[e]), b = fabsf(y[e]);
+        top = fmaxf(top, fmaxf(a < INFINITY ? a : 0.f, b < INFINITY ? b : 0.f));
+    }
+    top = fmaxf(top, dpp_f<kDppXor1>(top));
+    top = fmaxf(top, dpp_f<kDppXor2>(top));
+    if constexpr (kItems >= 8) top = fmaxf(top, dpp_f<kDppHalfMirror>(top));
+    static_assert(kItems == 4 || kItems == 8, "lanes of a row");
+    return top;
+}
+
+// s + 127 of the smallest 2^s >= 2^-126 with top <= 448 2^s = 1.75 2^(s + 8): the exponent, one more above 1.75 of its power.
+__device__ __forceinline__ int scale_byte(float top) { return max((int)((__float_as_uint(top) + 0x1fffffu) >> 23) - 8, 1); }
+
+// Eight numbers times 2^-s, to the nearest e4m3 (the conversion's own rounding; NaN and infinities become its NaN).
+typedef int i32x2_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ i32x2_t e4m3_piece(const float (&x)[8], float shrink)
+{
+    i32x2_t c;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        int w = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i] * shrink, x[4 * i + 1] * shrink, 0, false);
+        c[i] = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i + 2] * shrink, x[4 * i + 3] * shrink, w, true);
+    }
+    return c;
+}
+
+template <bool kPast, typename V>
+__device__ __forceinline__ void store_past(V* p, const V& x)
+{
+    if constexpr (kPast) __builtin_nontemporal_store(x, p);
+    else *p = x;
+}
+
 }  // namespace
 
 // A block takes some tokens and the rows (queries, keys, values) of some kv-heads.  Its angles are formed once, a value a
@@ -68,7 +108,10 @@ __device__ __forceinline__ void rotate(float& u, float& w, float c, float s)
 // (four prompts of 8192 tokens, 40 heads to rotate: 187 us, and 168 so).  Then a lane group takes a row, a lane two pieces
 // of 16 bytes that hold both halves of its pairs, kAhead rows requested together; a lane reads all of its elements before it
 // writes any, so queries may be turned in place.  Memory bounds it: those prompts, 805 MB read and written, 156 us, 5.2 TB/s.
-template <typename T, int D, bool kPast>
+//
+// k8: the cache is in 8 bits.  A row's largest modulus is found over its lanes, and its numbers go out as they are rounded, without
+// a rounding to T before.
+template <typename T, int D, bool kPast, bool k8>
 __global__ __launch_bounds__(256) void append_kernel(AppendArgs a)
 {
     constexpr int kPer = 16 / (int)sizeof(T);                  // elements of a piece: a lane takes two pieces of a row
@@ -143,10 +186,13 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a)
         for (int u = 0; u < kAhead; ++u) {
             const int r = r0 + u * step, k = r - n_q, v = k - heads;
             if (r >= rows || (r >= n_q && at < 0)) continue;
-            if (paired && v < 0) {
-                float x[kPer], y[kPer];
+            const bool coded = k8 && r >= n_q;
+            float x[kPer], y[kPer];
+            if (coded || (paired && v < 0)) {
                 Pack<T>::unpack(p0[u], x);
                 Pack<T>::unpack(p1[u], y);
+            }
+            if (paired && v < 0) {
                 if (!a.interleaved) {
 #pragma unroll
                     for (int e = 0; e < kPer; ++e) rotate(x[e], y[e], c[e], s[e]);
@@ -157,14 +203,27 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a)
                         rotate(y[2 * e], y[2 * e + 1], c[kPer / 2 + e], s[kPer / 2 + e]);
                     }
                 }
-                p0[u] = Pack<T>::pack(x);
-                p1[u] = Pack<T>::pack(y);
+                if (!coded) {
+                    p0[u] = Pack<T>::pack(x);
+                    p1[u] = Pack<T>::pack(y);
+                }
             }
             const long long row = at + (long long)(h0 + (v < 0 ? k : v)) * a.page_size;
-            T* dst = r < n_q ? q_out + r * a.qo_sh : reinterpret_cast<T*>(v < 0 ? a.k_pages : a.v_pages) + row * D;
-            const bool wide = r >= n_q || a.qo_wide;
-            store_piece<T, kPast>(dst + (v < 0 ? e0 : m0), wide, p0[u]);
-            store_piece<T, kPast>(dst + (v < 0 ? e1 : m1), wide, p1[u]);
+            if (coded) {
+                if constexpr (k8) {
+                    const int byte = scale_byte(row_top<kItems>(x, y));
+                    const float shrink = __uint_as_float((unsigned)(254 - byte) << 23);
+                    uint8_t* dst = reinterpret_cast<uint8_t*>(v < 0 ? a.k_pages : a.v_pages) + row * D;
+                    store_past<kPast>(reinterpret_cast<i32x2_t*>(dst + (v < 0 ? e0 : m0)), e4m3_piece(x, shrink));
+                    store_past<kPast>(reinterpret_cast<i32x2_t*>(dst + (v < 0 ? e1 : m1)), e4m3_piece(y, shrink));
+                    if (item == 0) (v < 0 ? a.k_scale : a.v_scale)[row] = (uint8_t)byte;
+                }
+            } else {
+                T* dst = r < n_q ? q_out + r * a.qo_sh : reinterpret_cast<T*>(v < 0 ? a.k_pages : a.v_pages) + row * D;
+                const bool wide = r >= n_q || a.qo_wide;
+                store_piece<T, kPast>(dst + (v < 0 ? e0 : m0), wide, p0[u]);
+                store_piece<T, kPast>(dst + (v < 0 ? e1 : m1), wide, p1[u]);
+            }
             if (a.pos_pages && r >= n_q && v < 0 && item == 0)
                 a.pos_pages[row] = a.positions ? a.positions[b * a.pos_sb + (h0 + k) * a.pos_sh + i * a.pos_sn] : (int)slot;
         }
@@ -182,7 +241,7 @@ int append_tokens(int rows, int row_bytes)
 }
 
 namespace {
-template <typename T, int D>
+template <typename T, int D, bool k8 = false>
 hipError_t launch(AppendArgs a, hipStream_t st)
 {
     const long long all = (long long)a.batch * a.n_new;
@@ -199,14 +258,63 @@ hipError_t launch(AppendArgs a, hipStream_t st)
     while (a.heads > 1 && blocks() < 512) a.heads = (a.heads + 1) / 2;
     while (a.tokens > 1 && blocks() < 512) a.tokens /= 2;
     const dim3 grid((unsigned)((all + a.tokens - 1) / a.tokens), (a.kv_heads + a.heads - 1) / a.heads);
-    if (past) append_kernel<T, D, true><<<grid, 256, 0, st>>>(a);
-    else append_kernel<T, D, false><<<grid, 256, 0, st>>>(a);
+    if (past) append_kernel<T, D, true, k8><<<grid, 256, 0, st>>>(a);
+    else append_kernel<T, D, false, k8><<<grid, 256, 0, st>>>(a);
     return hipGetLastError();
 }
 }  // namespace
 
+// Rows of 8-bit pages to 16 bits: a lane takes eight numbers of a row's keys and of its values, a lane group a row, kAhead rows
+// requested together.
+template <int D>
+__global__ __launch_bounds__(256) void read8_kernel(Read8Args a)
+{
+    constexpr int kItems = D / 8, kGroups = 256 / kItems, kAhead = kRead8Rows / kGroups;
+    const int per_head = (a.n_rows + kRead8Rows - 1) / kRead8Rows;
+    const int unit = blockIdx.x / per_head, b = unit / a.kv_heads, head = unit - b * a.kv_heads;
+    const int item = threadIdx.x % kItems, t0 = (blockIdx.x - unit * per_head) * kRead8Rows + threadIdx.x / kItems;
+    const long long most = (long long)a.max_pages * a.page_size;
+    const int len = (int)min((long long)min(max(a.lens[b], 0), a.n_rows), most);
+    if (t0 >= len) return;
+    typedef unsigned u32x2_t __attribute__((ext_vector_type(2)));
+    u32x2_t k[kAhead], v[kAhead];
+    int ks[kAhead], vs[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+        const int t = t0 + u * kGroups;
+        const int page = t < len ? a.page_table[(size_t)b * a.max_pages + t / a.page_size] : -1;
+        k[u] = v[u] = u32x2_t{0, 0};
+        ks[u] = vs[u] = 127;
+        if (page >= 0 && page < a.num_pages) {
+            const long long row = ((long long)page * a.kv_heads + head) * a.page_size + t % a.page_size;
+            k[u] = *reinterpret_cast<const u32x2_t*>(static_cast<const char*>(a.k_pages) + row * D + 8 * item);
+            v[u] = *reinterpret_cast<const u32x2_t*>(static_cast<const char*>(a.v_pages) + row * D + 8 * item);
+            ks[u] = a.k_scale[row];
+            vs[u] = a.v_scale[row];
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+        const int t = t0 + u * kGroups;
+        if (t >= len) break;
+        store_piece<bf16_t, false>(static_cast<bf16_t*>(a.k_out) + b * a.ko_sb + head * a.ko_sh + t * a.ko_sn + 8 * item, a.wide,
+                                   widen8(k[u][0], k[u][1], scale_of_byte(ks[u])));
+        store_piece<bf16_t, false>(static_cast<bf16_t*>(a.v_out) + b * a.vo_sb + head * a.vo_sh + t * a.vo_sn + 8 * item, a.wide,
+                                   widen8(v[u][0], v[u][1], scale_of_byte(vs[u])));
+    }
+}
+
+hipError_t launch_read8(const Read8Args& a, int head_dim, hipStream_t st)
+{
+    const unsigned blocks = (unsigned)((long long)a.batch * a.kv_heads * ((a.n_rows + kRead8Rows - 1) / kRead8Rows));
+    if (head_dim == 64) read8_kernel<64><<<blocks, 256, 0, st>>>(a);
+    else read8_kernel<128><<<blocks, 256, 0, st>>>(a);
+    return hipGetLastError();
+}
+
 hipError_t launch_append(const AppendArgs& a, int head_dim, bool f32, hipStream_t st)
 {
+    if (a.k_scale) return head_dim == 64 ? launch<bf16_t, 64, true>(a, st) : launch<bf16_t, 128, true>(a, st);
     if (f32) return head_dim == 64 ? launch<float, 64>(a, st) : launch<float, 128>(a, st);
     return head_dim == 64 ? launch<bf16_t, 64>(a, st) : launch<bf16_t, 128>(a, st);
 }

@@ -149,22 +149,27 @@ __device__ __forceinline__ float column_reduce(float v)
 
 }  // namespace
 
-template <typename T, int D, bool kTable, int kW, bool kPast, int kQt, bool kSparse>
+// T: queries and output, C: keys and values (T, or the bytes of a cache in 8 bits, whose numbers become bf16 as they go into the
+// products, the row's power of two with them).
+template <typename T, typename C, int D, bool kTable, int kW, bool kPast, int kQt, bool kSparse>
 __global__ __launch_bounds__(64 * kW, (kQt == 2 ? 2 : kW == 4 ? 3 : kW / 4)) void attend_kernel(AttendArgs a)
 {
     constexpr int kTurn = kW * kLook;                          // rows of a block's turn
-    constexpr int kTiles = kRowBytesOf<T, D> <= 256 ? 2 : 1;    // 16-row tiles of a step: their keys and values wait in registers
+    constexpr bool k8 = sizeof(C) == 1;
+    constexpr int kTiles = kRowBytesOf<C, D> <= 256 ? 2 : 1;    // 16-row tiles of a step: their keys and values wait in registers
     constexpr int kStep = 16 * kTiles, kSteps = kLook / kStep;
-    constexpr int kPieces = D * (int)sizeof(T) / 64;           // 16-byte pieces of a key row that a lane reads
+    constexpr int kPieces = D * (int)sizeof(T) / 64;           // 16-byte pieces of a query that a lane reads
+    constexpr int kKeyPieces = D * (int)sizeof(C) / 64;        // and of a key row: the same columns
     constexpr int kOut = D / 16;                               // output tiles (16 columns of V each)
     constexpr int kCols = D / 16;                              // columns of V that a lane holds of a row
-    constexpr size_t kRowBytes = kRowBytesOf<T, D>;
-    // a piece of a value row: kCols columns at kCols col (16-bit elements), or four at 4 col of every 64 (float32)
-    constexpr int kVec = sizeof(T) == 2 ? kCols / 2 : 4;       // dwords
+    constexpr size_t kRowBytes = kRowBytesOf<C, D>;
+    // a piece of a value row: kCols columns at kCols col (16-bit elements, bytes), or four at 4 col of every 64 (float32)
+    constexpr int kVec = k8 ? kCols / 4 : sizeof(T) == 2 ? kCols / 2 : 4;       // dwords
     constexpr int kParts = sizeof(T) == 2 ? 1 : D / 64;
     typedef int vec_t __attribute__((ext_vector_type(kVec)));
     constexpr int kRing = 128;
     __shared__ __align__(16) int row_of[kW][kSparse ? kRing : 2 * kLook];       // two batches, or a ring of live rows
+    __shared__ __align__(16) int scale_of[kW][!k8 ? 4 : kSparse ? kRing : 2 * kLook];       // the rows' powers of two: keys' byte, values' above
     __shared__ __align__(16) float factor_of[kW][2][kTable ? kLook : 4];
     __shared__ __align__(16) float red_o[kW][kQt * kAttendQ][D + 4];
     __shared__ float red_ml[kW][kQt * kAttendQ][2];
@@ -199,7 +204,7 @@ __global__ __launch_bounds__(64 * kW, (kQt == 2 ? 2 : kW == 4 ? 3 : kW / 4)) voi
             for (int c = 0; c < kPieces; ++c) {
                 qf[j][c] = zero_frag();
                 if (qi < n_q) {
-                    const T* at = q + (4 * c + quad) * (16 / (int)sizeof(T));
+                    const T* at = q + (k8 ? 64 * (c / 2) + 16 * quad + 8 * (c % 2) : (4 * c + quad) * (16 / (int)sizeof(T)));
                     if (a.q_wide) qf[j][c] = *reinterpret_cast<const frag_t*>(at);
                     else {
                         struct Elems { T x[16 / sizeof(T)]; } e;
@@ -224,13 +229,13 @@ __global__ __launch_bounds__(64 * kW, (kQt == 2 ? 2 : kW == 4 ? 3 : kW / 4)) voi
         // requested a step ahead, as soon as the registers that take them are free.
         const int t_first = first * kTurn + wave * kLook + lane % kLook + (kSparse ? lane / kLook * kTurn : 0);
         int t_end = 0;                                         // set below: the first trip does not wait for the lengths
-        struct Look { int row, mask; float norm; };            // mask: the position; norms of the token and of its row
+        struct Look { int row, mask; float norm; int scale; };  // mask: the position; norms of the token and of its row
         const auto table_trip = [&](int t) -> int {
             if constexpr (kTable) return t < a.n_tok ? a.tok_row[(size_t)unit * a.n_tok + t] : kNoRow;
             return t < a.max_pages * a.page_size ? a.page_table[(size_t)b * a.max_pages + page_of(a, t)] : kNoRow;
         };
         const auto row_trip = [&](int t, int entry) -> Look {
-            Look r{kNoRow, 0, 0.f};
+            Look r{kNoRow, 0, 0.f, 0};
             if constexpr (kTable) {
                 // (the index says which is the new token: a caller's element may hold any number)
                 r.row = t == a.n_tok ? kNewRow : (unsigned)entry < (unsigned)a.budget ? entry : kNoRow;
@@ -241,6 +246,7 @@ __global__ __launch_bounds__(64 * kW, (kQt == 2 ? 2 : kW == 4 ? 3 : kW / 4)) voi
             } else if (t < t_end && entry >= 0 && entry < a.num_pages) {
                 r.row = (entry * a.kv_heads + head - page_of(a, t)) * a.page_size + t;       // t % page_size rows into the page
                 if (a.pos_pages) r.mask = a.pos_pages[r.row];
+                if constexpr (k8) r.scale = a.k_scale[r.row] | a.v_scale[r.row] << 8;
             }
             return r;
         };
@@ -256,6 +262,10 @@ __global__ __launch_bounds__(64 * kW, (kQt == 2 ? 2 : kW == 4 ? 3 : kW / 4)) voi
             const unsigned live = (unsigned)__ballot(row != kNoRow);            // the upper lanes look up what others do
             const int spare = live ? __builtin_amdgcn_readlane(row, __builtin_ctz(live)) : 0;
             if (lane < kLook) row_of[wave][kLook * buf + lane] = row != kNoRow ? row : spare;
+            if constexpr (k8) {
+                const int other = live ? __builtin_amdgcn_readlane(k.scale, __builtin_ctz(live)) : 0;
+                if (lane < kLook) scale_of[wave][kLook * buf + lane] = row != kNoRow ? k.scale : other;
+            }
             wave_handover();
             return live;
         };
@@ -267,13 +277,16 @@ __global__ __launch_bounds__(64 * kW, (kQt == 2 ? 2 : kW == 4 ? 3 : kW / 4)) voi
             }
             return p + (size_t)(unsigned)r * kRowBytes;
         };
-        frag_t kf[kTiles][kPieces];
+        frag_t kf[kTiles][kKeyPieces];
+        float ks[kTiles], vs[kTiles][4];                       // the rows' powers of two (8 bits)
         const auto load_keys = [&](int buf, int at) {
 #pragma unroll
             for (int i = 0; i < kTiles; ++i) {
-                const char* p = address(a.k, a.k_new, row_of[wave][kSparse ? (buf + 16 * i + col) % kRing : kLook * buf + kStep * at + 16 * i + col]) + 16 * quad;
+                const int n = kSparse ? (buf + 16 * i + col) % kRing : kLook * buf + kStep * at + 16 * i + col;
+                const char* p = address(a.k, a.k_new, row_of[wave][n]) + 16 * quad;
+                if constexpr (k8) ks[i] = scale_of_byte(scale_of[wave][n] & 255);
 #pragma unroll
-                for (int c = 0; c < kPieces; ++c) kf[i][c] = read<kPast>(reinterpret_cast<const frag_t*>(p + 64 * c));
+                for (int c = 0; c < kKeyPieces; ++c) kf[i][c] = read<kPast>(reinterpret_cast<const frag_t*>(p + 64 * c));
             }
         };
         vec_t vf[kTiles][4][kParts];                           // rows 16 i + 4 quad + r
@@ -282,7 +295,9 @@ __global__ __launch_bounds__(64 * kW, (kQt == 2 ? 2 : kW == 4 ? 3 : kW / 4)) voi
             for (int i = 0; i < kTiles; ++i)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const char* p = address(a.v, a.v_new, row_of[wave][kSparse ? (buf + 16 * i + 4 * quad) % kRing + r : kLook * buf + kStep * at + 16 * i + 4 * quad + r]) + 4 * kVec * col;
+                    const int n = kSparse ? (buf + 16 * i + 4 * quad) % kRing + r : kLook * buf + kStep * at + 16 * i + 4 * quad + r;
+                    const char* p = address(a.v, a.v_new, row_of[wave][n]) + 4 * kVec * col;
+                    if constexpr (k8) vs[i][r] = scale_of_byte(scale_of[wave][n] >> 8);
 #pragma unroll
                     for (int h = 0; h < kParts; ++h) vf[i][r][h] = read<kPast>(reinterpret_cast<const vec_t*>(p + 256 * h));
                 }
@@ -299,7 +314,10 @@ __global__ __launch_bounds__(64 * kW, (kQt == 2 ? 2 : kW == 4 ? 3 : kW / 4)) voi
 #pragma unroll
                     for (int c = 0; c < kPieces; ++c) {
                         if constexpr (sizeof(T) == 2) {
-                            s[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kf[i][c]),
+                            frag_t x;
+                            if constexpr (k8) x = widen8(kf[i][c / 2][2 * (c % 2)], kf[i][c / 2][2 * (c % 2) + 1], ks[i]);
+                            else x = kf[i][c];
+                            s[j][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, x),
                                                                               __builtin_bit_cast(bf16x8_t, qf[j][c]), s[j][i], 0, 0, 0);
                         } else {
                             const f32x4_t x = __builtin_bit_cast(f32x4_t, kf[i][c]), y = __builtin_bit_cast(f32x4_t, qf[j][c]);
@@ -357,12 +375,18 @@ __global__ __launch_bounds__(64 * kW, (kQt == 2 ? 2 : kW == 4 ? 3 : kW / 4)) voi
                                 p -= (float)piece[j][n][r];
                             }
                         }
+                    const auto value_pair = [&](int row, int d) -> unsigned {              // columns 2 d, 2 d + 1 of one of the lane's rows
+                        const auto& x = vf[row / 4][row % 4][0];
+                        if constexpr (!k8) return x[d];
+                        return __builtin_bit_cast(unsigned, d % 2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)x[d / 2], vs[row / 4][row % 4], true)
+                                                                  : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)x[d / 2], vs[row / 4][row % 4], false));
+                    };
 #pragma unroll
                     for (int e = 0; e < kCols; ++e) {
                         frag_t x;
 #pragma unroll
                         for (int d = 0; d < 4; ++d)
-                            x[d] = __builtin_amdgcn_perm(vf[(2 * d + 1) / 4][(2 * d + 1) % 4][0][e / 2], vf[2 * d / 4][2 * d % 4][0][e / 2],
+                            x[d] = __builtin_amdgcn_perm(value_pair(2 * d + 1, e / 2), value_pair(2 * d, e / 2),
                                                          e % 2 ? 0x07060302 : 0x05040100);
 #pragma unroll
                         for (int j = 0; j < kQt; ++j)
@@ -414,8 +438,13 @@ __global__ __launch_bounds__(64 * kW, (kQt == 2 ? 2 : kW == 4 ? 3 : kW / 4)) voi
                         const int at = found + __builtin_amdgcn_mbcnt_hi((unsigned)(live >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)live, 0));
                         const int last = __builtin_amdgcn_readlane(next.row, 63 - __builtin_clzll(live));
                         if (on) row_of[wave][at % kRing] = next.row;
+                        if (k8 && on) scale_of[wave][at % kRing] = next.scale;
                         found += __builtin_popcountll(live);
                         if (lane < kStep) row_of[wave][(found + lane) % kRing] = last;
+                        if constexpr (k8) {
+                            const int scale = __builtin_amdgcn_readlane(next.scale, 63 - __builtin_clzll(live));
+                            if (lane < kStep) scale_of[wave][(found + lane) % kRing] = scale;
+                        }
                     }
                     ++batch;
                     const int t = t_first + 2 * kTurn * batch;
@@ -444,7 +473,7 @@ __global__ __launch_bounds__(64 * kW, (kQt == 2 ? 2 : kW == 4 ? 3 : kW / 4)) voi
             entry = table_trip(t_first + kTurn);
             load_keys(0, 0);
             load_values(0, 0);
-            Look next{kNoRow, 0, 0.f};
+            Look next{kNoRow, 0, 0.f, 0};
 #pragma unroll 1
             for (int i = 0, t = t_first + kTurn; i < n_steps; ++i) {           // t: the lane's row of the next batch
                 const int at = i % kSteps, buf = i / kSteps & 1;
@@ -618,7 +647,7 @@ int attend_workers(int batch, int kv_heads, int group, long long max_len, int ro
 }
 
 namespace {
-template <typename T, int D, bool kTable>
+template <typename T, typename C, int D, bool kTable>
 hipError_t launch(AttendArgs a, hipStream_t st)
 {
     a.page_shift = 0;
@@ -639,7 +668,7 @@ hipError_t launch(AttendArgs a, hipStream_t st)
     // the caches (64 q-heads 62 / 83, a compact cache of 32 x 8 heads and 2048 rows 66 / 70).  The lengths are on the device: what
     // the table admits decides, and a table wider than its sequences costs what it would not have to (32 sequences of 1024
     // rows, 8 heads, 26.3 us by a table of 1024 rows, 31.7 by one of 4096 or 16384).
-    const bool past = !kTable && tiles == 1 && blocks * max_len * 2 * kRowBytesOf<T, D> > 80 << 20;
+    const bool past = !kTable && tiles == 1 && blocks * max_len * 2 * kRowBytesOf<C, D> > 80 << 20;
     //
     // Where such a cache has positions its live rows are packed into full steps.  That costs a little where all are live and
     // saves the steps' loads of nothing where few are (us, packed / not: 128 sequences of 1500 rows, 8 heads, 1 % masked 135
@@ -650,17 +679,17 @@ hipError_t launch(AttendArgs a, hipStream_t st)
     // there is less than two blocks' work for a compute unit (us at 8 heads of 128 and 512 rows, eight waves / four:
     // 16 sequences 11.5 / 12.4, 32 15.2 / 15.8, 64 29.7 / 27.5, 128 56.6 / 50.4).
     if (a.group > kAttendQ) {
-        if (past && a.pos_pages) attend_kernel<T, D, kTable, kWaves, !kTable, 2, !kTable><<<grid, 256, 0, st>>>(a);
-        else if (past) attend_kernel<T, D, kTable, kWaves, !kTable, 2, false><<<grid, 256, 0, st>>>(a);
-        else attend_kernel<T, D, kTable, kWaves, false, 2, false><<<grid, 256, 0, st>>>(a);
+        if (past && a.pos_pages) attend_kernel<T, C, D, kTable, kWaves, !kTable, 2, !kTable><<<grid, 256, 0, st>>>(a);
+        else if (past) attend_kernel<T, C, D, kTable, kWaves, !kTable, 2, false><<<grid, 256, 0, st>>>(a);
+        else attend_kernel<T, C, D, kTable, kWaves, false, 2, false><<<grid, 256, 0, st>>>(a);
     } else if (!a.workers && max_len > kUnit && blocks < 512) {
-        attend_kernel<T, D, kTable, kWide, false, 1, false><<<grid, 64 * kWide, 0, st>>>(a);
+        attend_kernel<T, C, D, kTable, kWide, false, 1, false><<<grid, 64 * kWide, 0, st>>>(a);
     } else if (past && a.pos_pages) {
-        attend_kernel<T, D, kTable, kWaves, !kTable, 1, !kTable><<<grid, 256, 0, st>>>(a);
+        attend_kernel<T, C, D, kTable, kWaves, !kTable, 1, !kTable><<<grid, 256, 0, st>>>(a);
     } else if (past) {
-        attend_kernel<T, D, kTable, kWaves, !kTable, 1, false><<<grid, 256, 0, st>>>(a);
+        attend_kernel<T, C, D, kTable, kWaves, !kTable, 1, false><<<grid, 256, 0, st>>>(a);
     } else {
-        attend_kernel<T, D, kTable, kWaves, false, 1, false><<<grid, 256, 0, st>>>(a);
+        attend_kernel<T, C, D, kTable, kWaves, false, 1, false><<<grid, 256, 0, st>>>(a);
     }
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && a.workers) {
@@ -672,13 +701,14 @@ hipError_t launch(AttendArgs a, hipStream_t st)
 template <typename T>
 hipError_t launch_rows(const AttendArgs& a, hipStream_t st)
 {
-    if (a.page_table) return a.head_dim == 64 ? launch<T, 64, false>(a, st) : launch<T, 128, false>(a, st);
-    return a.head_dim == 64 ? launch<T, 64, true>(a, st) : launch<T, 128, true>(a, st);
+    if (a.page_table) return a.head_dim == 64 ? launch<T, T, 64, false>(a, st) : launch<T, T, 128, false>(a, st);
+    return a.head_dim == 64 ? launch<T, T, 64, true>(a, st) : launch<T, T, 128, true>(a, st);
 }
 }  // namespace
 
 hipError_t launch_attend(const AttendArgs& a, bool f32, hipStream_t st)
 {
+    if (a.k_scale) return a.head_dim == 64 ? launch<bf16_t, uint8_t, 64, false>(a, st) : launch<bf16_t, uint8_t, 128, false>(a, st);
     return f32 ? launch_rows<float>(a, st) : launch_rows<bf16_t>(a, st);
 }
 

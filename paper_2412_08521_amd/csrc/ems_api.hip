@@ -605,10 +605,10 @@ static bool wide_rows(const void* p, const ems_strides& s, bool f32)
 // Attention workspace: what the workers of a kv-head found of sequences that they share, two of them at most.
 struct AttendPlan { int workers; size_t off_ml, total; };
 
-static AttendPlan plan_attend(int batch, int kv_heads, int group, int head_dim, long long max_len, int dtype)
+static AttendPlan plan_attend(int batch, int kv_heads, int group, int head_dim, long long max_len, int row_bytes)
 {
     AttendPlan a{};
-    a.workers = ems::attend_workers(batch, kv_heads, group, max_len, head_dim * (dtype == EMS_F32 ? 4 : 2));
+    a.workers = ems::attend_workers(batch, kv_heads, group, max_len, row_bytes);
     const int tiles = (group + ems::kAttendQ - 1) / ems::kAttendQ;
     const size_t parts = (size_t)kv_heads * tiles * a.workers * 2 * ems::kAttendQ;
     a.off_ml = align_up(sizeof(float) * parts * head_dim);
@@ -642,7 +642,8 @@ static bool decode_attention_params_ok(const ems_params* p, int* why)
 
 static AttendPlan plan_decode_attention(const ems_params* p)
 {
-    return plan_attend(p->batch, p->kv_heads, p->q_heads / p->kv_heads, p->head_dim, decode_table(p) + 1ll, p->dtype);
+    return plan_attend(p->batch, p->kv_heads, p->q_heads / p->kv_heads, p->head_dim, decode_table(p) + 1ll,
+                       p->head_dim * (p->dtype == EMS_F32 ? 4 : 2));
 }
 
 int ems_decode_attention_workspace_bytes(const ems_params* p, size_t* attention_ws)
@@ -694,18 +695,17 @@ static bool paged_cache_ok(const ems_paged_cache* c)
     return c && c->k_pages && c->v_pages && c->page_table && aligned16(c->k_pages) && aligned16(c->v_pages);
 }
 
-int ems_paged_append(const ems_paged_params* p, const ems_paged_cache* cache, int32_t n_new,
-                     const int32_t* start, const int32_t* new_len_opt,
-                     const void* k, const ems_strides* k_strides,
-                     const void* v, const ems_strides* v_strides,
-                     const int32_t* positions_opt, const ems_strides* positions_strides,
-                     const float* inv_freq_opt, int32_t rot_dim, int32_t interleaved,
-                     const void* q_opt, const ems_strides* q_strides,
-                     void* q_out, const ems_strides* q_out_strides,
-                     int32_t* len_out_opt, void* hip_stream)
+// What both kinds of cache share; k_scale, v_scale: of one in 8 bits, else null.
+static int append(const ems_paged_params* p, const ems_paged_cache* cache, uint8_t* k_scale, uint8_t* v_scale, int32_t n_new,
+                  const int32_t* start, const int32_t* new_len_opt,
+                  const void* k, const ems_strides* k_strides,
+                  const void* v, const ems_strides* v_strides,
+                  const int32_t* positions_opt, const ems_strides* positions_strides,
+                  const float* inv_freq_opt, int32_t rot_dim, int32_t interleaved,
+                  const void* q_opt, const ems_strides* q_strides,
+                  void* q_out, const ems_strides* q_out_strides,
+                  int32_t* len_out_opt, void* hip_stream)
 {
-    int why;
-    if (!paged_params_ok(p, &why)) return why;
     if (!paged_cache_ok(cache) || n_new < 1 || !start || !k || !k_strides || !v || !v_strides) return EMS_ERR_INVALID_ARG;
     if (positions_opt && !positions_strides) return EMS_ERR_INVALID_ARG;
     if (rot_dim < 0 || rot_dim > p->head_dim || (rot_dim > 0) != (inv_freq_opt != nullptr)) return EMS_ERR_INVALID_ARG;
@@ -731,6 +731,7 @@ int ems_paged_append(const ems_paged_params* p, const ems_paged_cache* cache, in
     if (positions_opt) { a.pos_sb = positions_strides->batch; a.pos_sh = positions_strides->head; a.pos_sn = positions_strides->token; }
     a.start = start; a.new_len = new_len_opt; a.inv_freq = inv_freq_opt; a.len_out = len_out_opt;
     a.k_pages = cache->k_pages; a.v_pages = cache->v_pages; a.pos_pages = cache->positions; a.page_table = cache->page_table;
+    a.k_scale = k_scale; a.v_scale = v_scale;
     a.batch = p->batch; a.n_new = n_new; a.kv_heads = p->kv_heads; a.group = p->q_heads / p->kv_heads;
     a.page_size = p->page_size; a.num_pages = p->num_pages; a.max_pages = p->max_pages; a.rot = rot_dim;
     a.interleaved = interleaved != 0;
@@ -738,9 +739,26 @@ int ems_paged_append(const ems_paged_params* p, const ems_paged_cache* cache, in
     return e == hipSuccess ? EMS_OK : EMS_ERR_LAUNCH;
 }
 
+int ems_paged_append(const ems_paged_params* p, const ems_paged_cache* cache, int32_t n_new,
+                     const int32_t* start, const int32_t* new_len_opt,
+                     const void* k, const ems_strides* k_strides,
+                     const void* v, const ems_strides* v_strides,
+                     const int32_t* positions_opt, const ems_strides* positions_strides,
+                     const float* inv_freq_opt, int32_t rot_dim, int32_t interleaved,
+                     const void* q_opt, const ems_strides* q_strides,
+                     void* q_out, const ems_strides* q_out_strides,
+                     int32_t* len_out_opt, void* hip_stream)
+{
+    int why;
+    if (!paged_params_ok(p, &why)) return why;
+    return append(p, cache, nullptr, nullptr, n_new, start, new_len_opt, k, k_strides, v, v_strides, positions_opt, positions_strides,
+                  inv_freq_opt, rot_dim, interleaved, q_opt, q_strides, q_out, q_out_strides, len_out_opt, hip_stream);
+}
+
 static AttendPlan plan_paged(const ems_paged_params* p)
 {
-    return plan_attend(p->batch, p->kv_heads, p->q_heads / p->kv_heads, p->head_dim, (long long)p->max_pages * p->page_size, p->dtype);
+    return plan_attend(p->batch, p->kv_heads, p->q_heads / p->kv_heads, p->head_dim, (long long)p->max_pages * p->page_size,
+                       p->head_dim * (p->dtype == EMS_F32 ? 4 : 2));
 }
 
 int ems_paged_workspace_bytes(const ems_paged_params* p, size_t* attention_ws)
@@ -751,23 +769,249 @@ int ems_paged_workspace_bytes(const ems_paged_params* p, size_t* attention_ws)
     return EMS_OK;
 }
 
-int ems_paged_attention(const ems_paged_params* p, const ems_paged_cache* cache, const int32_t* lens,
-                        const void* q, const ems_strides* q_strides, void* out, float* lse_opt,
-                        void* ws, size_t ws_bytes, void* hip_stream)
+// What both kinds of cache share.
+static int paged_attention(const ems_paged_params* p, const ems_paged_cache* cache, const uint8_t* k_scale, const uint8_t* v_scale,
+                           const AttendPlan& plan, const int32_t* lens, const void* q, const ems_strides* q_strides, void* out,
+                           float* lse_opt, void* ws, size_t ws_bytes, void* hip_stream)
 {
-    int why;
-    if (!paged_params_ok(p, &why)) return why;
     if (!paged_cache_ok(cache) || !lens || !q || !q_strides || !out || !aligned16(out)) return EMS_ERR_INVALID_ARG;
     const bool f32 = p->dtype == EMS_F32;
     ems::AttendArgs a{};
     a.q = q; a.q_sb = q_strides->batch; a.q_sh = q_strides->head;
     a.q_wide = wide_rows(q, ems_strides{q_strides->batch, q_strides->head, 0}, f32);
     a.k = cache->k_pages; a.v = cache->v_pages; a.out = out; a.lse = lse_opt;
+    a.k_scale = k_scale; a.v_scale = v_scale;
     a.page_table = cache->page_table; a.lens = lens; a.pos_pages = cache->positions;
     a.max_pages = p->max_pages; a.page_size = p->page_size; a.num_pages = p->num_pages;
     a.batch = p->batch; a.kv_heads = p->kv_heads; a.group = p->q_heads / p->kv_heads; a.head_dim = p->head_dim;
     a.scale_log2e = scale_log2e(p->softmax_scale, p->head_dim);
-    return attend(a, plan_paged(p), f32, ws, ws_bytes, hip_stream);
+    return attend(a, plan, f32, ws, ws_bytes, hip_stream);
+}
+
+int ems_paged_attention(const ems_paged_params* p, const ems_paged_cache* cache, const int32_t* lens,
+                        const void* q, const ems_strides* q_strides, void* out, float* lse_opt,
+                        void* ws, size_t ws_bytes, void* hip_stream)
+{
+    int why;
+    if (!paged_params_ok(p, &why)) return why;
+    return paged_attention(p, cache, nullptr, nullptr, plan_paged(p), lens, q, q_strides, out, lse_opt, ws, ws_bytes, hip_stream);
+}
+
+// ---- paged cache in 8 bits
+
+static bool quant_params_ok(const ems_paged_params* p, int* why)
+{
+    if (!paged_params_ok(p, why)) return false;
+    *why = EMS_ERR_UNSUPPORTED;
+    return p->dtype == EMS_BF16;          // float32 is the mode that checks the other: 8 bits have nothing for it
+}
+
+static bool quant_cache_ok(const ems_quant_cache* c) { return c && c->k_scale && c->v_scale; }
+
+static ems_paged_cache pages_of(const ems_quant_cache* c) { return {c->k_pages, c->v_pages, c->positions, c->page_table}; }
+
+int ems_quant_append(const ems_paged_params* p, const ems_quant_cache* cache, int32_t n_new,
+                      const int32_t* start, const int32_t* new_len_opt,
+                      const void* k, const ems_strides* k_strides,
+                      const void* v, const ems_strides* v_strides,
+                      const int32_t* positions_opt, const ems_strides* positions_strides,
+                      const float* inv_freq_opt, int32_t rot_dim, int32_t interleaved,
+                      const void* q_opt, const ems_strides* q_strides,
+                      void* q_out, const ems_strides* q_out_strides,
+                      int32_t* len_out_opt, void* hip_stream)
+{
+    int why;
+    if (!quant_params_ok(p, &why)) return why;
+    if (!quant_cache_ok(cache)) return EMS_ERR_INVALID_ARG;
+    const ems_paged_cache pages = pages_of(cache);
+    return append(p, &pages, cache->k_scale, cache->v_scale, n_new, start, new_len_opt, k, k_strides, v, v_strides, positions_opt,
+                  positions_strides, inv_freq_opt, rot_dim, interleaved, q_opt, q_strides, q_out, q_out_strides, len_out_opt, hip_stream);
+}
+
+int ems_quant_read(const ems_paged_params* p, const ems_quant_cache* cache, int32_t n_rows, const int32_t* lens,
+                    void* k_out, const ems_strides* k_out_strides,
+                    void* v_out, const ems_strides* v_out_strides, void* hip_stream)
+{
+    int why;
+    if (!quant_params_ok(p, &why)) return why;
+    if (!quant_cache_ok(cache)) return EMS_ERR_INVALID_ARG;
+    const ems_paged_cache pages = pages_of(cache);
+    if (!paged_cache_ok(&pages) || n_rows < 1 || !lens || !k_out || !k_out_strides || !v_out || !v_out_strides) return EMS_ERR_INVALID_ARG;
+    if ((long long)p->batch * n_rows > 0x7fffffffll / p->kv_heads) return EMS_ERR_UNSUPPORTED;
+    if ((long long)p->batch * p->kv_heads * ((n_rows + ems::kRead8Rows - 1) / ems::kRead8Rows) >= kMostBlocks) return EMS_ERR_UNSUPPORTED;
+    ems::Read8Args a{};
+    a.k_pages = cache->k_pages; a.v_pages = cache->v_pages; a.k_scale = cache->k_scale; a.v_scale = cache->v_scale;
+    a.page_table = cache->page_table; a.lens = lens;
+    a.k_out = k_out; a.ko_sb = k_out_strides->batch; a.ko_sh = k_out_strides->head; a.ko_sn = k_out_strides->token;
+    a.v_out = v_out; a.vo_sb = v_out_strides->batch; a.vo_sh = v_out_strides->head; a.vo_sn = v_out_strides->token;
+    a.wide = wide_rows(k_out, *k_out_strides, false) && wide_rows(v_out, *v_out_strides, false);
+    a.batch = p->batch; a.kv_heads = p->kv_heads; a.n_rows = n_rows;
+    a.page_size = p->page_size; a.num_pages = p->num_pages; a.max_pages = p->max_pages;
+    const hipError_t e = ems::launch_read8(a, p->head_dim, static_cast<hipStream_t>(hip_stream));
+    return e == hipSuccess ? EMS_OK : EMS_ERR_LAUNCH;
+}
+
+static AttendPlan plan_quant(const ems_paged_params* p)
+{
+    return plan_attend(p->batch, p->kv_heads, p->q_heads / p->kv_heads, p->head_dim, (long long)p->max_pages * p->page_size, p->head_dim);
+}
+
+int ems_quant_workspace_bytes(const ems_paged_params* p, size_t* attention_ws)
+{
+    int why;
+    if (!quant_params_ok(p, &why)) return why;
+    if (attention_ws) *attention_ws = plan_quant(p).total;
+    return EMS_OK;
+}
+
+int ems_quant_attention(const ems_paged_params* p, const ems_quant_cache* cache, const int32_t* lens,
+                         const void* q, const ems_strides* q_strides, void* out, float* lse_opt,
+                         void* ws, size_t ws_bytes, void* hip_stream)
+{
+    int why;
+    if (!quant_params_ok(p, &why)) return why;
+    if (!quant_cache_ok(cache)) return EMS_ERR_INVALID_ARG;
+    const ems_paged_cache pages = pages_of(cache);
+    return paged_attention(p, &pages, cache->k_scale, cache->v_scale, plan_quant(p), lens, q, q_strides, out, lse_opt, ws, ws_bytes, hip_stream);
+}
+
+// ---- attention of many queries: prompts, and chunks over pages
+
+// Workspace: what blocks that share a tile's rows found of it.
+struct PromptSizes { ems::PromptPlan plan; size_t off_ml, total; };
+
+static PromptSizes prompt_sizes(const ems::PromptPlan& plan, long long q_tokens, int q_heads, int head_dim)
+{
+    PromptSizes s{plan, 0, 0};
+    if (plan.splits > 1) {
+        const size_t parts = (size_t)q_tokens * q_heads * plan.splits;
+        s.off_ml = align_up(sizeof(float) * parts * head_dim);
+        s.total = s.off_ml + align_up(sizeof(float) * parts * 2);
+    }
+    return s;
+}
+
+static int many_queries(ems::PromptArgs& a, const PromptSizes& s, int head_dim, bool f32, void* ws, size_t ws_bytes, void* hip_stream)
+{
+    if (s.total && !ws_ok(ws, ws_bytes, s.total)) return EMS_ERR_WORKSPACE;
+    a.part_o = static_cast<float*>(ws);
+    a.part_ml = s.total ? reinterpret_cast<float*>(static_cast<char*>(ws) + s.off_ml) : nullptr;
+    const hipError_t e = ems::launch_prompt(a, s.plan, head_dim, f32, static_cast<hipStream_t>(hip_stream));
+    return e == hipSuccess ? EMS_OK : EMS_ERR_LAUNCH;
+}
+
+// Blocks of a launch: less than 2^32 threads in x.
+static bool prompt_grid_ok(const ems::PromptPlan& plan, int kv_heads) { return plan.tiles * kv_heads * plan.waves < (1ll << 26); }
+
+static bool chunk_params_ok(const ems_paged_params* p, int32_t n_new, PromptSizes* s, int* why)
+{
+    if (!paged_params_ok(p, why)) return false;
+    *why = EMS_ERR_INVALID_ARG;
+    if (n_new < 1) return false;
+    *why = EMS_ERR_UNSUPPORTED;
+    if ((long long)p->batch * n_new > 0x7fffffffll / p->q_heads) return false;
+    const long long rows = (long long)n_new * (p->q_heads / p->kv_heads), tokens = (long long)p->batch * n_new;
+    *s = prompt_sizes(ems::plan_prompt(p->batch, rows, p->batch * rows, p->kv_heads, (long long)p->max_pages * p->page_size), tokens, p->q_heads, p->head_dim);
+    return prompt_grid_ok(s->plan, p->kv_heads);
+}
+
+int ems_paged_chunk_workspace_bytes(const ems_paged_params* p, int32_t n_new, size_t* chunk_ws)
+{
+    int why;
+    PromptSizes s;
+    if (!chunk_params_ok(p, n_new, &s, &why)) return why;
+    if (chunk_ws) *chunk_ws = s.total;
+    return EMS_OK;
+}
+
+int ems_paged_chunk_attention(const ems_paged_params* p, const ems_paged_cache* cache, int32_t n_new,
+                              const int32_t* lens, const int32_t* new_len_opt,
+                              const void* q, const ems_strides* q_strides,
+                              void* out, const ems_strides* out_strides, float* lse_opt,
+                              void* ws, size_t ws_bytes, void* hip_stream)
+{
+    int why;
+    PromptSizes s;
+    if (!chunk_params_ok(p, n_new, &s, &why)) return why;
+    if (!paged_cache_ok(cache) || !lens || !q || !q_strides || !out || !out_strides) return EMS_ERR_INVALID_ARG;
+    const bool f32 = p->dtype == EMS_F32;
+    ems::PromptArgs a{};
+    a.q = q; a.q_sb = q_strides->batch; a.q_sh = q_strides->head; a.q_sn = q_strides->token; a.q_wide = wide_rows(q, *q_strides, f32);
+    a.out = out; a.o_sb = out_strides->batch; a.o_sh = out_strides->head; a.o_sn = out_strides->token; a.o_wide = wide_rows(out, *out_strides, f32);
+    a.lse = lse_opt; a.l_sb = (long long)p->q_heads * n_new; a.l_sh = n_new;
+    a.k = cache->k_pages; a.v = cache->v_pages; a.kv_wide = true;
+    a.page_table = cache->page_table; a.lens = lens; a.new_len = new_len_opt; a.pos_pages = cache->positions;
+    a.max_pages = p->max_pages; a.page_size = p->page_size; a.num_pages = p->num_pages;
+    a.batch = p->batch; a.kv_heads = p->kv_heads; a.group = p->q_heads / p->kv_heads; a.q_rows = n_new;
+    a.q_tokens = (long long)p->batch * n_new;
+    a.scale_log2e = scale_log2e(p->softmax_scale, p->head_dim);
+    return many_queries(a, s, p->head_dim, f32, ws, ws_bytes, hip_stream);
+}
+
+static bool prompt_params_ok(const ems_prompt_params* p, int* why)
+{
+    *why = EMS_ERR_INVALID_ARG;
+    if (!p) return false;
+    if (p->batch < 1 || p->q_heads < 1 || p->kv_heads < 1 || p->head_dim < 1) return false;
+    if (p->q_heads % p->kv_heads) return false;
+    if (p->q_rows < 1 || p->k_rows < 0) return false;
+    if (p->dtype != EMS_BF16 && p->dtype != EMS_F32) return false;
+    if (std::isnan(p->softmax_scale) || std::isinf(p->softmax_scale)) return false;
+    *why = EMS_ERR_UNSUPPORTED;
+    if (p->head_dim != 64 && p->head_dim != 128) return false;
+    return p->k_rows <= (1 << 30) && ((long long)p->batch + p->q_rows) * p->q_heads <= 0x7fffffffll;
+}
+
+// (The workspace's size is asked for without the starts: it is what either form needs.)
+static PromptSizes plan_prompts(const ems_prompt_params* p, bool packed)
+{
+    const int group = p->q_heads / p->kv_heads;
+    const long long rows = (long long)p->q_rows * group, tokens = packed ? p->q_rows : (long long)p->batch * p->q_rows;
+    return prompt_sizes(ems::plan_prompt(p->batch, rows, packed ? rows : p->batch * rows, p->kv_heads, p->k_rows), tokens, p->q_heads, p->head_dim);
+}
+
+static bool dense_prompt_ok(const ems_prompt_params* p) { return (long long)p->batch * p->q_rows <= 0x7fffffffll / p->q_heads; }
+
+int ems_prompt_workspace_bytes(const ems_prompt_params* p, size_t* prompt_ws)
+{
+    int why;
+    if (!prompt_params_ok(p, &why)) return why;
+    const size_t packed = plan_prompts(p, true).total, dense = dense_prompt_ok(p) ? plan_prompts(p, false).total : 0;
+    if (prompt_ws) *prompt_ws = packed > dense ? packed : dense;
+    return EMS_OK;
+}
+
+int ems_prompt_attention(const ems_prompt_params* p,
+                         const void* q, const ems_strides* q_strides,
+                         const void* k, const ems_strides* k_strides,
+                         const void* v, const ems_strides* v_strides,
+                         const int32_t* q_start_opt, const int32_t* k_start_opt,
+                         void* out, const ems_strides* out_strides, float* lse_opt,
+                         void* ws, size_t ws_bytes, void* hip_stream)
+{
+    int why;
+    if (!prompt_params_ok(p, &why)) return why;
+    if (!q || !q_strides || !k_strides || !v_strides || !out || !out_strides) return EMS_ERR_INVALID_ARG;
+    if (p->k_rows > 0 && (!k || !v)) return EMS_ERR_INVALID_ARG;
+    const bool packed = q_start_opt != nullptr;
+    if (packed != (k_start_opt != nullptr)) return EMS_ERR_INVALID_ARG;
+    if (!packed && !dense_prompt_ok(p)) return EMS_ERR_UNSUPPORTED;
+    const PromptSizes s = plan_prompts(p, packed);
+    if (!prompt_grid_ok(s.plan, p->kv_heads)) return EMS_ERR_UNSUPPORTED;
+    const bool f32 = p->dtype == EMS_F32;
+    const auto wide = [&](const void* x, ems_strides st) { if (packed) st.batch = 0; return wide_rows(x, st, f32); };
+    ems::PromptArgs a{};
+    a.q = q; a.q_sb = q_strides->batch; a.q_sh = q_strides->head; a.q_sn = q_strides->token; a.q_wide = wide(q, *q_strides);
+    a.k = k; a.k_sb = k_strides->batch; a.k_sh = k_strides->head; a.k_sn = k_strides->token;
+    a.v = v; a.v_sb = v_strides->batch; a.v_sh = v_strides->head; a.v_sn = v_strides->token;
+    a.kv_wide = wide(k, *k_strides) && wide(v, *v_strides);
+    a.out = out; a.o_sb = out_strides->batch; a.o_sh = out_strides->head; a.o_sn = out_strides->token; a.o_wide = wide(out, *out_strides);
+    a.lse = lse_opt; a.l_sb = packed ? 0 : (long long)p->q_heads * p->q_rows; a.l_sh = p->q_rows;
+    a.q_start = q_start_opt; a.k_start = k_start_opt; a.q_rows = p->q_rows; a.k_rows = p->k_rows;
+    a.batch = p->batch; a.kv_heads = p->kv_heads; a.group = p->q_heads / p->kv_heads;
+    a.q_tokens = packed ? p->q_rows : (long long)p->batch * p->q_rows;
+    a.scale_log2e = scale_log2e(p->softmax_scale, p->head_dim);
+    return many_queries(a, s, p->head_dim, f32, ws, ws_bytes, hip_stream);
 }
 
 }  // extern "C"

@@ -176,10 +176,27 @@ struct AppendArgs {
     void* k_pages;              // [num_pages, kv_heads, page_size, D]
     void* v_pages;
     int32_t* pos_pages;         // [num_pages, kv_heads, page_size] or null
+    uint8_t* k_scale;           // the same, of pages in 8 bits, or null
+    uint8_t* v_scale;
     const int32_t* page_table;  // [batch, max_pages]
     int batch, n_new, kv_heads, group, page_size, num_pages, max_pages, rot;
     int tokens, heads;          // tokens and kv-heads of a block (set by the launcher)
     bool interleaved, k_wide, v_wide, q_wide, qo_wide;
+};
+
+// Rows of 8-bit pages back to 16 bits.
+struct Read8Args {
+    const void* k_pages;        // [num_pages, kv_heads, page_size, D]
+    const void* v_pages;
+    const uint8_t* k_scale;     // [num_pages, kv_heads, page_size]
+    const uint8_t* v_scale;
+    const int32_t* page_table;  // [batch, max_pages]
+    const int32_t* lens;        // [batch]
+    void* k_out;                // [batch, kv_heads, n_rows, D]
+    void* v_out;
+    long long ko_sb, ko_sh, ko_sn, vo_sb, vo_sh, vo_sn;
+    int batch, kv_heads, n_rows, page_size, num_pages, max_pages;
+    bool wide;
 };
 
 // Attention of one new token per sequence.  Rows are those of a paged cache (page_table), or of a compact cache whose
@@ -194,6 +211,8 @@ struct AttendArgs {
     const int32_t* page_table;  // [batch, max_pages]
     const int32_t* lens;        // [batch]
     const int32_t* pos_pages;   // [num_pages, kv_heads, page_size] or null; < 0: masked
+    const uint8_t* k_scale;     // the same, of pages in 8 bits, or null
+    const uint8_t* v_scale;
     int max_pages, page_size, num_pages;
     const int32_t* tok_row;     // [batch * kv_heads, n_tok]
     const float* tok_norm;
@@ -211,11 +230,45 @@ struct AttendArgs {
     float* part_o;              // [kv_heads * tiles, workers, 2, 16, D] what a worker found of a sequence it shares (workspace)
     float* part_ml;             // [.., 16, 2] its maximum and sum
 };
+// Attention of many queries per sequence, each over the rows up to its own: whole prompts (rows with strides), or new tokens
+// over a paged cache (page_table).  Strides in elements.
+struct PromptArgs {
+    const void* q;              // [batch, Hq, q_rows, D], or with q_start [Hq, q_rows, D]
+    const void* k;              // the same of k_rows; the first row of a paged cache
+    const void* v;
+    void* out;
+    float* lse;                 // or null
+    long long q_sb, q_sh, q_sn, k_sb, k_sh, k_sn, v_sb, v_sh, v_sn, o_sb, o_sh, o_sn, l_sb, l_sh;
+    const int32_t* q_start;     // [batch + 1] first rows of packed sequences, or null
+    const int32_t* k_start;
+    int q_rows, k_rows;
+    const int32_t* page_table;  // [batch, max_pages]
+    const int32_t* lens;        // [batch]
+    const int32_t* new_len;     // [batch] or null: all q_rows
+    const int32_t* pos_pages;   // [num_pages, kv_heads, page_size] or null; < 0: masked
+    int max_pages, page_size, num_pages;
+    int batch, kv_heads, group;
+    long long q_tokens;         // of all sequences
+    bool q_wide;                // rows start at multiples of 16 bytes
+    bool kv_wide, o_wide;
+    float scale_log2e;
+    unsigned page_magic;        // division by page_size (set by the launcher)
+    int page_shift;
+    int splits;                 // blocks that share a tile's rows of keys and values
+    float* part_o;              // [q_tokens, Hq, splits, D] what a block found of a tile that it shares (workspace)
+    float* part_ml;             // [.., 2] its maximum and sum
+};
+struct PromptPlan { int waves, splits; long long tiles; };      // of a block; of a tile's rows; tiles of a kv-head at most
+// `sequences` of at most `rows` query rows (tokens x q-heads of a group) each and `all_rows` together, over at most `most` rows
+PromptPlan plan_prompt(long long sequences, long long rows, long long all_rows, int kv_heads, long long most);
+hipError_t launch_prompt(const PromptArgs& a, const PromptPlan& plan, int head_dim, bool f32, hipStream_t st);
 constexpr int kAttendQ = 16;    // q-heads of a group that a block takes: the columns of a matrix product
 constexpr int kAttendUnit = 128;        // rows that work is counted in
 int attend_workers(int batch, int kv_heads, int group, long long max_len, int row_bytes);      // AttendArgs::workers
 int append_tokens(int rows, int row_bytes);    // tokens of a block where there are many, `rows` (queries, keys, values) each
 hipError_t launch_append(const AppendArgs& a, int head_dim, bool f32, hipStream_t st);
+constexpr int kRead8Rows = 64;         // rows of a block
+hipError_t launch_read8(const Read8Args& a, int head_dim, hipStream_t st);
 hipError_t launch_attend(const AttendArgs& a, bool f32, hipStream_t st);
 
 int score_keys_per_block(int dtype_is_f32);

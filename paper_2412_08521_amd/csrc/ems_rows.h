@@ -95,6 +95,21 @@ template <> struct Pack<float> {
     }
 };
 
+// ---- rows in 8 bits: e4m3 numbers and a power of two a row
+
+__device__ __forceinline__ float scale_of_byte(int s) { return __uint_as_float((unsigned)s << 23); }
+
+// Eight of them, times the power of two, as bf16 (exact, but below 2^-126).
+__device__ __forceinline__ frag_t widen8(unsigned x, unsigned y, float scale)
+{
+    frag_t f;
+    f[0] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, false));
+    f[1] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, true));
+    f[2] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(y, scale, false));
+    f[3] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(y, scale, true));
+    return f;
+}
+
 // ---- DPP lane permutations (ALU latency, no LDS round trip)
 template <int kCtrl>
 __device__ __forceinline__ float dpp_f(float v)

@@ -1,0 +1,222 @@
+"""Host-side checks, without a GPU, of the attention of prompts and chunks and of the 8-bit paged cache: sizes, the refusal of what
+no kernel could run, and the plain forms that the GPU tests compare with."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paged_ref import attention
+from prompt_ref import attention_rows, causal
+from quant_ref import codes, exponent, top_of
+from paper_2412_08521_amd import binding as B
+
+INVALID, UNSUPPORTED, WORKSPACE = B.EMS_ERR_INVALID_ARG, B.EMS_ERR_UNSUPPORTED, B.EMS_ERR_WORKSPACE
+D = 1 << 12                                       # an address that no refused call touches
+BIG = 1 << 40
+
+
+def _st():
+    return B.ems_strides(1024, 128, 512)
+
+
+def _ref(x):
+    return None if x is None else C.byref(x)
+
+
+def _paged(**kw):
+    return B.PagedParams(**{**dict(batch=2, q_heads=4, kv_heads=2, head_dim=128, page_size=16, num_pages=100, max_pages=50), **kw})
+
+
+def _prompt(**kw):
+    return B.PromptParams(**{**dict(batch=2, q_heads=4, kv_heads=2, head_dim=128, q_rows=100, k_rows=100), **kw})
+
+
+def _call_prompt(p, **kw):
+    a = dict(q=D, qs=_st(), k=D, ks=_st(), v=D, vs=_st(), q_start=None, k_start=None, out=D, os=_st(), lse=None, ws=D, n=BIG)
+    a.update(kw)
+    return B.lib().ems_prompt_attention(_ref(p and p.c()), a["q"], _ref(a["qs"]), a["k"], _ref(a["ks"]), a["v"], _ref(a["vs"]), a["q_start"],
+                                        a["k_start"], a["out"], _ref(a["os"]), a["lse"], a["ws"], a["n"], None)
+
+
+def _call_chunk(p, **kw):
+    a = dict(cache=B.ems_paged_cache(D, D, None, D), n_new=4, lens=D, new_len=None, q=D, qs=_st(), out=D, os=_st(), lse=None, ws=D, n=BIG)
+    a.update(kw)
+    return B.lib().ems_paged_chunk_attention(_ref(p and p.c()), _ref(a["cache"]), a["n_new"], a["lens"], a["new_len"], a["q"], _ref(a["qs"]),
+                                             a["out"], _ref(a["os"]), a["lse"], a["ws"], a["n"], None)
+
+
+def _quant(**kw):
+    return B.ems_quant_cache(**{**dict(k_pages=D, v_pages=D, k_scale=D, v_scale=D, positions=None, page_table=D), **kw})
+
+
+def _call_append(p, **kw):
+    a = dict(cache=_quant(), n_new=1, start=D, new_len=None, k=D, ks=_st(), v=D, vs=_st(), pos=None, ps=None, freq=D, rot=128, q=D, qs=_st(),
+             q_out=D, qos=_st(), len_out=None)
+    a.update(kw)
+    return B.lib().ems_quant_append(_ref(p and p.c()), _ref(a["cache"]), a["n_new"], a["start"], a["new_len"], a["k"], _ref(a["ks"]), a["v"],
+                                    _ref(a["vs"]), a["pos"], _ref(a["ps"]), a["freq"], a["rot"], 0, a["q"], _ref(a["qs"]), a["q_out"],
+                                    _ref(a["qos"]), a["len_out"], None)
+
+
+def _call_read(p, **kw):
+    a = dict(cache=_quant(), rows=10, lens=D, k=D, ks=_st(), v=D, vs=_st())
+    a.update(kw)
+    return B.lib().ems_quant_read(_ref(p and p.c()), _ref(a["cache"]), a["rows"], a["lens"], a["k"], _ref(a["ks"]), a["v"], _ref(a["vs"]), None)
+
+
+def _call_attend(p, **kw):
+    a = dict(cache=_quant(), lens=D, q=D, qs=B.ems_strides(512, 128, 0), out=D, ws=D, n=BIG)
+    a.update(kw)
+    return B.lib().ems_quant_attention(_ref(p and p.c()), _ref(a["cache"]), a["lens"], a["q"], _ref(a["qs"]), a["out"], None, a["ws"], a["n"], None)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(batch=0), INVALID), (dict(q_heads=5), INVALID), (dict(kv_heads=0), INVALID), (dict(head_dim=0), INVALID), (dict(q_rows=0), INVALID),
+    (dict(k_rows=-1), INVALID), (dict(dtype=2), INVALID), (dict(softmax_scale=float("nan")), INVALID), (dict(softmax_scale=float("inf")), INVALID),
+    (dict(head_dim=96), UNSUPPORTED), (dict(k_rows=(1 << 30) + 1), UNSUPPORTED), (dict(q_rows=1 << 29), UNSUPPORTED),
+    (dict(q_heads=1 << 30, kv_heads=1 << 30), UNSUPPORTED)])
+def test_prompt_parameters(kw, code):
+    p = _prompt(**kw)
+    assert _call_prompt(p) == code
+    with pytest.raises(B.EmsError) as e:
+        B.ems_prompt_workspace_bytes(p)
+    assert e.value.status == code
+
+
+def test_prompt_arguments():
+    p = _prompt()
+    for kw in (dict(q=None), dict(qs=None), dict(k=None), dict(ks=None), dict(v=None), dict(vs=None), dict(out=None), dict(os=None),
+               dict(q_start=D), dict(k_start=D)):
+        assert _call_prompt(p, **kw) == INVALID, kw
+    assert _call_prompt(None) == INVALID
+    assert B.lib().ems_prompt_workspace_bytes(None, None) == INVALID
+    # packed: so many rows in all; side by side: of each of many sequences
+    assert _call_prompt(_prompt(batch=1 << 20, q_rows=1 << 10)) == UNSUPPORTED
+    few = _prompt(batch=1, q_rows=3, k_rows=100000)
+    need = B.ems_prompt_workspace_bytes(few)
+    assert need > 0 and need % 256 == 0
+    for kw in (dict(ws=None), dict(ws=D + 16), dict(n=need - 1)):
+        assert _call_prompt(few, **kw) == WORKSPACE, kw
+    assert B.ems_prompt_workspace_bytes(_prompt(batch=8, q_heads=32, kv_heads=8, q_rows=4096, k_rows=4096)) == 0
+
+
+def test_chunk_arguments():
+    p = _paged()
+    for kw in (dict(cache=None), dict(cache=B.ems_paged_cache(D, D, None, None)), dict(cache=B.ems_paged_cache(D, D + 8, None, D)), dict(n_new=0),
+               dict(n_new=-3), dict(lens=None), dict(q=None), dict(qs=None), dict(out=None), dict(os=None)):
+        assert _call_chunk(p, **kw) == INVALID, kw
+    assert _call_chunk(None) == INVALID and _call_chunk(_paged(q_heads=5)) == INVALID
+    assert _call_chunk(p, n_new=1 << 29) == UNSUPPORTED and _call_chunk(_paged(head_dim=80)) == UNSUPPORTED
+    long = _paged(max_pages=5000)
+    need = B.ems_paged_chunk_workspace_bytes(long, 4)
+    assert need > 0 and need % 256 == 0
+    for kw in (dict(ws=None), dict(ws=D + 16), dict(n=need - 1)):
+        assert _call_chunk(long, **kw) == WORKSPACE, kw
+    for n, code in ((0, INVALID), (1 << 29, UNSUPPORTED)):
+        with pytest.raises(B.EmsError) as e:
+            B.ems_paged_chunk_workspace_bytes(p, n)
+        assert e.value.status == code
+
+
+def test_quant_arguments():
+    p = _paged()
+    null = [dict(cache=None)] + [dict(cache=_quant(**{x: None})) for x in ("k_pages", "v_pages", "k_scale", "v_scale", "page_table")]
+    null += [dict(cache=_quant(k_pages=D + 8)), dict(cache=_quant(v_pages=D + 2)), dict(lens=None)]
+    for kw in null + [dict(rows=0), dict(rows=-1), dict(k=None), dict(ks=None), dict(v=None), dict(vs=None)]:
+        assert _call_read(p, **kw) == INVALID, kw
+    for kw in null + [dict(q=None), dict(qs=None), dict(out=None), dict(out=D + 8)]:
+        assert _call_attend(p, **kw) == INVALID, kw
+    for kw in null[:-1] + [dict(n_new=0), dict(start=None), dict(k=None), dict(ks=None), dict(v=None), dict(vs=None), dict(pos=D), dict(freq=None),
+                           dict(rot=0), dict(rot=144), dict(q=None), dict(q_out=None), dict(qs=None), dict(qos=None), dict(len_out=D)]:
+        assert _call_append(p, **kw) == INVALID, kw
+    for call in (_call_append, _call_read, _call_attend):
+        assert call(None) == INVALID and call(_paged(batch=0)) == INVALID
+        assert call(_paged(dtype=B.EMS_F32)) == UNSUPPORTED and call(_paged(head_dim=96)) == UNSUPPORTED
+    assert _call_append(p, rot=24) == UNSUPPORTED and _call_append(p, n_new=1 << 30) == UNSUPPORTED
+    assert _call_read(p, rows=1 << 29) == UNSUPPORTED
+    need = B.ems_quant_workspace_bytes(_paged(max_pages=500))
+    assert need > 0 and need % 256 == 0
+    for kw in (dict(ws=None), dict(ws=D + 16), dict(n=need - 1)):
+        assert _call_attend(_paged(max_pages=500), **kw) == WORKSPACE, kw
+    with pytest.raises(B.EmsError) as e:
+        B.ems_quant_workspace_bytes(_paged(dtype=B.EMS_F32))
+    assert e.value.status == UNSUPPORTED
+
+
+def test_binding_refuses_host_tensors_and_the_other_kind_of_cache():
+    p = _paged()
+    rows = (100, 2, 16, 128)
+    table, lens = torch.zeros((2, 50), dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    k8, s8 = torch.zeros(rows, dtype=torch.uint8).view(torch.float8_e4m3fn), torch.zeros(rows[:3], dtype=torch.uint8)
+    with pytest.raises(ValueError, match="k_scale must be a tensor of the current device"):
+        B.QuantCache(p, k8, k8, s8, s8, table)
+    with pytest.raises(ValueError, match="current device"):
+        B.alloc_quant_cache(p, table)
+    full, small = object.__new__(B.PagedCache), object.__new__(B.QuantCache)          # caches, had their tensors been a device's
+    k = torch.zeros(rows, dtype=torch.bfloat16)
+    full.k_pages, full.v_pages, full.page_table, full.positions = k, k, table, None
+    small.k_pages, small.v_pages, small.k_scale, small.v_scale, small.page_table, small.positions = k8, k8, s8, s8, table, None
+    full.device_index = small.device_index = B._current_device()
+    q, kn = torch.zeros((2, 4, 128), dtype=torch.bfloat16), torch.zeros((2, 2, 128), dtype=torch.bfloat16)
+    for call in (lambda: B.ems_quant_attention(p, full, lens, q), lambda: B.ems_quant_append(p, full, lens, kn, kn), lambda: B.ems_quant_read(p, full, lens)):
+        with pytest.raises(ValueError, match="a QuantCache"):
+            call()
+    for call in (lambda: B.ems_paged_attention(p, small, lens, q), lambda: B.ems_paged_append(p, small, lens, kn, kn),
+                 lambda: B.ems_paged_chunk_attention(p, small, lens, q[:, :, None])):
+        with pytest.raises(ValueError, match="a PagedCache"):
+            call()
+    for kw in (dict(num_pages=101), dict(page_size=32), dict(max_pages=51), dict(batch=1), dict(kv_heads=4), dict(head_dim=64)):
+        with pytest.raises(ValueError, match="does not fit"):
+            small._c(_paged(**kw), small.device_index)
+    with pytest.raises(ValueError, match="q must be a tensor of the current device"):
+        B.ems_quant_attention(p, small, lens, q)
+    with pytest.raises(ValueError, match="B, Hq, N, D"):
+        B.ems_paged_chunk_attention(p, full, lens, q)
+    pp = _prompt()
+    x, y = torch.zeros((2, 4, 100, 128), dtype=torch.bfloat16), torch.zeros((2, 2, 100, 128), dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="q must be a tensor of the current device"):
+        B.ems_prompt_attention(pp, x, y, y)
+    with pytest.raises(ValueError, match="k_start without q_start"):
+        B.ems_prompt_attention(pp, x, y, y, k_start=lens)
+
+
+def test_new_outputs_have_heads_and_tokens_in_the_queries_order():
+    x = torch.zeros((2, 5, 4, 8))
+    for q in (x, x.transpose(1, 2), x[:, :1], x[:, :, :1].transpose(1, 2), torch.zeros((2, 5, 7, 8))[:, :, 1:5].transpose(1, 2)):
+        o = B._out_like(q)
+        assert o.shape == q.shape
+        if q.shape[1] > 1 and q.shape[2] > 1:
+            assert (o.stride(1) > o.stride(2)) == (q.stride(1) > q.stride(2))
+
+
+# ---- the plain forms themselves
+
+def test_plain_rows_of_attention_agree_with_one_at_a_time():
+    gen = torch.Generator().manual_seed(1)
+    q, k, v = (torch.randn(s, generator=gen) for s in ((6, 16), (9, 16), (9, 16)))
+    seen = causal(6, 9) & (torch.rand(9, generator=gen) < 0.7)[None]
+    assert causal(3, 2).tolist() == [[False, False], [True, False], [True, True]]
+    out, lse, *_ = attention_rows(q, k, v, seen, 0.25, torch.float32)
+    for i in range(6):
+        o, z, _, _ = attention(q[i:i + 1], k, v, seen[i], 0.25, torch.float32)
+        assert torch.allclose(out[i], o[0], atol=1e-13) and torch.allclose(lse[i], z[0])
+    k2, v2 = k.clone(), v.clone()
+    nobody = ~seen.any(0)
+    k2[nobody], v2[nobody] = torch.nan, torch.inf
+    assert torch.equal(attention_rows(q, k2, v2, seen, 0.25, torch.float32)[0], out)
+
+
+def test_plain_codes_are_those_of_the_format():
+    every = torch.arange(256, dtype=torch.uint8).view(torch.float8_e4m3fn).float()
+    finite = every[every.isfinite()].double()
+    zero = torch.tensor(0, dtype=torch.int32)
+    assert torch.equal(codes(finite[:, None], zero.expand(len(finite)))[:, 0], finite)
+    gen = torch.Generator().manual_seed(2)
+    x = torch.cat([torch.randn((200, 16), generator=gen), torch.randn((200, 16), generator=gen) * 1e-3])
+    x[7] = 0
+    s = exponent(top_of(x))
+    assert (top_of(x).double() <= 448 * torch.exp2(s.double())).all()
+    up = s > -126
+    assert (top_of(x).double() > 224 * torch.exp2(s.double()))[up].all() and s[7] == -126
+    near = (x.double() * torch.exp2(-s.double())[:, None]).float().to(torch.float8_e4m3fn).float().double()
+    assert torch.equal(codes(x, s), near)                  # torch's own rounding
