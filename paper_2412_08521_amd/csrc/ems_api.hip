@@ -1004,7 +1004,8 @@ int ems_prompt_attention(const ems_prompt_params* p,
     a.q = q; a.q_sb = q_strides->batch; a.q_sh = q_strides->head; a.q_sn = q_strides->token; a.q_wide = wide(q, *q_strides);
     a.k = k; a.k_sb = k_strides->batch; a.k_sh = k_strides->head; a.k_sn = k_strides->token;
     a.v = v; a.v_sb = v_strides->batch; a.v_sh = v_strides->head; a.v_sn = v_strides->token;
-    a.kv_wide = wide(k, *k_strides) && wide(v, *v_strides);
+    const auto near = [](const ems_strides& st) { return st.token >= 0 && st.token < (1 << 24); };        // 32-bit offsets in a stage
+    a.kv_wide = wide(k, *k_strides) && wide(v, *v_strides) && near(*k_strides) && near(*v_strides);
     a.out = out; a.o_sb = out_strides->batch; a.o_sh = out_strides->head; a.o_sn = out_strides->token; a.o_wide = wide(out, *out_strides);
     a.lse = lse_opt; a.l_sb = packed ? 0 : (long long)p->q_heads * p->q_rows; a.l_sh = p->q_rows;
     a.q_start = q_start_opt; a.k_start = k_start_opt; a.q_rows = p->q_rows; a.k_rows = p->k_rows;

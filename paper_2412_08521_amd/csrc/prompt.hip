@@ -81,6 +81,9 @@ __device__ __forceinline__ void store4(T* p, float x0, float x1, float x2, float
     }
 }
 
+// A condition that hardly ever holds: what copies registers need go to its side.
+__device__ __forceinline__ bool rare(bool x) { return __builtin_expect_with_probability(x, 0, 0.9999); }
+
 // From global memory to LDS, a piece of 16 bytes a lane, from the wave's address on; wait_vmem counts it.
 __device__ __forceinline__ void dma16(const char* from, unsigned lds)
 {
@@ -90,7 +93,7 @@ __device__ __forceinline__ void dma16(const char* from, unsigned lds)
 }  // namespace
 
 template <typename T, int D, bool kPaged, int kW>
-__global__ __launch_bounds__(64 * kW, 2) void prompt_kernel(PromptArgs a)
+__global__ __launch_bounds__(64 * kW, 2) void prompt_simple_kernel(PromptArgs a)
 {
     using St = Stage<T, D>;
     constexpr int kKv = St::kRows, kSubs = kKv / 32;
@@ -409,6 +412,442 @@ __global__ __launch_bounds__(64 * kW, 2) void prompt_kernel(PromptArgs a)
     if (a.lse && half == 0) a.lse[(a.q_start ? q_token : b * a.l_sb + token) + q_head * a.l_sh] = (ref + log2_fast(l)) * 0.6931471805599453f;
 }
 
+// 16-bit rows.  A wave takes kQ tiles of 32 query rows (64 where there are many: every row of keys and values that it reads from
+// LDS goes into two products) and works on three steps of 32 rows at once, products of one beside the weights of another:
+//     S(n) = K(n) Q^T,   P(n - 1) = exp2(S(n - 1) - m),   O += V(n - 2)^T P(n - 2)^T
+template <int D, bool kPaged, int kQ, int kW>
+__global__ __launch_bounds__(64 * kW, D == 128 && kQ == 2 ? 1 : 2) void prompt_kernel(PromptArgs a)
+{
+    typedef bf16_t T;
+    using St = Stage<T, D>;
+    constexpr int kKv = St::kRows;
+    constexpr int kFrags = Tile<T, D>::kFrags, kOut = D / 32;
+    constexpr int kRowsOf = 32 * kQ * kW;
+    constexpr int kHold = 4;                                   // stages whose rows are known
+    __shared__ __align__(1024) char keys[2][St::kBytes];
+    __shared__ __align__(1024) char vals[3][St::kBytes];
+    __shared__ int row_of[kPaged ? kHold : 1][kKv];
+    __shared__ unsigned long long live_of[kPaged ? kHold : 1];
+
+    const int lane = threadIdx.x % kWave, wave = scalar((int)threadIdx.x / kWave);
+    const int col = lane % 32, half = lane / 32;
+    const int head = blockIdx.x % a.kv_heads;
+    int item = blockIdx.x / a.kv_heads, b = 0;
+    const int split = blockIdx.y;
+    Seq seq{};
+    int n_tiles = 0;
+    for (; b < a.batch; ++b) {
+        seq = sequence<kPaged>(a, b);
+        n_tiles = (int)(((long long)seq.n * a.group + kRowsOf - 1) / kRowsOf);
+        if (item < n_tiles) break;
+        item -= n_tiles;
+    }
+    if (b == a.batch) return;
+    const int tile = n_tiles - 1 - item;                       // the last tiles have the most rows to see
+    const int n_rows = seq.n * a.group;                        // (the host holds it to 31 bits)
+    const int r0 = tile * kRowsOf + 32 * kQ * wave;
+    int token[kQ], q_head[kQ], lim[kQ];                        // lim: rows that the lane's query sees (none: <= 0)
+#pragma unroll
+    for (int c = 0; c < kQ; ++c) {
+        const int row = min(r0 + 32 * c + col, n_rows - 1);
+        token[c] = row / a.group;
+        q_head[c] = head * a.group + row - token[c] * a.group;
+        lim[c] = min(token[c] + 1 + seq.m - seq.n, seq.m);
+    }
+    const int lim_min = __builtin_amdgcn_readlane(lim[0], 0), lim_max = __builtin_amdgcn_readlane(lim[kQ - 1], 31);
+    const int last_token = min(tile * kRowsOf + kRowsOf - 1, n_rows - 1) / a.group;
+    const int rows_end = min(max(last_token + 1 + seq.m - seq.n, 0), seq.m);
+    const int n_stages = (rows_end + kKv - 1) / kKv;
+    const int lo = (int)((long long)n_stages * split / a.splits), hi = (int)((long long)n_stages * (split + 1) / a.splits);
+
+    frag_t qf[kQ][kFrags];
+#pragma unroll
+    for (int c = 0; c < kQ; ++c) {
+        const T* q = reinterpret_cast<const T*>(a.q) + q_head[c] * a.q_sh + (a.q_start ? (seq.q_first + token[c]) * a.q_sn : b * a.q_sb + token[c] * a.q_sn);
+#pragma unroll
+        for (int f = 0; f < kFrags; ++f) qf[c][f] = load_piece(q + (2 * f + half) * 8, a.q_wide);
+    }
+
+    // ---- rows of a stage
+    const auto page_of = [&](int t) __attribute__((always_inline)) { return (int)(__umulhi(2u * (unsigned)t, a.page_magic) >> a.page_shift); };
+    const auto table_trip = [&](int it) __attribute__((always_inline)) -> int {
+        const int t = it * kKv + lane;
+        return it >= lo && t < rows_end ? a.page_table[(size_t)b * a.max_pages + page_of(t)] : kNoRow;
+    };
+    const auto row_trip = [&](int it, int entry, int& mask) __attribute__((always_inline)) -> int {
+        const int t = it * kKv + lane;
+        mask = 0;
+        if (entry < 0 || entry >= a.num_pages) return kNoRow;
+        const int r = (entry * a.kv_heads + head - page_of(t)) * a.page_size + t;
+        if (a.pos_pages) mask = a.pos_pages[r];
+        return r;
+    };
+    const auto settle = [&](int slot, int r, int mask) __attribute__((always_inline)) {
+        if (mask < 0) r = kNoRow;
+        const unsigned long long live = __ballot(r != kNoRow);
+        const int spare = live ? __builtin_amdgcn_readlane(r, __builtin_ctzll(live)) : 0;
+        row_of[slot % kHold][lane] = r != kNoRow ? r : spare;
+        if (lane == 0) live_of[slot % kHold] = live;
+    };
+
+    const unsigned k_lds = lds_address(&keys[0][0]), v_lds = lds_address(&vals[0][0]);
+    // A stage's rows go to LDS by kDma instructions, kLoads of them this wave's, each of kDmaRows rows.
+    constexpr int kLoads = (St::kDma + kW - 1) / kW;
+    static_assert(St::kDma % kW == 0, "every wave has as many");
+    const int lane_row = lane / St::kPieces, lane_piece = lane % St::kPieces;
+    const auto row_of_load = [&](int i) __attribute__((always_inline)) { return (i * kW + wave) * St::kDmaRows + lane_row; };
+    const auto key_piece = [&](int i) __attribute__((always_inline)) { return 16 * (lane_piece ^ St::key(row_of_load(i))); };
+    const auto value_piece = [&](int i) __attribute__((always_inline)) { return 16 * (lane_piece ^ St::value(row_of_load(i))); };
+    const T* k_first = nullptr;
+    const T* v_first = nullptr;
+    unsigned k_off[kLoads], v_off[kLoads];                     // from a stage's first row (the host holds strides to 24 bits)
+    if constexpr (!kPaged) {
+        k_first = reinterpret_cast<const T*>(a.k) + (a.q_start ? 0 : b * a.k_sb) + head * a.k_sh + seq.k_first * a.k_sn;
+        v_first = reinterpret_cast<const T*>(a.v) + (a.q_start ? 0 : b * a.v_sb) + head * a.v_sh + seq.k_first * a.v_sn;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            k_off[i] = (unsigned)(row_of_load(i) * (int)a.k_sn) * (unsigned)sizeof(T) + key_piece(i);
+            v_off[i] = (unsigned)(row_of_load(i) * (int)a.v_sn) * (unsigned)sizeof(T) + value_piece(i);
+        }
+    }
+    const auto load_stage = [&](int it, int slot, int kbuf, int vbuf) __attribute__((always_inline)) {
+        const unsigned k_to = k_lds + kbuf * St::kBytes + 1024 * wave, v_to = v_lds + vbuf * St::kBytes + 1024 * wave;
+        if constexpr (kPaged) {
+            if (live_of[slot % kHold] == 0) {                  // nothing there: zeros, which count nothing
+#pragma unroll
+                for (int i = 0; i < kLoads; ++i) {
+                    const int at = 1024 * (i * kW + wave) + 16 * lane;
+                    *reinterpret_cast<frag_t*>(&keys[kbuf][at]) = zero_frag();
+                    *reinterpret_cast<frag_t*>(&vals[vbuf][at]) = zero_frag();
+                }
+                return;
+            }
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const unsigned long long at = (unsigned long long)(unsigned)row_of[slot % kHold][row_of_load(i)] * St::kRowBytes;
+                dma16(reinterpret_cast<const char*>(a.k) + key_piece(i) + at, k_to + 1024 * kW * i);
+                dma16(reinterpret_cast<const char*>(a.v) + value_piece(i) + at, v_to + 1024 * kW * i);
+            }
+        } else if (a.kv_wide && it * kKv + kKv <= seq.m) {
+            const T* k = k_first + (long long)it * kKv * a.k_sn;
+            const T* v = v_first + (long long)it * kKv * a.v_sn;
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                dma_to_lds<16>(k, k_off[i], k_to + 1024 * kW * i);
+                dma_to_lds<16>(v, v_off[i], v_to + 1024 * kW * i);
+            }
+        } else {                                               // rows past the last are read as the last
+#pragma unroll 1
+            for (int i = 0; i < kLoads; ++i) {
+                const long long t = min(it * kKv + row_of_load(i), seq.m - 1);
+                const T* k = k_first + t * a.k_sn + key_piece(i) / (int)sizeof(T);
+                const T* v = v_first + t * a.v_sn + value_piece(i) / (int)sizeof(T);
+                const int at = 1024 * (i * kW + wave) + 16 * lane;
+                *reinterpret_cast<frag_t*>(&keys[kbuf][at]) = load_piece(k, a.kv_wide);
+                *reinterpret_cast<frag_t*>(&vals[vbuf][at]) = load_piece(v, a.kv_wide);
+            }
+        }
+    };
+
+    // ---- the wave's state
+    f32x16_t o[kQ][kOut], s[2][kQ];                            // s: of the step whose products run, and of the one before
+    frag_t p[2][kQ][2];                                        // weights, the same way
+    frag_t kf[kFrags], vf[2][kOut];
+    float m[kQ], l[kQ];                                        // of the lane's queries; l: this lane's rows only
+#pragma unroll
+    for (int c = 0; c < kQ; ++c) {
+#pragma unroll
+        for (int i = 0; i < kOut; ++i) o[c][i] = zero_acc();
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[1][c][r] = -INFINITY;
+        p[0][c][0] = p[0][c][1] = zero_frag();
+        m[c] = -INFINITY; l[c] = 0.f;
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < kOut; ++i) vf[t][i] = zero_frag();
+    struct Step { int row; unsigned live; bool edge; };        // first row; rows that are there; some query does not see all of them
+    Step before{0, 0, true}, old{0, 0, false};                 // of s[1 - cur] and of vf: first of none, with values that are anything
+
+    const unsigned k_base = col * St::kRowBytes + 16 * (half ^ St::key(col));
+    const int v_row = 4 * half + lane % 16 / 4;
+    const unsigned v_base = v_row * St::kRowBytes + 16 * ((2 * (lane / 16 % 2) + lane % 4 / 2) ^ St::value(v_row)) + 8 * (lane % 2);
+    const auto lds_frag = [](unsigned at) __attribute__((always_inline)) { return *(const __attribute__((address_space(3))) frag_t*)(uintptr_t)at; };
+    const auto value_frag = [&](unsigned at, int t, int i) __attribute__((always_inline)) {   // rows 16 t .. 16 t + 15 of a step
+        const s16x4_t x = read_transposed(((v_base + at) ^ (64 * i)) + 16 * t * St::kRowBytes);
+        const s16x4_t y = read_transposed(((v_base + at) ^ (64 * i)) + (16 * t + 8) * St::kRowBytes);
+        return __builtin_bit_cast(frag_t, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    constexpr bool kAcc = D == 128 && kQ == 2;
+    const auto add_out = [&](f32x16_t& x, const frag_t& v, const frag_t& w) __attribute__((always_inline)) {
+        if constexpr (kAcc) asm("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(x) : "v"(v), "v"(w));
+        else mma<T>(x, v, w);
+    };
+    const auto settle_out = [&]() __attribute__((always_inline)) {
+        if constexpr (kAcc)
+#pragma unroll
+            for (int c = 0; c < kQ; ++c)
+                asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 3" : "+a"(o[c][0]), "+a"(o[c][1]), "+a"(o[c][2]), "+a"(o[c][kOut - 1]));
+    };
+    // which of a step's rows 4 half + (0..3) + 8 (0..3) the lane's query sees, bit acc_row(r, 0)
+    const auto seen = [&](const Step& st, int c) __attribute__((always_inline)) {
+        const int left = lim[c] - st.row;
+        return ((left >= 32 ? ~0u : left <= 0 ? 0u : (1u << left) - 1) & st.live) >> (4 * half);
+    };
+    const auto hide = [&](f32x16_t (&x)[kQ], const Step& st) __attribute__((always_inline)) {
+#pragma unroll
+        for (int c = 0; c < kQ; ++c) {
+            const unsigned bits = seen(st, c);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) x[c][r] = (bits >> acc_row(r, 0)) & 1 ? x[c][r] : -INFINITY;
+        }
+    };
+    // Where some query does not see a row, the row's value counts 0 times: an infinity or NaN there must not.  It is taken out of
+    // the products (hardly ever there), and a second product says which queries see one.
+    const auto take_out = [&](const Step& st) __attribute__((always_inline)) {
+        typedef short s16x8_t __attribute__((ext_vector_type(8)));
+        typedef unsigned short u16x8_t __attribute__((ext_vector_type(8)));
+        s16x8_t up = 0;
+        u16x8_t down = 0;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < kOut; ++i) {
+                up = __builtin_elementwise_max(up, __builtin_bit_cast(s16x8_t, vf[t][i]));
+                down = __builtin_elementwise_max(down, __builtin_bit_cast(u16x8_t, vf[t][i]));
+            }
+        bool odd = false;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) odd |= up[e] >= 0x7f80 || down[e] >= 0xff80;
+        if (!rare(__any(odd))) return;
+        settle_out();
+#pragma unroll
+        for (int c = 0; c < kQ; ++c) {
+            const unsigned bits = seen(st, c);
+#pragma unroll
+            for (int i = 0; i < kOut; ++i) {
+                f32x16_t count = zero_acc();
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const bf16x8_t x = __builtin_bit_cast(bf16x8_t, vf[t][i]);
+                    bf16x8_t not_finite, sees;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        not_finite[e] = (bf16_t)(fabsf((float)x[e]) < INFINITY ? 0.f : 1.f);
+                        sees[e] = (bf16_t)((bits >> acc_row(8 * t + e, 0)) & 1 ? 1.f : 0.f);
+                    }
+                    mma<T>(count, __builtin_bit_cast(frag_t, not_finite), __builtin_bit_cast(frag_t, sees));
+                }
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[c][i][r] = count[r] > 0.f ? NAN : o[c][i][r];
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < kOut; ++i) {
+                bf16x8_t x = __builtin_bit_cast(bf16x8_t, vf[t][i]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = fabsf((float)x[e]) < INFINITY ? x[e] : (bf16_t)0.f;
+                vf[t][i] = __builtin_bit_cast(frag_t, x);
+            }
+    };
+    // The reference m stays where it is while the weights' sum has room: a row's weights are relative to it, and nothing is lost by
+    // their size.  Else it goes up to the largest logit, and the step's weights are formed again.
+    constexpr float kRoom = 0x1p30f;
+    const auto raise = [&](const f32x16_t (&x)[kQ], frag_t (&w)[kQ][2], float (&sum)[kQ]) __attribute__((always_inline)) {
+        settle_out();
+#pragma unroll
+        for (int c = 0; c < kQ; ++c) {
+            float top = x[c][0];
+#pragma unroll
+            for (int r = 1; r < 16; ++r) top = fmaxf(top, x[c][r]);
+            const float m_new = fmaxf(m[c], halves_max(top) * a.scale_log2e), ref = m_new > -INFINITY ? m_new : 0.f;
+            const float shrink = exp2_fast(m[c] - ref);
+            l[c] *= shrink;
+#pragma unroll
+            for (int i = 0; i < kOut; ++i) o[c][i] *= shrink;
+            m[c] = m_new;
+            sum[c] = 0.f;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                bf16x8_t y;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float z = exp2_fast(__builtin_fmaf(x[c][8 * t + e], a.scale_log2e, -ref));
+                    sum[c] += z;
+                    y[e] = (bf16_t)z;
+                }
+                w[c][t] = __builtin_bit_cast(frag_t, y);
+            }
+        }
+    };
+
+    // One turn: the products of step n (keys at k_at) go to s[cur], the weights of step n - 1 come from s[1 - cur], the values of
+    // step n - 2 are in vf, and those of step n - 1 (at v_at) take their place.
+    constexpr int kPv = 2 * kOut * kQ, kQk = kFrags * kQ, kSlots = kPv + kQk, kElems = 16 * kQ;
+    const auto turn = [&](auto cur_, unsigned k_at, unsigned v_at) __attribute__((always_inline)) {
+        constexpr int cur = decltype(cur_)::value;
+        float sum[kQ], ref[kQ], y[kElems];
+#pragma unroll
+        for (int c = 0; c < kQ; ++c) { sum[c] = 0.f; ref[c] = m[c] > -INFINITY ? m[c] : 0.f; }
+        const auto element = [&](int e) __attribute__((always_inline)) {
+            if (e < kElems) y[e] = __builtin_fmaf(s[1 - cur][e / 16][e % 16], a.scale_log2e, -ref[e / 16]);
+            if (e >= 1 && e - 1 < kElems) y[e - 1] = exp2_fast(y[e - 1]);
+            if (e >= 2 && e - 2 < kElems) {
+                sum[(e - 2) / 16] += y[e - 2];
+                if (e % 2 == 1) {
+                    const int c = (e - 2) / 16, t = (e - 2) % 16 / 8, i = (e - 2) % 8 / 2;
+                    typedef bf16_t pair_t __attribute__((ext_vector_type(2)));
+                    p[1 - cur][c][t][i] = __builtin_bit_cast(int, pair_t{(bf16_t)y[e - 3], (bf16_t)y[e - 2]});
+                }
+            }
+        };
+#pragma unroll
+        for (int n = 0; n < kPv; ++n) {
+            const int t = n / (kOut * kQ), i = n / kQ % kOut, c = n % kQ;
+            add_out(o[c][i], vf[t][i], p[cur][c][t]);
+            if (n < kFrags) kf[n] = lds_frag((k_base + k_at) ^ (32 * n));
+#pragma unroll
+            for (int e = n * kElems / kSlots; e < (n + 1) * kElems / kSlots; ++e) element(e);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int n = 0; n < kQk; ++n) {
+            const int f = n / kQ, c = n % kQ;
+            if (f == 0) mma_first<T>(s[cur][c], kf[f], qf[c][f]);
+            else mma<T>(s[cur][c], kf[f], qf[c][f]);
+            constexpr int kV = 2 * kOut;
+#pragma unroll
+            for (int x = n * kV / kQk; x < (n + 1) * kV / kQk; ++x) vf[x / kOut][x % kOut] = value_frag(v_at, x / kOut, x % kOut);
+#pragma unroll
+            for (int e = (n + kPv) * kElems / kSlots; e < (n + kPv + 1) * kElems / kSlots; ++e) element(e);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        element(kElems);
+        element(kElems + 1);
+        bool room = true;
+#pragma unroll
+        for (int c = 0; c < kQ; ++c) room &= sum[c] <= kRoom && m[c] > -INFINITY;
+        if (rare(!__all(room))) raise(s[1 - cur], p[1 - cur], sum);
+#pragma unroll
+        for (int c = 0; c < kQ; ++c) l[c] += sum[c];
+    };
+
+    // Stages come last rows first.  One is in flight while one is worked on; rows of pages are looked up two further on.
+    int entry = kNoRow, far = kNoRow, far_mask = 0;
+    if constexpr (kPaged) {
+        if (wave == 0 && hi > lo) {
+#pragma unroll
+            for (int i = 1; i <= 2; ++i) {
+                int mask;
+                const int r = row_trip(hi - i, table_trip(hi - i), mask);
+                settle(hi - i + kHold, r, mask);               // (hi - 2 may be -1)
+            }
+            far = row_trip(hi - 3, table_trip(hi - 3), far_mask);
+            entry = table_trip(hi - 4);
+        }
+        __syncthreads();
+    }
+    int kbuf = 0, vbuf = 0;
+    unsigned v_prev = v_lds;                                   // values of the step before (any, where there is none)
+    if (hi > lo) load_stage(hi - 1, hi - 1 + kHold, 0, 0);
+    const bool works = r0 < n_rows;
+    int it = hi - 1;
+    const auto stage = [&](auto top_) __attribute__((always_inline)) {
+        constexpr bool kTop = decltype(top_)::value;           // some query may not see all of the rows at hand
+        wait_vmem_all_visible();
+        __syncthreads();
+        const int vnext = vbuf == 2 ? 0 : vbuf + 1;
+        if (it > lo) load_stage(it - 1, it - 1 + kHold, kbuf ^ 1, vnext);
+        unsigned long long live = ~0ull;
+        if constexpr (kPaged) {
+            live = live_of[it % kHold];
+            live = ((unsigned long long)(unsigned)scalar((int)(live >> 32)) << 32) | (unsigned)scalar((int)live);
+            if (wave == 0) {
+                settle(it - 2 + kHold, far, far_mask);
+                far = row_trip(it - 3, entry, far_mask);
+                entry = table_trip(it - 4);
+            }
+        }
+        if (works && (!kTop || it * kKv < lim_max)) {
+#pragma unroll
+            for (int j = 1; j >= 0; --j) {
+                const Step now{it * kKv + 32 * j, (unsigned)(live >> (32 * j)), it * kKv + 32 * j + 32 > lim_min};
+                if (rare((kTop && before.edge) || (kPaged && before.live != ~0u))) hide(j == 1 ? s[1] : s[0], before);
+                if constexpr (kTop) if (rare(old.edge)) take_out(old);
+                if (j == 1) turn(ic<0>{}, k_lds + kbuf * St::kBytes + 32 * St::kRowBytes, v_prev);
+                else turn(ic<1>{}, k_lds + kbuf * St::kBytes, v_prev);
+                v_prev = v_lds + vbuf * St::kBytes + 32 * j * St::kRowBytes;
+                old = before;
+                before = now;
+            }
+        }
+        kbuf ^= 1;
+        vbuf = vnext;
+    };
+    // stages that some query does not see whole, and one more for what is under way; then those that need no look at it
+    const int whole = lim_min / kKv - 1;
+    for (; it >= lo && it >= whole; --it) stage(std::true_type{});
+    for (; it >= lo; --it) stage(std::false_type{});
+
+    // the last two steps' ends: weights of s[1], values of vf and of v_prev
+    if (before.edge || (kPaged && before.live != ~0u)) hide(s[1], before);
+    if (old.edge) take_out(old);
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < kOut; ++i)
+#pragma unroll
+            for (int c = 0; c < kQ; ++c) add_out(o[c][i], vf[t][i], p[0][c][t]);
+    if (hi > lo) {
+        float sum[kQ];
+        raise(s[1], p[1], sum);
+#pragma unroll
+        for (int c = 0; c < kQ; ++c) l[c] += sum[c];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < kOut; ++i) vf[t][i] = value_frag(v_prev, t, i);
+        if (before.edge) take_out(before);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < kOut; ++i)
+#pragma unroll
+                for (int c = 0; c < kQ; ++c) add_out(o[c][i], vf[t][i], p[1][c][t]);
+    }
+    settle_out();
+
+    // ---- the lane's queries: columns 32 i + acc_row(r, half)
+#pragma unroll
+    for (int c = 0; c < kQ; ++c) {
+        const float total = halves_sum(l[c]);
+        if (r0 + 32 * c + col >= n_rows) continue;
+        const float ref = m[c] > -INFINITY ? m[c] : 0.f;
+        const long long q_token = seq.q_first + token[c];
+        if (a.splits > 1) {
+            const long long at = (q_token * a.kv_heads * a.group + q_head[c]) * a.splits + split;
+#pragma unroll
+            for (int i = 0; i < kOut; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; r += 4)
+                    *reinterpret_cast<f32x4_t*>(a.part_o + at * D + 32 * i + acc_row(r, half)) = f32x4_t{o[c][i][r], o[c][i][r + 1], o[c][i][r + 2], o[c][i][r + 3]};
+            if (half == 0) { a.part_ml[2 * at] = m[c]; a.part_ml[2 * at + 1] = total; }
+            continue;
+        }
+        const float inv = total == 0.f ? 0.f : 1.f / total;    // (NaN stays)
+        T* out = reinterpret_cast<T*>(a.out) + q_head[c] * a.o_sh + (a.q_start ? q_token * a.o_sn : b * a.o_sb + token[c] * a.o_sn);
+#pragma unroll
+        for (int i = 0; i < kOut; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4)
+                store4(out + 32 * i + acc_row(r, half), o[c][i][r] * inv, o[c][i][r + 1] * inv, o[c][i][r + 2] * inv, o[c][i][r + 3] * inv, a.o_wide);
+        if (a.lse && half == 0) a.lse[(a.q_start ? q_token : b * a.l_sb + token[c]) + q_head[c] * a.l_sh] = (ref + log2_fast(total)) * 0.6931471805599453f;
+    }
+}
+
 // ---- joining
 
 template <typename T, int D, bool kPaged>
@@ -481,10 +920,17 @@ hipError_t launch(PromptArgs a, const PromptPlan& plan, hipStream_t st)
     a.page_magic = kPaged ? (unsigned)(((1ull << (31 + a.page_shift)) + a.page_size - 1) / a.page_size) : 0;
     a.splits = plan.splits;
     const dim3 grid((unsigned)(plan.tiles * a.kv_heads), plan.splits);
-    if (plan.waves == 8) prompt_kernel<T, D, kPaged, 8><<<grid, 512, 0, st>>>(a);
-    else if (plan.waves == 4) prompt_kernel<T, D, kPaged, 4><<<grid, 256, 0, st>>>(a);
-    else if (plan.waves == 2) prompt_kernel<T, D, kPaged, 2><<<grid, 128, 0, st>>>(a);
-    else prompt_kernel<T, D, kPaged, 1><<<grid, 64, 0, st>>>(a);
+    if constexpr (sizeof(T) == 2) {
+        if (plan.waves == 8) prompt_kernel<D, kPaged, 2, 4><<<grid, 256, 0, st>>>(a);
+        else if (plan.waves == 4) prompt_kernel<D, kPaged, 1, 4><<<grid, 256, 0, st>>>(a);
+        else if (plan.waves == 2) prompt_kernel<D, kPaged, 1, 2><<<grid, 128, 0, st>>>(a);
+        else prompt_kernel<D, kPaged, 1, 1><<<grid, 64, 0, st>>>(a);
+    } else {
+        if (plan.waves == 8) prompt_simple_kernel<T, D, kPaged, 8><<<grid, 512, 0, st>>>(a);
+        else if (plan.waves == 4) prompt_simple_kernel<T, D, kPaged, 4><<<grid, 256, 0, st>>>(a);
+        else if (plan.waves == 2) prompt_simple_kernel<T, D, kPaged, 2><<<grid, 128, 0, st>>>(a);
+        else prompt_simple_kernel<T, D, kPaged, 1><<<grid, 64, 0, st>>>(a);
+    }
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && a.splits > 1) {
         const long long rows = a.q_tokens * a.kv_heads * a.group, per = 256 / (D / 4);
