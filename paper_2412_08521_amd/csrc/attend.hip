@@ -59,20 +59,6 @@ __device__ __forceinline__ void wave_handover()
     __builtin_amdgcn_wave_barrier();
 }
 
-// Inclusive sums over the lanes of a wave.
-template <int kCtrl, int kRowMask>
-__device__ __forceinline__ int dpp_or_zero(int v) { return __builtin_amdgcn_update_dpp(0, v, kCtrl, kRowMask, 0xf, false); }
-__device__ __forceinline__ int wave_scan(int v)
-{
-    v += dpp_or_zero<0x111, 0xf>(v);       // one lane up inside each row of 16
-    v += dpp_or_zero<0x112, 0xf>(v);
-    v += dpp_or_zero<0x114, 0xf>(v);
-    v += dpp_or_zero<0x118, 0xf>(v);
-    v += dpp_or_zero<0x142, 0xa>(v);       // lane 15 of a row to the next row
-    v += dpp_or_zero<0x143, 0xc>(v);       // lane 31 to the upper half
-    return v;
-}
-
 // Workers share the units of a kv-head's sequences evenly: worker w takes `per` of them, one of the first `more` one more.
 struct Share {
     int per, more, workers;

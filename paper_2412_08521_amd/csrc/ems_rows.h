@@ -126,6 +126,20 @@ constexpr int kDppXor2 = 0x4E;         // quad_perm [2,3,0,1]
 constexpr int kDppHalfMirror = 0x141;  // lane i <-> 7 - i inside each group of 8
 constexpr int kDppMirror = 0x140;      // lane i <-> 15 - i inside each row of 16
 
+// Inclusive sums over the lanes of a wave.
+template <int kCtrl, int kRowMask>
+__device__ __forceinline__ int dpp_or_zero(int v) { return __builtin_amdgcn_update_dpp(0, v, kCtrl, kRowMask, 0xf, false); }
+__device__ __forceinline__ int wave_scan(int v)
+{
+    v += dpp_or_zero<0x111, 0xf>(v);       // one lane up inside each row of 16
+    v += dpp_or_zero<0x112, 0xf>(v);
+    v += dpp_or_zero<0x114, 0xf>(v);
+    v += dpp_or_zero<0x118, 0xf>(v);
+    v += dpp_or_zero<0x142, 0xa>(v);       // lane 15 of a row to the next row
+    v += dpp_or_zero<0x143, 0xc>(v);       // lane 31 to the upper half
+    return v;
+}
+
 template <bool kMax> __device__ __forceinline__ float comb(float a, float b) { return kMax ? fmaxf(a, b) : a + b; }
 __device__ __forceinline__ float lane_value(float v, int lane)
 {

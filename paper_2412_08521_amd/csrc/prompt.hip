@@ -19,7 +19,7 @@ namespace {
 constexpr int kNoRow = -1;
 
 // A sequence: its queries, its rows, and where they begin.
-struct Seq { int n, m; long long q_first, k_first; };
+struct Seq { int n, m, q_first, k_first; };
 
 template <bool kPaged>
 __device__ __forceinline__ Seq sequence(const PromptArgs& a, int b)
@@ -27,12 +27,68 @@ __device__ __forceinline__ Seq sequence(const PromptArgs& a, int b)
     if constexpr (kPaged) {
         const long long most = (long long)a.max_pages * a.page_size;
         const int n = a.new_len ? min(max(a.new_len[b], 0), a.q_rows) : a.q_rows;
-        return {n, (int)min((long long)max(a.lens[b], 0), most), (long long)b * a.q_rows, 0};
+        return {n, (int)min((long long)max(a.lens[b], 0), most), b * a.q_rows, 0};
     }
-    if (!a.q_start) return {a.q_rows, a.k_rows, (long long)b * a.q_rows, 0};
+    if (!a.q_start) return {a.q_rows, a.k_rows, b * a.q_rows, 0};
     const int q0 = min(max(a.q_start[b], 0), a.q_rows), q1 = min(max(a.q_start[b + 1], q0), a.q_rows);
     const int k0 = min(max(a.k_start[b], 0), a.k_rows), k1 = min(max(a.k_start[b + 1], k0), a.k_rows);
     return {q1 - q0, k1 - k0, q0, k0};
+}
+
+// Which sequence and tile of kRowsOf query rows is the j-th of a kv-head; b = -1: there are not as many.  Tiles with the most rows to
+// see come first: blocks begin in this order, and the last ones are then short.
+struct Place { int b, tile, n_tiles; Seq seq; };
+__device__ __forceinline__ int tiles_of_rows(long long rows, int rows_of) { return (int)((rows + rows_of - 1) / rows_of); }
+
+template <bool kPaged>
+__device__ __forceinline__ Place find_tile(const PromptArgs& a, int j, int rows_of)
+{
+    const int lane = threadIdx.x % kWave;
+    if (kPaged ? a.batch == 1 || (a.batch > kWave && !a.new_len) : !a.q_start) {         // tiles of every sequence alike
+        const int b = j % a.batch;
+        const Seq s = sequence<kPaged>(a, b);
+        const int n = tiles_of_rows((long long)s.n * a.group, rows_of), t = n - 1 - j / a.batch;
+        return {t >= 0 ? b : -1, t, n, s};
+    }
+    const auto from_lane = [](const Seq& s, int b) {
+        return Seq{__builtin_amdgcn_readlane(s.n, b), __builtin_amdgcn_readlane(s.m, b), __builtin_amdgcn_readlane(s.q_first, b),
+                   __builtin_amdgcn_readlane(s.k_first, b)};
+    };
+    const auto total = [](int x) { return __builtin_amdgcn_readlane(wave_scan(x), 63); };
+    if (a.batch <= kWave) {
+        // tile t of a sequence has level base + t: the tiles' worth of rows that its queries see, about
+        const Seq s = lane < a.batch ? sequence<kPaged>(a, lane) : Seq{0, 0, 0, 0};
+        const int n = tiles_of_rows((long long)s.n * a.group, rows_of);
+        const int base = s.m > s.n ? (int)((long long)(s.m - s.n) * a.group / rows_of) : 0;
+        const auto from = [&](int level) { return total(min(max(base + n - level, 0), n)); };         // tiles of that level and above
+        int lo = 0, hi = n ? base + n : 0;                     // from(lo) > j >= from(hi)
+        for (int x = 1; x < kWave; x *= 2) hi = max(hi, __shfl_xor(hi, x));
+        hi = scalar(hi);
+        int above = 0;                                         // from(hi)
+        if (from(0) <= j) return {-1, 0, 0, s};
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1, x = from(mid);
+            if (x > j) lo = mid;
+            else { hi = mid; above = x; }
+        }
+        const bool has = n > 0 && base <= lo && lo < base + n;
+        const unsigned long long those = __ballot(has);
+        const int before = __builtin_amdgcn_mbcnt_hi((unsigned)(those >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)those, 0));
+        const int b = __builtin_ctzll(__ballot(has && before == j - above));
+        return {b, lo - __builtin_amdgcn_readlane(base, b), __builtin_amdgcn_readlane(n, b), from_lane(s, b)};
+    }
+    for (int b0 = 0; b0 < a.batch; b0 += kWave) {              // many sequences: in their order
+        const Seq s = b0 + lane < a.batch ? sequence<kPaged>(a, b0 + lane) : Seq{0, 0, 0, 0};
+        const int n = tiles_of_rows((long long)s.n * a.group, rows_of), sum = wave_scan(n);
+        const unsigned long long past = __ballot(sum > j);
+        if (past) {
+            const int at = __builtin_ctzll(past);
+            const int n_at = __builtin_amdgcn_readlane(n, at);
+            return {b0 + at, __builtin_amdgcn_readlane(sum, at) - 1 - j, n_at, from_lane(s, at)};
+        }
+        j -= __builtin_amdgcn_readlane(sum, 63);
+    }
+    return {-1, 0, 0, Seq{0, 0, 0, 0}};
 }
 
 // Bytes of LDS that a stage of keys (or values) takes, and where its pieces of 16 bytes are: a row's pieces change places by
@@ -90,6 +146,33 @@ __device__ __forceinline__ void dma16(const char* from, unsigned lds)
     asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(scalar((int)lds)) : "memory", "m0");
 }
 
+// The same for two or four instructions on neighbouring KiB of LDS, from `base` on by 32-bit offsets or from 64-bit addresses.  An
+// instruction's own offset (0, 1024, ..) counts on both sides, so those that are passed are that much lower (kDmaBias higher).
+constexpr unsigned kDmaBias = 3072;
+template <int kN>
+__device__ __forceinline__ void dma_group(const void* base, const unsigned (&off)[kN], unsigned lds)
+{
+    const char* b = static_cast<const char*>(base) - kDmaBias;
+    if constexpr (kN == 4)
+        asm volatile("s_mov_b32 m0, %5\n\tglobal_load_lds_dwordx4 %0, %4\n\tglobal_load_lds_dwordx4 %1, %4 offset:1024\n\t"
+                     "global_load_lds_dwordx4 %2, %4 offset:2048\n\tglobal_load_lds_dwordx4 %3, %4 offset:3072"
+                     ::"v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(b), "s"(lds) : "memory", "m0");
+    else
+        asm volatile("s_mov_b32 m0, %3\n\tglobal_load_lds_dwordx4 %0, %2\n\tglobal_load_lds_dwordx4 %1, %2 offset:1024"
+                     ::"v"(off[0]), "v"(off[1]), "s"(b), "s"(lds) : "memory", "m0");
+}
+template <int kN>
+__device__ __forceinline__ void dma_group(const char* const (&from)[kN], unsigned lds)
+{
+    if constexpr (kN == 4)
+        asm volatile("s_mov_b32 m0, %4\n\tglobal_load_lds_dwordx4 %0, off\n\tglobal_load_lds_dwordx4 %1, off offset:1024\n\t"
+                     "global_load_lds_dwordx4 %2, off offset:2048\n\tglobal_load_lds_dwordx4 %3, off offset:3072"
+                     ::"v"(from[0]), "v"(from[1]), "v"(from[2]), "v"(from[3]), "s"(lds) : "memory", "m0");
+    else
+        asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, off\n\tglobal_load_lds_dwordx4 %1, off offset:1024"
+                     ::"v"(from[0]), "v"(from[1]), "s"(lds) : "memory", "m0");
+}
+
 }  // namespace
 
 template <typename T, int D, bool kPaged, int kW>
@@ -106,19 +189,11 @@ __global__ __launch_bounds__(64 * kW, 2) void prompt_simple_kernel(PromptArgs a)
 
     const int lane = threadIdx.x % kWave, wave = scalar((int)threadIdx.x / kWave);
     const int col = lane % 32, half = lane / 32;
-    const int head = blockIdx.x % a.kv_heads;
-    int item = blockIdx.x / a.kv_heads, b = 0;
-    const int split = blockIdx.y;
-    Seq seq{};
-    int n_tiles = 0;
-    for (; b < a.batch; ++b) {
-        seq = sequence<kPaged>(a, b);
-        n_tiles = (int)(((long long)seq.n * a.group + kRowsOf - 1) / kRowsOf);
-        if (item < n_tiles) break;
-        item -= n_tiles;
-    }
-    if (b == a.batch) return;
-    const int tile = n_tiles - 1 - item;                       // the last tiles have the most rows to see
+    const int head = blockIdx.x % a.kv_heads, split = blockIdx.y;
+    const Place place = find_tile<kPaged>(a, blockIdx.x / a.kv_heads, kRowsOf);
+    if (place.b < 0) return;
+    const int b = scalar(place.b), tile = scalar(place.tile);
+    const Seq seq{scalar(place.seq.n), scalar(place.seq.m), scalar(place.seq.q_first), scalar(place.seq.k_first)};
     const int n_rows = seq.n * a.group;                        // (the host holds it to 31 bits)
     const int r0 = tile * kRowsOf + 32 * wave;
     const int row = min(r0 + col, n_rows - 1);
@@ -431,19 +506,12 @@ __global__ __launch_bounds__(64 * kW, D == 128 && kQ == 2 ? 1 : 2) void prompt_k
 
     const int lane = threadIdx.x % kWave, wave = scalar((int)threadIdx.x / kWave);
     const int col = lane % 32, half = lane / 32;
-    const int head = blockIdx.x % a.kv_heads;
-    int item = blockIdx.x / a.kv_heads, b = 0;
     const int split = blockIdx.y;
-    Seq seq{};
-    int n_tiles = 0;
-    for (; b < a.batch; ++b) {
-        seq = sequence<kPaged>(a, b);
-        n_tiles = (int)(((long long)seq.n * a.group + kRowsOf - 1) / kRowsOf);
-        if (item < n_tiles) break;
-        item -= n_tiles;
-    }
-    if (b == a.batch) return;
-    const int tile = n_tiles - 1 - item;                       // the last tiles have the most rows to see
+    const int head = blockIdx.x % a.kv_heads;
+    const Place place = find_tile<kPaged>(a, blockIdx.x / a.kv_heads, kRowsOf);
+    if (scalar(place.b) < 0) return;
+    const int b = scalar(place.b), tile = scalar(place.tile);
+    const Seq seq{scalar(place.seq.n), scalar(place.seq.m), scalar(place.seq.q_first), scalar(place.seq.k_first)};
     const int n_rows = seq.n * a.group;                        // (the host holds it to 31 bits)
     const int r0 = tile * kRowsOf + 32 * kQ * wave;
     int token[kQ], q_head[kQ], lim[kQ];                        // lim: rows that the lane's query sees (none: <= 0)
@@ -491,62 +559,73 @@ __global__ __launch_bounds__(64 * kW, D == 128 && kQ == 2 ? 1 : 2) void prompt_k
     };
 
     const unsigned k_lds = lds_address(&keys[0][0]), v_lds = lds_address(&vals[0][0]);
-    // A stage's rows go to LDS by kDma instructions, kLoads of them this wave's, each of kDmaRows rows.
-    constexpr int kLoads = (St::kDma + kW - 1) / kW;
-    static_assert(St::kDma % kW == 0, "every wave has as many");
-    const int lane_row = lane / St::kPieces, lane_piece = lane % St::kPieces;
-    const auto row_of_load = [&](int i) __attribute__((always_inline)) { return (i * kW + wave) * St::kDmaRows + lane_row; };
-    const auto key_piece = [&](int i) __attribute__((always_inline)) { return 16 * (lane_piece ^ St::key(row_of_load(i))); };
-    const auto value_piece = [&](int i) __attribute__((always_inline)) { return 16 * (lane_piece ^ St::value(row_of_load(i))); };
-    const T* k_first = nullptr;
-    const T* v_first = nullptr;
+    // A stage's rows go to LDS by kDma instructions, neighbouring ones of which are a wave's, in groups under one LDS address.
+    constexpr int kLoads = St::kDma / kW, kGroup = kLoads < 4 ? kLoads : 4;
+    static_assert(St::kDma % kW == 0 && kLoads % kGroup == 0 && (kGroup == 2 || kGroup == 4), "every wave has whole groups");
+    const auto row_of_load = [&](int i) __attribute__((always_inline)) { return (wave * kLoads + i) * St::kDmaRows + lane / St::kPieces; };
+    const auto key_piece = [&](int i) __attribute__((always_inline)) { return 16 * (lane % St::kPieces ^ St::key(row_of_load(i))); };
+    const auto value_piece = [&](int i) __attribute__((always_inline)) { return 16 * (lane % St::kPieces ^ St::value(row_of_load(i))); };
+    const char* k_first = nullptr;                             // the sequence's rows
+    const char* v_first = nullptr;
+    const char* k_next = nullptr;                              // those of the stage that is loaded next
+    const char* v_next = nullptr;
+    const long long k_step = a.k_sn * (long long)sizeof(T), v_step = a.v_sn * (long long)sizeof(T);       // bytes from row to row
     unsigned k_off[kLoads], v_off[kLoads];                     // from a stage's first row (the host holds strides to 24 bits)
     if constexpr (!kPaged) {
-        k_first = reinterpret_cast<const T*>(a.k) + (a.q_start ? 0 : b * a.k_sb) + head * a.k_sh + seq.k_first * a.k_sn;
-        v_first = reinterpret_cast<const T*>(a.v) + (a.q_start ? 0 : b * a.v_sb) + head * a.v_sh + seq.k_first * a.v_sn;
+        k_first = reinterpret_cast<const char*>(reinterpret_cast<const T*>(a.k) + (a.q_start ? 0 : b * a.k_sb) + head * a.k_sh + seq.k_first * a.k_sn);
+        v_first = reinterpret_cast<const char*>(reinterpret_cast<const T*>(a.v) + (a.q_start ? 0 : b * a.v_sb) + head * a.v_sh + seq.k_first * a.v_sn);
+        k_next = k_first + (hi - 1) * kKv * k_step;
+        v_next = v_first + (hi - 1) * kKv * v_step;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            k_off[i] = (unsigned)(row_of_load(i) * (int)a.k_sn) * (unsigned)sizeof(T) + key_piece(i);
-            v_off[i] = (unsigned)(row_of_load(i) * (int)a.v_sn) * (unsigned)sizeof(T) + value_piece(i);
+            k_off[i] = (unsigned)row_of_load(i) * (unsigned)k_step + key_piece(i) + kDmaBias - 1024 * (i % kGroup);
+            v_off[i] = (unsigned)row_of_load(i) * (unsigned)v_step + value_piece(i) + kDmaBias - 1024 * (i % kGroup);
         }
     }
     const auto load_stage = [&](int it, int slot, int kbuf, int vbuf) __attribute__((always_inline)) {
-        const unsigned k_to = k_lds + kbuf * St::kBytes + 1024 * wave, v_to = v_lds + vbuf * St::kBytes + 1024 * wave;
+        const unsigned k_to = scalar((int)(k_lds + kbuf * St::kBytes)) + 1024 * kLoads * wave, v_to = scalar((int)(v_lds + vbuf * St::kBytes)) + 1024 * kLoads * wave;
         if constexpr (kPaged) {
             if (live_of[slot % kHold] == 0) {                  // nothing there: zeros, which count nothing
 #pragma unroll
                 for (int i = 0; i < kLoads; ++i) {
-                    const int at = 1024 * (i * kW + wave) + 16 * lane;
+                    const int at = 1024 * (wave * kLoads + i) + 16 * lane;
                     *reinterpret_cast<frag_t*>(&keys[kbuf][at]) = zero_frag();
                     *reinterpret_cast<frag_t*>(&vals[vbuf][at]) = zero_frag();
                 }
                 return;
             }
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                const unsigned long long at = (unsigned long long)(unsigned)row_of[slot % kHold][row_of_load(i)] * St::kRowBytes;
-                dma16(reinterpret_cast<const char*>(a.k) + key_piece(i) + at, k_to + 1024 * kW * i);
-                dma16(reinterpret_cast<const char*>(a.v) + value_piece(i) + at, v_to + 1024 * kW * i);
-            }
-        } else if (a.kv_wide && it * kKv + kKv <= seq.m) {
-            const T* k = k_first + (long long)it * kKv * a.k_sn;
-            const T* v = v_first + (long long)it * kKv * a.v_sn;
+            for (int g = 0; g < kLoads; g += kGroup) {
+                const char *k[kGroup], *v[kGroup];
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) {
-                dma_to_lds<16>(k, k_off[i], k_to + 1024 * kW * i);
-                dma_to_lds<16>(v, v_off[i], v_to + 1024 * kW * i);
+                for (int i = 0; i < kGroup; ++i) {
+                    const unsigned long long at = (unsigned long long)(unsigned)row_of[slot % kHold][row_of_load(g + i)] * St::kRowBytes;
+                    k[i] = reinterpret_cast<const char*>(a.k) + key_piece(g + i) - 1024 * i + at;
+                    v[i] = reinterpret_cast<const char*>(a.v) + value_piece(g + i) - 1024 * i + at;
+                }
+                dma_group<kGroup>(k, k_to + 1024 * g);
+                dma_group<kGroup>(v, v_to + 1024 * g);
+            }
+        } else if (!rare(!a.kv_wide || it * kKv + kKv > seq.m)) {
+#pragma unroll
+            for (int g = 0; g < kLoads; g += kGroup) {
+                unsigned k[kGroup], v[kGroup];
+#pragma unroll
+                for (int i = 0; i < kGroup; ++i) { k[i] = k_off[g + i]; v[i] = v_off[g + i]; }
+                dma_group<kGroup>(k_next, k, k_to + 1024 * g);
+                dma_group<kGroup>(v_next, v, v_to + 1024 * g);
             }
         } else {                                               // rows past the last are read as the last
 #pragma unroll 1
             for (int i = 0; i < kLoads; ++i) {
                 const long long t = min(it * kKv + row_of_load(i), seq.m - 1);
-                const T* k = k_first + t * a.k_sn + key_piece(i) / (int)sizeof(T);
-                const T* v = v_first + t * a.v_sn + value_piece(i) / (int)sizeof(T);
-                const int at = 1024 * (i * kW + wave) + 16 * lane;
-                *reinterpret_cast<frag_t*>(&keys[kbuf][at]) = load_piece(k, a.kv_wide);
-                *reinterpret_cast<frag_t*>(&vals[vbuf][at]) = load_piece(v, a.kv_wide);
+                const int at = 1024 * (wave * kLoads + i) + 16 * lane;
+                *reinterpret_cast<frag_t*>(&keys[kbuf][at]) = load_piece(reinterpret_cast<const T*>(k_first + t * k_step + key_piece(i)), a.kv_wide);
+                *reinterpret_cast<frag_t*>(&vals[vbuf][at]) = load_piece(reinterpret_cast<const T*>(v_first + t * v_step + value_piece(i)), a.kv_wide);
             }
         }
+        k_next -= kKv * k_step;
+        v_next -= kKv * v_step;
     };
 
     // ---- the wave's state
@@ -560,7 +639,7 @@ __global__ __launch_bounds__(64 * kW, D == 128 && kQ == 2 ? 1 : 2) void prompt_k
         for (int i = 0; i < kOut; ++i) o[c][i] = zero_acc();
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[1][c][r] = -INFINITY;
-        p[0][c][0] = p[0][c][1] = zero_frag();
+        p[1][c][0] = p[1][c][1] = zero_frag();
         m[c] = -INFINITY; l[c] = 0.f;
     }
 #pragma unroll
@@ -581,9 +660,10 @@ __global__ __launch_bounds__(64 * kW, D == 128 && kQ == 2 ? 1 : 2) void prompt_k
     };
     constexpr bool kAcc = D == 128 && kQ == 2;
     const auto add_out = [&](f32x16_t& x, const frag_t& v, const frag_t& w) __attribute__((always_inline)) {
-        if constexpr (kAcc) asm("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(x) : "v"(v), "v"(w));
+        if constexpr (kAcc) asm("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(x) : "v"(v), "v"(w));
         else mma<T>(x, v, w);
     };
+    const auto settle_weights = [&]() __attribute__((always_inline)) { if constexpr (kAcc) asm volatile("s_nop 1" ::: "memory"); };
     const auto settle_out = [&]() __attribute__((always_inline)) {
         if constexpr (kAcc)
 #pragma unroll
@@ -656,18 +736,20 @@ __global__ __launch_bounds__(64 * kW, D == 128 && kQ == 2 ? 1 : 2) void prompt_k
     // The reference m stays where it is while the weights' sum has room: a row's weights are relative to it, and nothing is lost by
     // their size.  Else it goes up to the largest logit, and the step's weights are formed again.
     constexpr float kRoom = 0x1p30f;
+    const auto has_room = [&](float sum, int c) __attribute__((always_inline)) { return sum <= kRoom && m[c] > -INFINITY; };
     const auto raise = [&](const f32x16_t (&x)[kQ], frag_t (&w)[kQ][2], float (&sum)[kQ]) __attribute__((always_inline)) {
-        settle_out();
+        float shrink[kQ];
+        bool shrinks = false;
 #pragma unroll
         for (int c = 0; c < kQ; ++c) {
             float top = x[c][0];
 #pragma unroll
             for (int r = 1; r < 16; ++r) top = fmaxf(top, x[c][r]);
-            const float m_new = fmaxf(m[c], halves_max(top) * a.scale_log2e), ref = m_new > -INFINITY ? m_new : 0.f;
-            const float shrink = exp2_fast(m[c] - ref);
-            l[c] *= shrink;
-#pragma unroll
-            for (int i = 0; i < kOut; ++i) o[c][i] *= shrink;
+            top = fmaxf(m[c], halves_max(top) * a.scale_log2e);
+            const bool full = halves_max(has_room(sum[c], c) ? 0.f : 1.f) > 0.f;
+            const float m_new = full ? top : m[c], ref = m_new > -INFINITY ? m_new : 0.f;
+            shrink[c] = exp2_fast(m[c] - ref);                 // (what there is of a query without a reference is 0)
+            shrinks |= full && m[c] > -INFINITY;
             m[c] = m_new;
             sum[c] = 0.f;
 #pragma unroll
@@ -682,13 +764,35 @@ __global__ __launch_bounds__(64 * kW, D == 128 && kQ == 2 ? 1 : 2) void prompt_k
                 w[c][t] = __builtin_bit_cast(frag_t, y);
             }
         }
+        if (rare(__any(shrinks))) {
+            settle_out();
+#pragma unroll
+            for (int c = 0; c < kQ; ++c) {
+                const float f = m[c] > -INFINITY ? shrink[c] : 1.f;
+                l[c] *= f;
+#pragma unroll
+                for (int i = 0; i < kOut; ++i) o[c][i] *= f;
+            }
+        }
     };
 
     // One turn: the products of step n (keys at k_at) go to s[cur], the weights of step n - 1 come from s[1 - cur], the values of
     // step n - 2 are in vf, and those of step n - 1 (at v_at) take their place.
     constexpr int kPv = 2 * kOut * kQ, kQk = kFrags * kQ, kSlots = kPv + kQk, kElems = 16 * kQ;
+    const auto first_turn = [&](unsigned k_at) __attribute__((always_inline)) {              // products alone
+#pragma unroll
+        for (int f = 0; f < kFrags; ++f) {
+            const frag_t x = lds_frag((k_base + k_at) ^ (32 * f));
+#pragma unroll
+            for (int c = 0; c < kQ; ++c) {
+                if (f == 0) mma_first<T>(s[0][c], x, qf[c][f]);
+                else mma<T>(s[0][c], x, qf[c][f]);
+            }
+        }
+    };
     const auto turn = [&](auto cur_, unsigned k_at, unsigned v_at) __attribute__((always_inline)) {
         constexpr int cur = decltype(cur_)::value;
+        settle_weights();
         float sum[kQ], ref[kQ], y[kElems];
 #pragma unroll
         for (int c = 0; c < kQ; ++c) { sum[c] = 0.f; ref[c] = m[c] > -INFINITY ? m[c] : 0.f; }
@@ -720,7 +824,7 @@ __global__ __launch_bounds__(64 * kW, D == 128 && kQ == 2 ? 1 : 2) void prompt_k
             else mma<T>(s[cur][c], kf[f], qf[c][f]);
             constexpr int kV = 2 * kOut;
 #pragma unroll
-            for (int x = n * kV / kQk; x < (n + 1) * kV / kQk; ++x) vf[x / kOut][x % kOut] = value_frag(v_at, x / kOut, x % kOut);
+            for (int x = n; x < min(n + 1, kV); ++x) vf[x / kOut][x % kOut] = value_frag(v_at, x / kOut, x % kOut);
 #pragma unroll
             for (int e = (n + kPv) * kElems / kSlots; e < (n + kPv + 1) * kElems / kSlots; ++e) element(e);
             __builtin_amdgcn_sched_barrier(0);
@@ -729,7 +833,7 @@ __global__ __launch_bounds__(64 * kW, D == 128 && kQ == 2 ? 1 : 2) void prompt_k
         element(kElems + 1);
         bool room = true;
 #pragma unroll
-        for (int c = 0; c < kQ; ++c) room &= sum[c] <= kRoom && m[c] > -INFINITY;
+        for (int c = 0; c < kQ; ++c) room &= has_room(sum[c], c);
         if (rare(!__all(room))) raise(s[1 - cur], p[1 - cur], sum);
 #pragma unroll
         for (int c = 0; c < kQ; ++c) l[c] += sum[c];
@@ -754,6 +858,7 @@ __global__ __launch_bounds__(64 * kW, D == 128 && kQ == 2 ? 1 : 2) void prompt_k
     unsigned v_prev = v_lds;                                   // values of the step before (any, where there is none)
     if (hi > lo) load_stage(hi - 1, hi - 1 + kHold, 0, 0);
     const bool works = r0 < n_rows;
+    bool begun = false;
     int it = hi - 1;
     const auto stage = [&](auto top_) __attribute__((always_inline)) {
         constexpr bool kTop = decltype(top_)::value;           // some query may not see all of the rows at hand
@@ -777,7 +882,10 @@ __global__ __launch_bounds__(64 * kW, D == 128 && kQ == 2 ? 1 : 2) void prompt_k
                 const Step now{it * kKv + 32 * j, (unsigned)(live >> (32 * j)), it * kKv + 32 * j + 32 > lim_min};
                 if (rare((kTop && before.edge) || (kPaged && before.live != ~0u))) hide(j == 1 ? s[1] : s[0], before);
                 if constexpr (kTop) if (rare(old.edge)) take_out(old);
-                if (j == 1) turn(ic<0>{}, k_lds + kbuf * St::kBytes + 32 * St::kRowBytes, v_prev);
+                if (kTop && j == 1 && !begun) {
+                    first_turn(k_lds + kbuf * St::kBytes + 32 * St::kRowBytes);
+                    begun = true;
+                } else if (j == 1) turn(ic<0>{}, k_lds + kbuf * St::kBytes + 32 * St::kRowBytes, v_prev);
                 else turn(ic<1>{}, k_lds + kbuf * St::kBytes, v_prev);
                 v_prev = v_lds + vbuf * St::kBytes + 32 * j * St::kRowBytes;
                 old = before;
@@ -787,12 +895,13 @@ __global__ __launch_bounds__(64 * kW, D == 128 && kQ == 2 ? 1 : 2) void prompt_k
         kbuf ^= 1;
         vbuf = vnext;
     };
-    // stages that some query does not see whole, and one more for what is under way; then those that need no look at it
-    const int whole = lim_min / kKv - 1;
+    // the first stage and those that some query does not see whole, and one more for what is under way; then those that need no look
+    const int whole = min(lim_min / kKv, hi) - 1;
     for (; it >= lo && it >= whole; --it) stage(std::true_type{});
     for (; it >= lo; --it) stage(std::false_type{});
 
     // the last two steps' ends: weights of s[1], values of vf and of v_prev
+    if (begun) {
     if (before.edge || (kPaged && before.live != ~0u)) hide(s[1], before);
     if (old.edge) take_out(old);
 #pragma unroll
@@ -801,8 +910,9 @@ __global__ __launch_bounds__(64 * kW, D == 128 && kQ == 2 ? 1 : 2) void prompt_k
         for (int i = 0; i < kOut; ++i)
 #pragma unroll
             for (int c = 0; c < kQ; ++c) add_out(o[c][i], vf[t][i], p[0][c][t]);
-    if (hi > lo) {
         float sum[kQ];
+#pragma unroll
+        for (int c = 0; c < kQ; ++c) sum[c] = INFINITY;        // (the weights are formed here)
         raise(s[1], p[1], sum);
 #pragma unroll
         for (int c = 0; c < kQ; ++c) l[c] += sum[c];
@@ -824,10 +934,10 @@ __global__ __launch_bounds__(64 * kW, D == 128 && kQ == 2 ? 1 : 2) void prompt_k
 #pragma unroll
     for (int c = 0; c < kQ; ++c) {
         const float total = halves_sum(l[c]);
-        if (r0 + 32 * c + col >= n_rows) continue;
         const float ref = m[c] > -INFINITY ? m[c] : 0.f;
         const long long q_token = seq.q_first + token[c];
         if (a.splits > 1) {
+            if (r0 + 32 * c + col >= n_rows) continue;
             const long long at = (q_token * a.kv_heads * a.group + q_head[c]) * a.splits + split;
 #pragma unroll
             for (int i = 0; i < kOut; ++i)
@@ -839,14 +949,41 @@ __global__ __launch_bounds__(64 * kW, D == 128 && kQ == 2 ? 1 : 2) void prompt_k
         }
         const float inv = total == 0.f ? 0.f : 1.f / total;    // (NaN stays)
         T* out = reinterpret_cast<T*>(a.out) + q_head[c] * a.o_sh + (a.q_start ? q_token * a.o_sn : b * a.o_sb + token[c] * a.o_sn);
+        // eight neighbouring elements a lane: four of its own and the four that the lane 32 away has
+        frag_t pieces[kOut][2];
 #pragma unroll
         for (int i = 0; i < kOut; ++i)
 #pragma unroll
-            for (int r = 0; r < 16; r += 4)
-                store4(out + 32 * i + acc_row(r, half), o[c][i][r] * inv, o[c][i][r + 1] * inv, o[c][i][r + 2] * inv, o[c][i][r + 3] * inv, a.o_wide);
+            for (int q = 0; q < 2; ++q)
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    typedef bf16_t pair_t __attribute__((ext_vector_type(2)));
+                    const int r = 8 * q + 2 * x;
+                    const pair_t even{(bf16_t)(o[c][i][r] * inv), (bf16_t)(o[c][i][r + 1] * inv)};
+                    const pair_t odd{(bf16_t)(o[c][i][r + 4] * inv), (bf16_t)(o[c][i][r + 5] * inv)};
+                    const auto both = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, even), __builtin_bit_cast(unsigned, odd), false, false);
+                    pieces[i][q][x] = (int)both[0];
+                    pieces[i][q][2 + x] = (int)both[1];
+                }
+        if (r0 + 32 * c + col >= n_rows) continue;
+        out += 8 * half;
+        if (a.o_wide) {
+#pragma unroll
+            for (int i = 0; i < kOut; ++i)
+#pragma unroll
+                for (int q = 0; q < 2; ++q) *reinterpret_cast<frag_t*>(out + 32 * i + 16 * q) = pieces[i][q];
+        } else {
+#pragma unroll
+            for (int i = 0; i < kOut; ++i)
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    const bf16x8_t x = __builtin_bit_cast(bf16x8_t, pieces[i][q]);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) out[32 * i + 16 * q + e] = x[e];
+                }
+        }
         if (a.lse && half == 0) a.lse[(a.q_start ? q_token : b * a.l_sb + token[c]) + q_head[c] * a.l_sh] = (ref + log2_fast(total)) * 0.6931471805599453f;
-    }
-}
+    }}
 
 // ---- joining
 
