@@ -140,6 +140,14 @@ __device__ __forceinline__ void store4(T* p, float x0, float x1, float x2, float
 // A condition that hardly ever holds: what copies registers need go to its side.
 __device__ __forceinline__ bool rare(bool x) { return __builtin_expect_with_probability(x, 0, 0.9999); }
 
+constexpr int kMinusInf = (int)0xff800000;
+
+// Four bytes a lane from global memory to LDS; wait_vmem counts it.
+__device__ __forceinline__ void dma4(const void* from, unsigned lds)
+{
+    asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(scalar((int)lds)) : "memory", "m0");
+}
+
 // From global memory to LDS, a piece of 16 bytes a lane, from the wave's address on; wait_vmem counts it.
 __device__ __forceinline__ void dma16(const char* from, unsigned lds)
 {
@@ -490,7 +498,8 @@ __global__ __launch_bounds__(64 * kW, 2) void prompt_simple_kernel(PromptArgs a)
 // 16-bit rows.  A wave takes kQ tiles of 32 query rows (64 where there are many: every row of keys and values that it reads from
 // LDS goes into two products) and works on three steps of 32 rows at once, products of one beside the weights of another:
 //     S(n) = K(n) Q^T,   P(n - 1) = exp2(S(n - 1) - m),   O += V(n - 2)^T P(n - 2)^T
-template <int D, bool kPaged, int kQ, int kW>
+// kSome: rows of the cache are masked (by their positions); their logits begin at -inf.
+template <int D, bool kPaged, bool kSome, int kQ, int kW>
 __global__ __launch_bounds__(64 * kW, D == 128 && kQ == 2 ? 1 : 2) void prompt_kernel(PromptArgs a)
 {
     typedef bf16_t T;
@@ -498,11 +507,12 @@ __global__ __launch_bounds__(64 * kW, D == 128 && kQ == 2 ? 1 : 2) void prompt_k
     constexpr int kKv = St::kRows;
     constexpr int kFrags = Tile<T, D>::kFrags, kOut = D / 32;
     constexpr int kRowsOf = 32 * kQ * kW;
-    constexpr int kHold = 4;                                   // stages whose rows are known
+    constexpr int kBatch = 4, kHold = 2 * kBatch;              // stages whose rows are looked up together, and are known
     __shared__ __align__(1024) char keys[2][St::kBytes];
     __shared__ __align__(1024) char vals[3][St::kBytes];
     __shared__ int row_of[kPaged ? kHold : 1][kKv];
     __shared__ unsigned long long live_of[kPaged ? kHold : 1];
+    __shared__ int found[kPaged ? kBatch : 1][2][kWave];       // table elements and positions
 
     const int lane = threadIdx.x % kWave, wave = scalar((int)threadIdx.x / kWave);
     const int col = lane % 32, half = lane / 32;
@@ -536,26 +546,34 @@ __global__ __launch_bounds__(64 * kW, D == 128 && kQ == 2 ? 1 : 2) void prompt_k
         for (int f = 0; f < kFrags; ++f) qf[c][f] = load_piece(q + (2 * f + half) * 8, a.q_wide);
     }
 
-    // ---- rows of a stage
+    // ---- rows of a stage, found four stages at a time: a batch's stages are the waves', one after the other.  The trips of the
+    // batch below are made while one is worked on (the table; positions; then its rows are settled), from memory to LDS, so that
+    // no register waits for them: the loads of the stages are in flight behind them.
+    constexpr int kMine = kBatch / kW;
+    static_assert(kBatch % kW == 0, "every wave has as many");
     const auto page_of = [&](int t) __attribute__((always_inline)) { return (int)(__umulhi(2u * (unsigned)t, a.page_magic) >> a.page_shift); };
-    const auto table_trip = [&](int it) __attribute__((always_inline)) -> int {
-        const int t = it * kKv + lane;
-        return it >= lo && t < rows_end ? a.page_table[(size_t)b * a.max_pages + page_of(t)] : kNoRow;
-    };
-    const auto row_trip = [&](int it, int entry, int& mask) __attribute__((always_inline)) -> int {
-        const int t = it * kKv + lane;
-        mask = 0;
-        if (entry < 0 || entry >= a.num_pages) return kNoRow;
-        const int r = (entry * a.kv_heads + head - page_of(t)) * a.page_size + t;
-        if (a.pos_pages) mask = a.pos_pages[r];
-        return r;
-    };
-    const auto settle = [&](int slot, int r, int mask) __attribute__((always_inline)) {
-        if (mask < 0) r = kNoRow;
-        const unsigned long long live = __ballot(r != kNoRow);
-        const int spare = live ? __builtin_amdgcn_readlane(r, __builtin_ctzll(live)) : 0;
-        row_of[slot % kHold][lane] = r != kNoRow ? r : spare;
-        if (lane == 0) live_of[slot % kHold] = live;
+    const auto look_up = [&](int batch, int trip) __attribute__((always_inline)) {
+        if (batch < 0) return;
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            const int n = wave * kMine + i, it = batch * kBatch + n, t = min(it * kKv + lane, a.max_pages * a.page_size - 1), page = page_of(t);
+            if (trip == 0) {
+                dma_to_lds<4>(a.page_table + (size_t)b * a.max_pages, 4u * (unsigned)page, lds_address(&found[n][0][0]));
+                continue;
+            }
+            const int entry = found[n][0][lane];
+            int r = kNoRow;
+            if (it >= lo && it * kKv + lane < rows_end && entry >= 0 && entry < a.num_pages) r = (entry * a.kv_heads + head - page) * a.page_size + t;
+            if (trip == 1) {
+                if constexpr (kSome) dma4(a.pos_pages + max(r, 0), lds_address(&found[n][1][0]));
+                continue;
+            }
+            if (kSome && found[n][1][lane] < 0) r = kNoRow;
+            const unsigned long long live = __ballot(r != kNoRow);
+            const int spare = live ? __builtin_amdgcn_readlane(r, __builtin_ctzll(live)) : 0;
+            row_of[it % kHold][lane] = r != kNoRow ? r : spare;
+            if (lane == 0) live_of[it % kHold] = live;
+        }
     };
 
     const unsigned k_lds = lds_address(&keys[0][0]), v_lds = lds_address(&vals[0][0]);
@@ -582,10 +600,10 @@ __global__ __launch_bounds__(64 * kW, D == 128 && kQ == 2 ? 1 : 2) void prompt_k
             v_off[i] = (unsigned)row_of_load(i) * (unsigned)v_step + value_piece(i) + kDmaBias - 1024 * (i % kGroup);
         }
     }
-    const auto load_stage = [&](int it, int slot, int kbuf, int vbuf) __attribute__((always_inline)) {
+    const auto load_stage = [&](int it, int kbuf, int vbuf) __attribute__((always_inline)) {
         const unsigned k_to = scalar((int)(k_lds + kbuf * St::kBytes)) + 1024 * kLoads * wave, v_to = scalar((int)(v_lds + vbuf * St::kBytes)) + 1024 * kLoads * wave;
         if constexpr (kPaged) {
-            if (live_of[slot % kHold] == 0) {                  // nothing there: zeros, which count nothing
+            if (live_of[it % kHold] == 0) {                  // nothing there: zeros, which count nothing
 #pragma unroll
                 for (int i = 0; i < kLoads; ++i) {
                     const int at = 1024 * (wave * kLoads + i) + 16 * lane;
@@ -599,7 +617,7 @@ __global__ __launch_bounds__(64 * kW, D == 128 && kQ == 2 ? 1 : 2) void prompt_k
                 const char *k[kGroup], *v[kGroup];
 #pragma unroll
                 for (int i = 0; i < kGroup; ++i) {
-                    const unsigned long long at = (unsigned long long)(unsigned)row_of[slot % kHold][row_of_load(g + i)] * St::kRowBytes;
+                    const unsigned long long at = (unsigned long long)(unsigned)row_of[it % kHold][row_of_load(g + i)] * St::kRowBytes;
                     k[i] = reinterpret_cast<const char*>(a.k) + key_piece(g + i) - 1024 * i + at;
                     v[i] = reinterpret_cast<const char*>(a.v) + value_piece(g + i) - 1024 * i + at;
                 }
@@ -615,13 +633,26 @@ __global__ __launch_bounds__(64 * kW, D == 128 && kQ == 2 ? 1 : 2) void prompt_k
                 dma_group<kGroup>(k_next, k, k_to + 1024 * g);
                 dma_group<kGroup>(v_next, v, v_to + 1024 * g);
             }
-        } else {                                               // rows past the last are read as the last
-#pragma unroll 1
+        } else if (a.kv_wide) {                                // rows past the last are read as the last
+#pragma unroll
+            for (int g = 0; g < kLoads; g += kGroup) {
+                const char *k[kGroup], *v[kGroup];
+#pragma unroll
+                for (int i = 0; i < kGroup; ++i) {
+                    const unsigned t = min(it * kKv + row_of_load(g + i), seq.m - 1);
+                    k[i] = k_first + t * (unsigned long long)(unsigned)k_step + key_piece(g + i) - 1024 * i;
+                    v[i] = v_first + t * (unsigned long long)(unsigned)v_step + value_piece(g + i) - 1024 * i;
+                }
+                dma_group<kGroup>(k, k_to + 1024 * g);
+                dma_group<kGroup>(v, v_to + 1024 * g);
+            }
+        } else {
+#pragma unroll 4
             for (int i = 0; i < kLoads; ++i) {
                 const long long t = min(it * kKv + row_of_load(i), seq.m - 1);
                 const int at = 1024 * (wave * kLoads + i) + 16 * lane;
-                *reinterpret_cast<frag_t*>(&keys[kbuf][at]) = load_piece(reinterpret_cast<const T*>(k_first + t * k_step + key_piece(i)), a.kv_wide);
-                *reinterpret_cast<frag_t*>(&vals[vbuf][at]) = load_piece(reinterpret_cast<const T*>(v_first + t * v_step + value_piece(i)), a.kv_wide);
+                *reinterpret_cast<frag_t*>(&keys[kbuf][at]) = load_piece(reinterpret_cast<const T*>(k_first + t * k_step + key_piece(i)), false);
+                *reinterpret_cast<frag_t*>(&vals[vbuf][at]) = load_piece(reinterpret_cast<const T*>(v_first + t * v_step + value_piece(i)), false);
             }
         }
         k_next -= kKv * k_step;
@@ -646,8 +677,9 @@ __global__ __launch_bounds__(64 * kW, D == 128 && kQ == 2 ? 1 : 2) void prompt_k
     for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int i = 0; i < kOut; ++i) vf[t][i] = zero_frag();
-    struct Step { int row; unsigned live; bool edge; };        // first row; rows that are there; some query does not see all of them
-    Step before{0, 0, true}, old{0, 0, false};                 // of s[1 - cur] and of vf: first of none, with values that are anything
+    // first row; rows that are there; some query does not see all of them; logits are to be hidden yet
+    struct Step { int row; unsigned live; bool edge, shown; };
+    Step before{0, 0, true, false}, old{0, 0, false, false};   // of s[1 - cur] and of vf: first of none, with values that are anything
 
     const unsigned k_base = col * St::kRowBytes + 16 * (half ^ St::key(col));
     const int v_row = 4 * half + lane % 16 / 4;
@@ -680,7 +712,10 @@ __global__ __launch_bounds__(64 * kW, D == 128 && kQ == 2 ? 1 : 2) void prompt_k
         for (int c = 0; c < kQ; ++c) {
             const unsigned bits = seen(st, c);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) x[c][r] = (bits >> acc_row(r, 0)) & 1 ? x[c][r] : -INFINITY;
+            for (int r = 0; r < 16; ++r) {
+                const int keep = __builtin_amdgcn_sbfe(bits, acc_row(r, 0), 1);
+                x[c][r] = __int_as_float((__float_as_int(x[c][r]) & keep) | (kMinusInf & ~keep));
+            }
         }
     };
     // Where some query does not see a row, the row's value counts 0 times: an infinity or NaN there must not.  It is taken out of
@@ -779,19 +814,30 @@ __global__ __launch_bounds__(64 * kW, D == 128 && kQ == 2 ? 1 : 2) void prompt_k
     // One turn: the products of step n (keys at k_at) go to s[cur], the weights of step n - 1 come from s[1 - cur], the values of
     // step n - 2 are in vf, and those of step n - 1 (at v_at) take their place.
     constexpr int kPv = 2 * kOut * kQ, kQk = kFrags * kQ, kSlots = kPv + kQk, kElems = 16 * kQ;
-    const auto first_turn = [&](unsigned k_at) __attribute__((always_inline)) {              // products alone
+    const auto begin = [&](f32x16_t (&x)[kQ], unsigned live) __attribute__((always_inline)) {
+        const unsigned gone = ~live >> (4 * half);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const float y = __int_as_float(__builtin_amdgcn_sbfe(gone, acc_row(r, 0), 1) & kMinusInf);
+#pragma unroll
+            for (int c = 0; c < kQ; ++c) x[c][r] = y;
+        }
+    };
+    const auto first_turn = [&](unsigned live, unsigned k_at) __attribute__((always_inline)) {              // products alone
+        if constexpr (kSome) begin(s[0], live);
 #pragma unroll
         for (int f = 0; f < kFrags; ++f) {
             const frag_t x = lds_frag((k_base + k_at) ^ (32 * f));
 #pragma unroll
             for (int c = 0; c < kQ; ++c) {
-                if (f == 0) mma_first<T>(s[0][c], x, qf[c][f]);
+                if (f == 0 && !kSome) mma_first<T>(s[0][c], x, qf[c][f]);
                 else mma<T>(s[0][c], x, qf[c][f]);
             }
         }
     };
-    const auto turn = [&](auto cur_, unsigned k_at, unsigned v_at) __attribute__((always_inline)) {
+    const auto turn = [&](auto cur_, unsigned live, unsigned k_at, unsigned v_at) __attribute__((always_inline)) {
         constexpr int cur = decltype(cur_)::value;
+        if constexpr (kSome) begin(s[cur], live);
         settle_weights();
         float sum[kQ], ref[kQ], y[kElems];
 #pragma unroll
@@ -820,7 +866,7 @@ __global__ __launch_bounds__(64 * kW, D == 128 && kQ == 2 ? 1 : 2) void prompt_k
 #pragma unroll
         for (int n = 0; n < kQk; ++n) {
             const int f = n / kQ, c = n % kQ;
-            if (f == 0) mma_first<T>(s[cur][c], kf[f], qf[c][f]);
+            if (f == 0 && !kSome) mma_first<T>(s[cur][c], kf[f], qf[c][f]);
             else mma<T>(s[cur][c], kf[f], qf[c][f]);
             constexpr int kV = 2 * kOut;
 #pragma unroll
@@ -840,53 +886,55 @@ __global__ __launch_bounds__(64 * kW, D == 128 && kQ == 2 ? 1 : 2) void prompt_k
     };
 
     // Stages come last rows first.  One is in flight while one is worked on; rows of pages are looked up two further on.
-    int entry = kNoRow, far = kNoRow, far_mask = 0;
+    const int first_batch = (hi - 1) / kBatch;
     if constexpr (kPaged) {
-        if (wave == 0 && hi > lo) {
+        if (hi > lo) {
 #pragma unroll
-            for (int i = 1; i <= 2; ++i) {
-                int mask;
-                const int r = row_trip(hi - i, table_trip(hi - i), mask);
-                settle(hi - i + kHold, r, mask);               // (hi - 2 may be -1)
-            }
-            far = row_trip(hi - 3, table_trip(hi - 3), far_mask);
-            entry = table_trip(hi - 4);
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int trip = 0; trip < 3; ++trip) {
+                    look_up(first_batch - i, trip);
+                    wait_vmem<0>();
+                }
         }
         __syncthreads();
     }
     int kbuf = 0, vbuf = 0;
     unsigned v_prev = v_lds;                                   // values of the step before (any, where there is none)
-    if (hi > lo) load_stage(hi - 1, hi - 1 + kHold, 0, 0);
+    if (hi > lo) load_stage(hi - 1, 0, 0);
     const bool works = r0 < n_rows;
     bool begun = false;
     int it = hi - 1;
     const auto stage = [&](auto top_) __attribute__((always_inline)) {
         constexpr bool kTop = decltype(top_)::value;           // some query may not see all of the rows at hand
-        wait_vmem_all_visible();
+        wait_vmem<0>();
         __syncthreads();
         const int vnext = vbuf == 2 ? 0 : vbuf + 1;
-        if (it > lo) load_stage(it - 1, it - 1 + kHold, kbuf ^ 1, vnext);
+        if (it > lo) load_stage(it - 1, kbuf ^ 1, vnext);
         unsigned long long live = ~0ull;
         if constexpr (kPaged) {
             live = live_of[it % kHold];
             live = ((unsigned long long)(unsigned)scalar((int)(live >> 32)) << 32) | (unsigned)scalar((int)live);
-            if (wave == 0) {
-                settle(it - 2 + kHold, far, far_mask);
-                far = row_trip(it - 3, entry, far_mask);
-                entry = table_trip(it - 4);
+            if (it / kBatch < first_batch) {
+                const int trip = kBatch - 1 - it % kBatch;
+                if (trip == 0) look_up(it / kBatch - 1, 0);
+                else if (trip == 1) look_up(it / kBatch - 1, 1);
+                else if (trip == 2) look_up(it / kBatch - 1, 2);
             }
         }
         if (works && (!kTop || it * kKv < lim_max)) {
 #pragma unroll
             for (int j = 1; j >= 0; --j) {
-                const Step now{it * kKv + 32 * j, (unsigned)(live >> (32 * j)), it * kKv + 32 * j + 32 > lim_min};
-                if (rare((kTop && before.edge) || (kPaged && before.live != ~0u))) hide(j == 1 ? s[1] : s[0], before);
+                const unsigned here = (unsigned)(live >> (32 * j)), k_at = k_lds + kbuf * St::kBytes + 32 * j * St::kRowBytes;
+                const bool edge = kTop && it * kKv + 32 * j + 32 > lim_min;
+                const Step now{it * kKv + 32 * j, here, edge, edge || (kPaged && !kSome && here != ~0u)};
+                if (rare(before.shown)) hide(j == 1 ? s[1] : s[0], before);
                 if constexpr (kTop) if (rare(old.edge)) take_out(old);
                 if (kTop && j == 1 && !begun) {
-                    first_turn(k_lds + kbuf * St::kBytes + 32 * St::kRowBytes);
+                    first_turn(here, k_at);
                     begun = true;
-                } else if (j == 1) turn(ic<0>{}, k_lds + kbuf * St::kBytes + 32 * St::kRowBytes, v_prev);
-                else turn(ic<1>{}, k_lds + kbuf * St::kBytes, v_prev);
+                } else if (j == 1) turn(ic<0>{}, here, k_at, v_prev);
+                else turn(ic<1>{}, here, k_at, v_prev);
                 v_prev = v_lds + vbuf * St::kBytes + 32 * j * St::kRowBytes;
                 old = before;
                 before = now;
@@ -902,7 +950,7 @@ __global__ __launch_bounds__(64 * kW, D == 128 && kQ == 2 ? 1 : 2) void prompt_k
 
     // the last two steps' ends: weights of s[1], values of vf and of v_prev
     if (begun) {
-    if (before.edge || (kPaged && before.live != ~0u)) hide(s[1], before);
+    if (before.shown) hide(s[1], before);
     if (old.edge) take_out(old);
 #pragma unroll
     for (int t = 0; t < 2; ++t)
@@ -1044,11 +1092,20 @@ PromptPlan plan_prompt(long long sequences, long long rows, long long all_rows, 
     p.tiles = blocks(p.waves) / kv_heads;
     p.splits = 1;
     const long long n = blocks(p.waves);
-    if (n < 512 && most >= 1024) p.splits = (int)std::min({(512 + n - 1) / n, most / 512, 64ll});
+    if (n < 256 && most >= 1024) p.splits = (int)std::min({(512 + n - 1) / n, most / 512, 64ll});
     return p;
 }
 
 namespace {
+template <int D, bool kPaged, bool kSome>
+void launch_tiles(const PromptArgs& a, int waves, dim3 grid, hipStream_t st)
+{
+    if (waves == 8) prompt_kernel<D, kPaged, kSome, 2, 4><<<grid, 256, 0, st>>>(a);
+    else if (waves == 4) prompt_kernel<D, kPaged, kSome, 1, 4><<<grid, 256, 0, st>>>(a);
+    else if (waves == 2) prompt_kernel<D, kPaged, kSome, 1, 2><<<grid, 128, 0, st>>>(a);
+    else prompt_kernel<D, kPaged, kSome, 1, 1><<<grid, 64, 0, st>>>(a);
+}
+
 template <typename T, int D, bool kPaged>
 hipError_t launch(PromptArgs a, const PromptPlan& plan, hipStream_t st)
 {
@@ -1058,10 +1115,8 @@ hipError_t launch(PromptArgs a, const PromptPlan& plan, hipStream_t st)
     a.splits = plan.splits;
     const dim3 grid((unsigned)(plan.tiles * a.kv_heads), plan.splits);
     if constexpr (sizeof(T) == 2) {
-        if (plan.waves == 8) prompt_kernel<D, kPaged, 2, 4><<<grid, 256, 0, st>>>(a);
-        else if (plan.waves == 4) prompt_kernel<D, kPaged, 1, 4><<<grid, 256, 0, st>>>(a);
-        else if (plan.waves == 2) prompt_kernel<D, kPaged, 1, 2><<<grid, 128, 0, st>>>(a);
-        else prompt_kernel<D, kPaged, 1, 1><<<grid, 64, 0, st>>>(a);
+        if (kPaged && a.pos_pages) launch_tiles<D, kPaged, kPaged>(a, plan.waves, grid, st);
+        else launch_tiles<D, kPaged, false>(a, plan.waves, grid, st);
     } else {
         if (plan.waves == 8) prompt_simple_kernel<T, D, kPaged, 8><<<grid, 512, 0, st>>>(a);
         else if (plan.waves == 4) prompt_simple_kernel<T, D, kPaged, 4><<<grid, 256, 0, st>>>(a);
