@@ -36,9 +36,16 @@ static_assert(kUnit == kWaves * kLook, "a turn");
 
 template <typename T, int D> constexpr int kRowBytesOf = D * (int)sizeof(T);
 
+// New tokens of a sequence (kMany: a q-head of a token is a column; else there is one, and it has them all).
+__device__ __forceinline__ int fresh_tokens(const AttendArgs& a, int b)
+{
+    return a.new_len ? min(max(a.new_len[b], 0), a.tokens) : a.tokens;
+}
+
 __device__ __forceinline__ int live_len(const AttendArgs& a, bool table, int b)
 {
     if (table) return a.n_tok + 1;
+    if (a.new_len && a.new_len[b] <= 0) return 0;
     const long long most = (long long)a.max_pages * a.page_size;
     return (int)min((long long)max(a.lens[b], 0), most);
 }
@@ -137,7 +144,10 @@ __device__ __forceinline__ float column_reduce(float v)
 
 // T: queries and output, C: keys and values (T, or the bytes of a cache in 8 bits, whose numbers become bf16 as they go into the
 // products, the row's power of two with them).
-template <typename T, typename C, int D, bool kTable, int kW, bool kPast, int kQt, bool kSparse>
+//
+// kMany: several new tokens a sequence, the q-heads of each side by side in the columns (a.group of them): a column's token
+// sees rows up to its own.
+template <typename T, typename C, int D, bool kTable, int kW, bool kPast, int kQt, bool kSparse, bool kMany = false>
 __global__ __launch_bounds__(64 * kW, (kQt == 2 ? 2 : kW == 4 ? 3 : kW / 4)) void attend_kernel(AttendArgs a)
 {
     constexpr int kTurn = kW * kLook;                          // rows of a block's turn
@@ -177,6 +187,7 @@ __global__ __launch_bounds__(64 * kW, (kQt == 2 ? 2 : kW == 4 ? 3 : kW / 4)) voi
 
     for (;;) {
         const int first = u - base;
+        const int fresh = kMany ? fresh_tokens(a, b) : 1;
         const int unit = b * a.kv_heads + head;
         const size_t q_head = (size_t)unit * a.group + q0;                          // = b * Hq + head * group + q0
 
@@ -185,11 +196,13 @@ __global__ __launch_bounds__(64 * kW, (kQt == 2 ? 2 : kW == 4 ? 3 : kW / 4)) voi
 #pragma unroll
         for (int j = 0; j < kQt; ++j) {
             const int qi = kAttendQ * j + col;
-            const T* q = reinterpret_cast<const T*>(a.q) + b * a.q_sb + (long long)(head * a.group + q0 + qi) * a.q_sh;
+            const int token = kMany ? (q0 + qi) / a.heads : 0;
+            const T* q = reinterpret_cast<const T*>(a.q) + b * a.q_sb + (kMany ? (long long)(head * a.heads + q0 + qi - token * a.heads) * a.q_sh + token * a.q_sn
+                                                                              : (long long)(head * a.group + q0 + qi) * a.q_sh);
 #pragma unroll
             for (int c = 0; c < kPieces; ++c) {
                 qf[j][c] = zero_frag();
-                if (qi < n_q) {
+                if (qi < n_q && token < fresh) {
                     const T* at = q + (k8 ? 64 * (c / 2) + 16 * quad + 8 * (c % 2) : (4 * c + quad) * (16 / (int)sizeof(T)));
                     if (a.q_wide) qf[j][c] = *reinterpret_cast<const frag_t*>(at);
                     else {
@@ -288,8 +301,66 @@ __global__ __launch_bounds__(64 * kW, (kQt == 2 ? 2 : kW == 4 ? 3 : kW / 4)) voi
                     for (int h = 0; h < kParts; ++h) vf[i][r][h] = read<kPast>(reinterpret_cast<const vec_t*>(p + 256 * h));
                 }
         };
+        // Values of rows that some column does not see count 0 times there: infinities and NaN among them (hardly ever) are taken out of
+        // the products, and a product of their own says which columns see one.
+        const auto take_out = [&](const unsigned (&seen)[kQt]) {
+            bool odd = false;
+#pragma unroll
+            for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int h = 0; h < kParts; ++h)
+#pragma unroll
+                        for (int d = 0; d < kVec; ++d) {
+                            const unsigned x = (unsigned)vf[i][r][h][d];
+                            if constexpr (sizeof(T) == 2) odd |= (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u;
+                            else odd |= (x & 0x7f800000u) == 0x7f800000u;
+                        }
+            if (!__any(odd)) return;
+            const auto not_finite = [&](int row, int e) -> bool {        // of the lane's rows, output tile e
+                const unsigned x = (unsigned)(sizeof(T) == 2 ? vf[row / 4][row % 4][0][e / 2] : vf[row / 4][row % 4][e / 4][e % 4]);
+                return sizeof(T) == 2 ? ((e % 2 ? x >> 16 : x) & 0x7f80u) == 0x7f80u : (x & 0x7f800000u) == 0x7f800000u;
+            };
+#pragma unroll
+            for (int e = 0; e < kOut; ++e)
+#pragma unroll
+                for (int j = 0; j < kQt; ++j) {
+                    f32x4_t count = {0.f, 0.f, 0.f, 0.f};
+                    if constexpr (sizeof(T) == 2) {
+                        bf16x8_t x, y;
+#pragma unroll
+                        for (int r = 0; r < 8; ++r) {
+                            x[r] = (bf16_t)(not_finite(r, e) ? 1.f : 0.f);
+                            y[r] = (bf16_t)((seen[j] >> (16 * (r / 4) + r % 4)) & 1 ? 1.f : 0.f);
+                        }
+                        count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, count, 0, 0, 0);
+                    } else {
+#pragma unroll
+                        for (int r = 0; r < 4 * kTiles; ++r)
+                            count = __builtin_amdgcn_mfma_f32_16x16x4f32(not_finite(r, e) ? 1.f : 0.f, (seen[j] >> (16 * (r / 4) + r % 4)) & 1 ? 1.f : 0.f, count, 0, 0, 0);
+                    }
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) o[j][e][r] = count[r] > 0.f ? NAN : o[j][e][r];
+                }
+#pragma unroll
+            for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int h = 0; h < kParts; ++h)
+#pragma unroll
+                        for (int d = 0; d < kVec; ++d) {
+                            unsigned x = (unsigned)vf[i][r][h][d];
+                            if constexpr (sizeof(T) == 2) {
+                                if ((x & 0x7f80u) == 0x7f80u) x &= 0xffff0000u;
+                                if ((x & 0x7f800000u) == 0x7f800000u) x &= 0xffffu;
+                            } else if ((x & 0x7f800000u) == 0x7f800000u) x = 0;
+                            vf[i][r][h][d] = (int)x;
+                        }
+        };
         // one step on the rows in kf and vf, which the rows of (next_buf, next_at) then take
-        const auto step = [&](unsigned live, int buf, int at, int next_buf, int next_at) {
+        const auto step = [&](unsigned live, int buf, int at, int next_buf, int next_at, int row = 0) {
             live = uniform((int)(kTiles == 2 ? live : live & 0xffff));
             f32x4_t s[kQt][kTiles];
 #pragma unroll
@@ -317,7 +388,18 @@ __global__ __launch_bounds__(64 * kW, (kQt == 2 ? 2 : kW == 4 ? 3 : kW / 4)) voi
             __builtin_amdgcn_sched_barrier(0);
             if (live) {                                        // (row 0 may hold anything)
                 // logits in units of ln 2, dead rows -inf whatever their products are
-                live >>= 4 * quad;
+                const bool edge = kMany && row + kStep > len - fresh + 1;       // some column does not see all of the rows
+                unsigned seen[kQt];                            // rows 16 i + 4 quad + r, bit 16 i + r
+#pragma unroll
+                for (int j = 0; j < kQt; ++j) {
+                    seen[j] = live;
+                    if (edge) {
+                        const int left = len - fresh + 1 + (q0 + kAttendQ * j + col) / a.heads - row;
+                        seen[j] &= left >= 32 ? ~0u : left <= 0 ? 0u : (1u << left) - 1;
+                    }
+                    seen[j] >>= 4 * quad;
+                }
+                if constexpr (kMany) if (edge) take_out(seen);
                 f32x4_t f[kTiles];
 #pragma unroll
                 for (int i = 0; i < kTiles; ++i) {
@@ -331,7 +413,7 @@ __global__ __launch_bounds__(64 * kW, (kQt == 2 ? 2 : kW == 4 ? 3 : kW / 4)) voi
                     for (int i = 0; i < kTiles; ++i)
 #pragma unroll
                         for (int r = 0; r < 4; ++r) {
-                            s[j][i][r] = (live >> (16 * i + r)) & 1 ? s[j][i][r] * f[i][r] : -INFINITY;
+                            s[j][i][r] = (seen[j] >> (16 * i + r)) & 1 ? s[j][i][r] * f[i][r] : -INFINITY;
                             top = fmaxf(top, s[j][i][r]);
                         }
                     const float m_new = fmaxf(m[j], column_reduce<true>(top));
@@ -473,7 +555,7 @@ __global__ __launch_bounds__(64 * kW, (kQt == 2 ? 2 : kW == 4 ? 3 : kW / 4)) voi
                     live = settle(t, next, 1 - buf);
                     t += kTurn;
                 }
-                step(now, buf, at, turn ? 1 - buf : buf, turn ? 0 : at + 1);
+                step(now, buf, at, turn ? 1 - buf : buf, turn ? 0 : at + 1, t_first - lane % kLook + i / kSteps * kTurn + kStep * at);
             }
         }
 #pragma unroll
@@ -517,10 +599,13 @@ __global__ __launch_bounds__(64 * kW, (kQt == 2 ? 2 : kW == 4 ? 3 : kW / 4)) voi
                 }
                 if (whole) {
                     const float inv = sum == 0.f ? 0.f : 1.f / sum;                     // (NaN stays)
-                    T* out = reinterpret_cast<T*>(a.out) + (q_head + q) * D + d;
+                    const int token = kMany ? (q0 + q) / a.heads : 0;
+                    if (token >= fresh) continue;
+                    const long long h = head * a.heads + q0 + q - token * a.heads;
+                    T* out = reinterpret_cast<T*>(a.out) + (kMany ? b * a.o_sb + h * a.o_sh + token * a.o_sn : (q_head + q) * D) + d;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) out[e] = (T)(x[e] * inv);
-                    if (a.lse && d == 0) a.lse[q_head + q] = (ref + log2_fast(sum)) * 0.6931471805599453f;
+                    if (a.lse && d == 0) a.lse[kMany ? b * a.l_sb + h * a.l_sh + token : q_head + q] = (ref + log2_fast(sum)) * 0.6931471805599453f;
                 } else {
                     const size_t at = ((((size_t)(q0 + q) / kAttendQ * a.kv_heads + head) * a.workers + worker) * 2 + (first == 0)) * kAttendQ + q % kAttendQ;
                     *reinterpret_cast<f32x4_t*>(a.part_o + at * D + d) = x;
@@ -537,7 +622,7 @@ __global__ __launch_bounds__(64 * kW, (kQt == 2 ? 2 : kW == 4 ? 3 : kW / 4)) voi
 }
 
 // A block takes join_q q-heads of a sequence; D / 4 lanes take a q-head's columns, and lanes that are left share its workers.
-template <typename T, int D, bool kTable>
+template <typename T, int D, bool kTable, bool kMany>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a)
 {
     constexpr int kLanes = D / 4, kSlots = 256 / kLanes, kAhead = 4;
@@ -546,10 +631,17 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a)
     const int b = blockIdx.x, head = blockIdx.y, q0 = blockIdx.z * a.join_q;                   // q0: of the group
     const int len = live_len(a, kTable, b);
     const size_t q_head = ((size_t)b * a.kv_heads + head) * a.group + q0;
-    T* out = reinterpret_cast<T*>(a.out) + q_head * D;
+    const int fresh = kMany ? fresh_tokens(a, b) : 1;
+    // element c of the block's q-head (column) i, if there is such a token
+    const auto put = [&](int i, int c, float x, float lse) {
+        const int token = kMany ? (q0 + i) / a.heads : 0;
+        if (token >= fresh) return;
+        const long long h = head * a.heads + q0 + i - token * a.heads;
+        reinterpret_cast<T*>(a.out)[kMany ? b * a.o_sb + h * a.o_sh + token * a.o_sn + c : (long long)(q_head + i) * D + c] = (T)x;
+        if (a.lse && c == 0) a.lse[kMany ? b * a.l_sb + h * a.l_sh + token : q_head + i] = lse;
+    };
     if (len == 0) {
-        for (int i = threadIdx.x; i < a.join_q * D; i += 256) out[i] = (T)0.f;
-        if (a.lse && (int)threadIdx.x < a.join_q) a.lse[q_head + threadIdx.x] = -INFINITY;
+        for (int i = threadIdx.x; i < a.join_q * D; i += 256) put(i / D, i % D, 0.f, -INFINITY);
         return;
     }
     const Units units = count_units(a, kTable, b);
@@ -606,8 +698,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a)
             sum += f * red_ml[s0 + g][1];
             y += f * red_o[s0 + g][c];
         }
-        out[i] = (T)(y * (sum == 0.f ? 0.f : 1.f / sum));
-        if (a.lse && c == 0) a.lse[q_head + i / D] = (ref + log2_fast(sum)) * 0.6931471805599453f;
+        put(i / D, c, y * (sum == 0.f ? 0.f : 1.f / sum), (ref + log2_fast(sum)) * 0.6931471805599453f);
     }
 }
 
@@ -633,7 +724,7 @@ int attend_workers(int batch, int kv_heads, int group, long long max_len, int ro
 }
 
 namespace {
-template <typename T, typename C, int D, bool kTable>
+template <typename T, typename C, int D, bool kTable, bool kMany = false>
 hipError_t launch(AttendArgs a, hipStream_t st)
 {
     a.page_shift = 0;
@@ -664,7 +755,12 @@ hipError_t launch(AttendArgs a, hipStream_t st)
     // A block per sequence has eight waves (or 16, as the registers allow) where it would need several turns of four, and
     // there is less than two blocks' work for a compute unit (us at 8 heads of 128 and 512 rows, eight waves / four:
     // 16 sequences 11.5 / 12.4, 32 15.2 / 15.8, 64 29.7 / 27.5, 128 56.6 / 50.4).
-    if (a.group > kAttendQ) {
+    if constexpr (kMany) {
+        if (a.group > kAttendQ && past) attend_kernel<T, C, D, kTable, kWaves, true, 2, false, true><<<grid, 256, 0, st>>>(a);
+        else if (a.group > kAttendQ) attend_kernel<T, C, D, kTable, kWaves, false, 2, false, true><<<grid, 256, 0, st>>>(a);
+        else if (past) attend_kernel<T, C, D, kTable, kWaves, true, 1, false, true><<<grid, 256, 0, st>>>(a);
+        else attend_kernel<T, C, D, kTable, kWaves, false, 1, false, true><<<grid, 256, 0, st>>>(a);
+    } else if (a.group > kAttendQ) {
         if (past && a.pos_pages) attend_kernel<T, C, D, kTable, kWaves, !kTable, 2, !kTable><<<grid, 256, 0, st>>>(a);
         else if (past) attend_kernel<T, C, D, kTable, kWaves, !kTable, 2, false><<<grid, 256, 0, st>>>(a);
         else attend_kernel<T, C, D, kTable, kWaves, false, 2, false><<<grid, 256, 0, st>>>(a);
@@ -679,7 +775,7 @@ hipError_t launch(AttendArgs a, hipStream_t st)
     }
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && a.workers) {
-        attend_join_kernel<T, D, kTable><<<dim3(a.batch, a.kv_heads, a.group / a.join_q), 256, 0, st>>>(a);
+        attend_join_kernel<T, D, kTable, kMany><<<dim3(a.batch, a.kv_heads, a.group / a.join_q), 256, 0, st>>>(a);
         e = hipGetLastError();
     }
     return e;
@@ -687,6 +783,7 @@ hipError_t launch(AttendArgs a, hipStream_t st)
 template <typename T>
 hipError_t launch_rows(const AttendArgs& a, hipStream_t st)
 {
+    if (a.many) return a.head_dim == 64 ? launch<T, T, 64, false, true>(a, st) : launch<T, T, 128, false, true>(a, st);
     if (a.page_table) return a.head_dim == 64 ? launch<T, T, 64, false>(a, st) : launch<T, T, 128, false>(a, st);
     return a.head_dim == 64 ? launch<T, T, 64, true>(a, st) : launch<T, T, 128, true>(a, st);
 }

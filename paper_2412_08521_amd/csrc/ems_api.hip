@@ -3,6 +3,7 @@
 #include "../../include/ems.h"
 #include "ems_kernels.h"
 
+#include <algorithm>
 #include <cmath>
 #include <mutex>
 
@@ -618,6 +619,7 @@ static AttendPlan plan_attend(int batch, int kv_heads, int group, int head_dim, 
 
 static int attend(ems::AttendArgs& a, const AttendPlan& plan, bool f32, void* ws, size_t ws_bytes, void* hip_stream)
 {
+    if (!a.many) { a.tokens = 1; a.heads = a.group; }
     if (plan.total && !ws_ok(ws, ws_bytes, plan.total)) return EMS_ERR_WORKSPACE;
     a.workers = plan.workers;
     a.part_o = static_cast<float*>(ws);
@@ -903,6 +905,20 @@ static int many_queries(ems::PromptArgs& a, const PromptSizes& s, int head_dim, 
 // Blocks of a launch: less than 2^32 threads in x.
 static bool prompt_grid_ok(const ems::PromptPlan& plan, int kv_heads) { return plan.tiles * kv_heads * plan.waves < (1ll << 26); }
 
+// Few columns (new tokens x q-heads of a kv-head) go by the kernel of single tokens, whose products have 32 of them at most.
+constexpr int kFewColumns = 2 * ems::kAttendQ;
+static bool few_columns(const ems_paged_params* p, int32_t n_new)
+{
+    const int group = p->q_heads / p->kv_heads;
+    return n_new <= kFewColumns / group && attend_grid_ok(p->batch, p->q_heads * n_new, (long long)p->max_pages * p->page_size);
+}
+
+static AttendPlan plan_few(const ems_paged_params* p, int32_t n_new)
+{
+    return plan_attend(p->batch, p->kv_heads, p->q_heads / p->kv_heads * n_new, p->head_dim, (long long)p->max_pages * p->page_size,
+                       p->head_dim * (p->dtype == EMS_F32 ? 4 : 2));
+}
+
 static bool chunk_params_ok(const ems_paged_params* p, int32_t n_new, PromptSizes* s, int* why)
 {
     if (!paged_params_ok(p, why)) return false;
@@ -911,7 +927,8 @@ static bool chunk_params_ok(const ems_paged_params* p, int32_t n_new, PromptSize
     *why = EMS_ERR_UNSUPPORTED;
     if ((long long)p->batch * n_new > 0x7fffffffll / p->q_heads) return false;
     const long long rows = (long long)n_new * (p->q_heads / p->kv_heads), tokens = (long long)p->batch * n_new;
-    *s = prompt_sizes(ems::plan_prompt(p->batch, rows, p->batch * rows, p->kv_heads, (long long)p->max_pages * p->page_size), tokens, p->q_heads, p->head_dim);
+    *s = prompt_sizes(ems::plan_prompt(p->batch, rows, p->batch * rows, p->kv_heads, p->q_heads / p->kv_heads, p->head_dim,
+                                        (long long)p->max_pages * p->page_size, p->dtype == EMS_F32), tokens, p->q_heads, p->head_dim);
     return prompt_grid_ok(s->plan, p->kv_heads);
 }
 
@@ -920,7 +937,7 @@ int ems_paged_chunk_workspace_bytes(const ems_paged_params* p, int32_t n_new, si
     int why;
     PromptSizes s;
     if (!chunk_params_ok(p, n_new, &s, &why)) return why;
-    if (chunk_ws) *chunk_ws = s.total;
+    if (chunk_ws) *chunk_ws = few_columns(p, n_new) ? plan_few(p, n_new).total : s.total;
     return EMS_OK;
 }
 
@@ -935,6 +952,19 @@ int ems_paged_chunk_attention(const ems_paged_params* p, const ems_paged_cache* 
     if (!chunk_params_ok(p, n_new, &s, &why)) return why;
     if (!paged_cache_ok(cache) || !lens || !q || !q_strides || !out || !out_strides) return EMS_ERR_INVALID_ARG;
     const bool f32 = p->dtype == EMS_F32;
+    if (few_columns(p, n_new)) {
+        ems::AttendArgs a{};
+        a.q = q; a.q_sb = q_strides->batch; a.q_sh = q_strides->head; a.q_sn = q_strides->token; a.q_wide = wide_rows(q, *q_strides, f32);
+        a.out = out; a.o_sb = out_strides->batch; a.o_sh = out_strides->head; a.o_sn = out_strides->token;
+        a.lse = lse_opt; a.l_sb = (long long)p->q_heads * n_new; a.l_sh = n_new;
+        a.k = cache->k_pages; a.v = cache->v_pages;
+        a.page_table = cache->page_table; a.lens = lens; a.new_len = new_len_opt; a.pos_pages = cache->positions;
+        a.max_pages = p->max_pages; a.page_size = p->page_size; a.num_pages = p->num_pages;
+        a.batch = p->batch; a.kv_heads = p->kv_heads; a.many = true; a.heads = p->q_heads / p->kv_heads; a.tokens = n_new; a.group = a.heads * n_new;
+        a.head_dim = p->head_dim;
+        a.scale_log2e = scale_log2e(p->softmax_scale, p->head_dim);
+        return attend(a, plan_few(p, n_new), f32, ws, ws_bytes, hip_stream);
+    }
     ems::PromptArgs a{};
     a.q = q; a.q_sb = q_strides->batch; a.q_sh = q_strides->head; a.q_sn = q_strides->token; a.q_wide = wide_rows(q, *q_strides, f32);
     a.out = out; a.o_sb = out_strides->batch; a.o_sh = out_strides->head; a.o_sn = out_strides->token; a.o_wide = wide_rows(out, *out_strides, f32);
@@ -967,7 +997,8 @@ static PromptSizes plan_prompts(const ems_prompt_params* p, bool packed)
 {
     const int group = p->q_heads / p->kv_heads;
     const long long rows = (long long)p->q_rows * group, tokens = packed ? p->q_rows : (long long)p->batch * p->q_rows;
-    return prompt_sizes(ems::plan_prompt(p->batch, rows, packed ? rows : p->batch * rows, p->kv_heads, p->k_rows), tokens, p->q_heads, p->head_dim);
+    return prompt_sizes(ems::plan_prompt(p->batch, rows, packed ? rows : p->batch * rows, p->kv_heads, group, p->head_dim,
+                                        std::max(p->k_rows, 1), p->dtype == EMS_F32), tokens, p->q_heads, p->head_dim);
 }
 
 static bool dense_prompt_ok(const ems_prompt_params* p) { return (long long)p->batch * p->q_rows <= 0x7fffffffll / p->q_heads; }

@@ -220,7 +220,11 @@ struct AttendArgs {
     const void* k_new;          // [batch * kv_heads, D]
     const void* v_new;
     int n_tok, budget;
-    int batch, kv_heads, group, head_dim;
+    const int32_t* new_len;     // several new tokens a sequence: [batch] how many, or null: all `tokens`
+    long long q_sn, o_sb, o_sh, o_sn, l_sb, l_sh;      // strides of their queries, outputs and log-sum-exps
+    bool many;                  // whether there may be several, with strides of their own
+    int tokens, heads;          // at most; q-heads of one
+    int batch, kv_heads, group, head_dim;      // group: q-heads of a kv-head, of all its new tokens
     int workers;                // per kv-head and tile of q-heads: they share its sequences evenly; 0 = a block per sequence
     bool q_wide;                // q rows start at multiples of 16 bytes
     float scale_log2e;
@@ -260,7 +264,7 @@ struct PromptArgs {
 };
 struct PromptPlan { int waves, splits; long long tiles; };      // of a block; of a tile's rows; tiles of a kv-head at most
 // `sequences` of at most `rows` query rows (tokens x q-heads of a group) each and `all_rows` together, over at most `most` rows
-PromptPlan plan_prompt(long long sequences, long long rows, long long all_rows, int kv_heads, long long most);
+PromptPlan plan_prompt(long long sequences, long long rows, long long all_rows, int kv_heads, int group, int head_dim, long long most, bool f32);
 hipError_t launch_prompt(const PromptArgs& a, const PromptPlan& plan, int head_dim, bool f32, hipStream_t st);
 constexpr int kAttendQ = 16;    // q-heads of a group that a block takes: the columns of a matrix product
 constexpr int kAttendUnit = 128;        // rows that work is counted in

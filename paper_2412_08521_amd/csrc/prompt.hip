@@ -1078,22 +1078,48 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a)
 
 // ---- launches
 
-// Waves of a block (32 query rows each) and blocks that share a tile's rows of keys and values.
-PromptPlan plan_prompt(long long sequences, long long rows, long long all_rows, int kv_heads, long long most)
+// Rows of a block (32 a wave; 64 a wave where there are 256) and blocks that share a tile's rows of keys and values: what an estimate
+// of the time (us) finds least.  A compute unit takes `unit` for 32 query rows by 64 rows of keys and values where it has as
+// many blocks as fit; a block alone takes `stage` for 64 rows of them, and no call is shorter than its longest block; a join is a
+// launch and its traffic.  The figures are those of prompts of 77 to 4096 tokens, each size measured with each choice; where two
+// choices are near each other the estimate may take the other.
+PromptPlan plan_prompt(long long sequences, long long rows, long long all_rows, int kv_heads, int group, int head_dim, long long most, bool f32)
 {
-    PromptPlan p{};
-    const auto blocks = [&](int waves) {
+    PromptPlan best{};
+    const auto tiles = [&](int waves) {
         const int tile = 32 * waves;
         const long long by_sequence = sequences * ((rows + tile - 1) / tile), together = (all_rows + tile - 1) / tile + sequences;
-        return kv_heads * (by_sequence < together ? by_sequence : together);
+        return by_sequence < together ? by_sequence : together;
     };
-    p.waves = 8;
-    while (p.waves > 1 && blocks(p.waves) < 256) p.waves /= 2;
-    p.tiles = blocks(p.waves) / kv_heads;
-    p.splits = 1;
-    const long long n = blocks(p.waves);
-    if (n < 256 && most >= 1024) p.splits = (int)std::min({(512 + n - 1) / n, most / 512, 64ll});
-    return p;
+    if (f32) {      // matrix products bound it: two waves a block, and blocks for two waves a SIMD
+        best.waves = 2;
+        best.tiles = tiles(2);
+        best.splits = (int)std::max(1ll, std::min({1024 / (best.tiles * kv_heads), most / 128, 8ll}));
+        return best;
+    }
+    struct Cost { int waves, fit; double unit, stage, begin; };
+    static constexpr Cost kWide[] = {{8, 1, 0.21, 1.7, 11.}, {4, 2, 0.27, 1.2, 5.7}, {2, 2, 0.32, 1.2, 5.3}, {1, 2, 0.58, 1.2, 5.1}};      // head size 128
+    static constexpr Cost kNarrow[] = {{8, 2, 0.13, 1.1, 11.}, {4, 3, 0.19, 0.66, 5.7}, {2, 4, 0.21, 0.62, 5.3}, {1, 4, 0.22, 0.62, 5.1}};     // 64
+    const double stages = (double)((most + 63) / 64), seen = 1. - std::min(1., (double)rows / group / most) / 2;         // of them by a query
+    double least = 0.;
+    for (const Cost& c : head_dim == 128 ? kWide : kNarrow) {
+        const long long n = tiles(c.waves);
+        for (int splits = 1; splits <= 16 && (splits == 1 || most >= 256 * splits); splits *= 2) {
+            const double blocks = (double)n * kv_heads * splits;
+            const double whole = (double)all_rows / 32 * kv_heads * stages * seen * c.unit / 256;
+            const double crowd = std::min((double)c.fit, blocks / 256);
+            const double longest = (stages / splits + 1) * std::max(c.stage, c.unit * c.waves * crowd);
+            const double join = splits > 1 ? 5. + (double)all_rows * kv_heads * splits * head_dim * 8 / 3e6 : 0.;
+            const double time = std::max(whole, longest) + c.begin + join;
+            if (best.waves == 0 || time < least) {
+                least = time;
+                best.waves = c.waves;
+                best.splits = splits;
+                best.tiles = n;
+            }
+        }
+    }
+    return best;
 }
 
 namespace {
