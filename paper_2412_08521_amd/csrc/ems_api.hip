@@ -928,7 +928,7 @@ static bool chunk_params_ok(const ems_paged_params* p, int32_t n_new, PromptSize
     if ((long long)p->batch * n_new > 0x7fffffffll / p->q_heads) return false;
     const long long rows = (long long)n_new * (p->q_heads / p->kv_heads), tokens = (long long)p->batch * n_new;
     *s = prompt_sizes(ems::plan_prompt(p->batch, rows, p->batch * rows, p->kv_heads, p->q_heads / p->kv_heads, p->head_dim,
-                                        (long long)p->max_pages * p->page_size, p->dtype == EMS_F32), tokens, p->q_heads, p->head_dim);
+                                        (long long)p->max_pages * p->page_size, true, p->dtype == EMS_F32), tokens, p->q_heads, p->head_dim);
     return prompt_grid_ok(s->plan, p->kv_heads);
 }
 
@@ -998,7 +998,7 @@ static PromptSizes plan_prompts(const ems_prompt_params* p, bool packed)
     const int group = p->q_heads / p->kv_heads;
     const long long rows = (long long)p->q_rows * group, tokens = packed ? p->q_rows : (long long)p->batch * p->q_rows;
     return prompt_sizes(ems::plan_prompt(p->batch, rows, packed ? rows : p->batch * rows, p->kv_heads, group, p->head_dim,
-                                        std::max(p->k_rows, 1), p->dtype == EMS_F32), tokens, p->q_heads, p->head_dim);
+                                        std::max(p->k_rows, 1), false, p->dtype == EMS_F32), tokens, p->q_heads, p->head_dim);
 }
 
 static bool dense_prompt_ok(const ems_prompt_params* p) { return (long long)p->batch * p->q_rows <= 0x7fffffffll / p->q_heads; }

@@ -264,7 +264,7 @@ struct PromptArgs {
 };
 struct PromptPlan { int waves, splits; long long tiles; };      // of a block; of a tile's rows; tiles of a kv-head at most
 // `sequences` of at most `rows` query rows (tokens x q-heads of a group) each and `all_rows` together, over at most `most` rows
-PromptPlan plan_prompt(long long sequences, long long rows, long long all_rows, int kv_heads, int group, int head_dim, long long most, bool f32);
+PromptPlan plan_prompt(long long sequences, long long rows, long long all_rows, int kv_heads, int group, int head_dim, long long most, bool paged, bool f32);
 hipError_t launch_prompt(const PromptArgs& a, const PromptPlan& plan, int head_dim, bool f32, hipStream_t st);
 constexpr int kAttendQ = 16;    // q-heads of a group that a block takes: the columns of a matrix product
 constexpr int kAttendUnit = 128;        // rows that work is counted in

@@ -7,6 +7,8 @@
 //                  S^T = K Q^T    32x32 products; a lane holds one query's column, 16 of a tile's 32 rows
 //                  O^T = V^T P^T  S^T's registers are the right operand as they are; the left one is read transposed
 // prompt_join    a tile whose rows several blocks share: their outputs, weighted by their maxima and sums
+#include <cmath>
+
 #include "ems_common.h"
 #include "ems_kernels.h"
 #include "ems_rows.h"
@@ -499,24 +501,32 @@ __global__ __launch_bounds__(64 * kW, 2) void prompt_simple_kernel(PromptArgs a)
 // LDS goes into two products) and works on three steps of 32 rows at once, products of one beside the weights of another:
 //     S(n) = K(n) Q^T,   P(n - 1) = exp2(S(n - 1) - m),   O += V(n - 2)^T P(n - 2)^T
 // kSome: rows of the cache are masked (by their positions); their logits begin at -inf.
-template <int D, bool kPaged, bool kSome, int kQ, int kW>
-__global__ __launch_bounds__(64 * kW, D == 128 && kQ == 2 ? 1 : 2) void prompt_kernel(PromptArgs a)
+// kS: waves that share the rows of keys and values of one tile (then kW = 1).  Each walks a part of its own, 32 rows a stage, and
+// meets the others at the end.
+template <int D, bool kPaged, bool kSome, int kQ, int kW, int kS>
+__global__ __launch_bounds__(64 * kW * kS, D == 128 && kQ == 2 ? 1 : 2) void prompt_kernel(PromptArgs a)
 {
     typedef bf16_t T;
     using St = Stage<T, D>;
-    constexpr int kKv = St::kRows;
+    constexpr int kKv = St::kRows, kRowsOfLoad = kS > 1 ? 32 : kKv, kLoadBytes = kRowsOfLoad * St::kRowBytes;
+    static_assert(kS == 1 || (kW == 1 && kQ == 1), "one tile");
     constexpr int kFrags = Tile<T, D>::kFrags, kOut = D / 32;
     constexpr int kRowsOf = 32 * kQ * kW;
     constexpr int kBatch = 4, kHold = 2 * kBatch;              // stages whose rows are looked up together, and are known
-    __shared__ __align__(1024) char keys[2][St::kBytes];
-    __shared__ __align__(1024) char vals[3][St::kBytes];
-    __shared__ int row_of[kPaged ? kHold : 1][kKv];
-    __shared__ unsigned long long live_of[kPaged ? kHold : 1];
-    __shared__ int found[kPaged ? kBatch : 1][2][kWave];       // table elements and positions
+    __shared__ __align__(1024) char rings[kS][5][kLoadBytes];              // two of keys, three of values
+    __shared__ int rows_of[kS][kPaged ? kHold : 1][kKv];
+    __shared__ unsigned long long lives_of[kS][kPaged ? kHold : 1];
+    __shared__ int founds[kS][kPaged ? kBatch : 1][2][kWave];  // table elements and positions
 
-    const int lane = threadIdx.x % kWave, wave = scalar((int)threadIdx.x / kWave);
+    const int lane = threadIdx.x % kWave, number = scalar((int)threadIdx.x / kWave);
+    const int wave = kS > 1 ? 0 : number, part = kS > 1 ? number : 0;
+    auto& row_of = rows_of[part];
+    auto& live_of = lives_of[part];
+    auto& found = founds[part];
+    char (&keys)[5][kLoadBytes] = rings[part];
+    char* const vals = rings[part][2];
     const int col = lane % 32, half = lane / 32;
-    const int split = blockIdx.y;
+    const int split = blockIdx.y * kS + part, splits = a.splits * kS;
     const int head = blockIdx.x % a.kv_heads;
     const Place place = find_tile<kPaged>(a, blockIdx.x / a.kv_heads, kRowsOf);
     if (scalar(place.b) < 0) return;
@@ -536,7 +546,7 @@ __global__ __launch_bounds__(64 * kW, D == 128 && kQ == 2 ? 1 : 2) void prompt_k
     const int last_token = min(tile * kRowsOf + kRowsOf - 1, n_rows - 1) / a.group;
     const int rows_end = min(max(last_token + 1 + seq.m - seq.n, 0), seq.m);
     const int n_stages = (rows_end + kKv - 1) / kKv;
-    const int lo = (int)((long long)n_stages * split / a.splits), hi = (int)((long long)n_stages * (split + 1) / a.splits);
+    const int lo = (int)((long long)n_stages * split / splits), hi = (int)((long long)n_stages * (split + 1) / splits);
 
     frag_t qf[kQ][kFrags];
 #pragma unroll
@@ -576,10 +586,10 @@ __global__ __launch_bounds__(64 * kW, D == 128 && kQ == 2 ? 1 : 2) void prompt_k
         }
     };
 
-    const unsigned k_lds = lds_address(&keys[0][0]), v_lds = lds_address(&vals[0][0]);
+    const unsigned k_lds = lds_address(&keys[0][0]), v_lds = lds_address(vals);
     // A stage's rows go to LDS by kDma instructions, neighbouring ones of which are a wave's, in groups under one LDS address.
-    constexpr int kLoads = St::kDma / kW, kGroup = kLoads < 4 ? kLoads : 4;
-    static_assert(St::kDma % kW == 0 && kLoads % kGroup == 0 && (kGroup == 2 || kGroup == 4), "every wave has whole groups");
+    constexpr int kDma = kLoadBytes / 1024, kLoads = kDma / kW, kGroup = kLoads < 4 ? kLoads : 4;
+    static_assert(kDma % kW == 0 && kLoads % kGroup == 0 && (kGroup == 2 || kGroup == 4), "every wave has whole groups");
     const auto row_of_load = [&](int i) __attribute__((always_inline)) { return (wave * kLoads + i) * St::kDmaRows + lane / St::kPieces; };
     const auto key_piece = [&](int i) __attribute__((always_inline)) { return 16 * (lane % St::kPieces ^ St::key(row_of_load(i))); };
     const auto value_piece = [&](int i) __attribute__((always_inline)) { return 16 * (lane % St::kPieces ^ St::value(row_of_load(i))); };
@@ -592,23 +602,24 @@ __global__ __launch_bounds__(64 * kW, D == 128 && kQ == 2 ? 1 : 2) void prompt_k
     if constexpr (!kPaged) {
         k_first = reinterpret_cast<const char*>(reinterpret_cast<const T*>(a.k) + (a.q_start ? 0 : b * a.k_sb) + head * a.k_sh + seq.k_first * a.k_sn);
         v_first = reinterpret_cast<const char*>(reinterpret_cast<const T*>(a.v) + (a.q_start ? 0 : b * a.v_sb) + head * a.v_sh + seq.k_first * a.v_sn);
-        k_next = k_first + (hi - 1) * kKv * k_step;
-        v_next = v_first + (hi - 1) * kKv * v_step;
+        k_next = k_first + (long long)(hi * kKv - kRowsOfLoad) * k_step;
+        v_next = v_first + (long long)(hi * kKv - kRowsOfLoad) * v_step;
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
             k_off[i] = (unsigned)row_of_load(i) * (unsigned)k_step + key_piece(i) + kDmaBias - 1024 * (i % kGroup);
             v_off[i] = (unsigned)row_of_load(i) * (unsigned)v_step + value_piece(i) + kDmaBias - 1024 * (i % kGroup);
         }
     }
-    const auto load_stage = [&](int it, int kbuf, int vbuf) __attribute__((always_inline)) {
-        const unsigned k_to = scalar((int)(k_lds + kbuf * St::kBytes)) + 1024 * kLoads * wave, v_to = scalar((int)(v_lds + vbuf * St::kBytes)) + 1024 * kLoads * wave;
+    const auto load_rows = [&](int first, int kbuf, int vbuf) __attribute__((always_inline)) {       // kRowsOfLoad rows, of one stage
+        const unsigned k_to = scalar((int)(k_lds + kbuf * kLoadBytes)) + 1024 * kLoads * wave, v_to = scalar((int)(v_lds + vbuf * kLoadBytes)) + 1024 * kLoads * wave;
+        const int it = first / kKv;
         if constexpr (kPaged) {
             if (live_of[it % kHold] == 0) {                  // nothing there: zeros, which count nothing
 #pragma unroll
                 for (int i = 0; i < kLoads; ++i) {
                     const int at = 1024 * (wave * kLoads + i) + 16 * lane;
                     *reinterpret_cast<frag_t*>(&keys[kbuf][at]) = zero_frag();
-                    *reinterpret_cast<frag_t*>(&vals[vbuf][at]) = zero_frag();
+                    *reinterpret_cast<frag_t*>(&vals[vbuf * kLoadBytes + at]) = zero_frag();
                 }
                 return;
             }
@@ -617,14 +628,14 @@ __global__ __launch_bounds__(64 * kW, D == 128 && kQ == 2 ? 1 : 2) void prompt_k
                 const char *k[kGroup], *v[kGroup];
 #pragma unroll
                 for (int i = 0; i < kGroup; ++i) {
-                    const unsigned long long at = (unsigned long long)(unsigned)row_of[it % kHold][row_of_load(g + i)] * St::kRowBytes;
+                    const unsigned long long at = (unsigned long long)(unsigned)row_of[it % kHold][first % kKv + row_of_load(g + i)] * St::kRowBytes;
                     k[i] = reinterpret_cast<const char*>(a.k) + key_piece(g + i) - 1024 * i + at;
                     v[i] = reinterpret_cast<const char*>(a.v) + value_piece(g + i) - 1024 * i + at;
                 }
                 dma_group<kGroup>(k, k_to + 1024 * g);
                 dma_group<kGroup>(v, v_to + 1024 * g);
             }
-        } else if (!rare(!a.kv_wide || it * kKv + kKv > seq.m)) {
+        } else if (!rare(!a.kv_wide || first + kRowsOfLoad > seq.m)) {
 #pragma unroll
             for (int g = 0; g < kLoads; g += kGroup) {
                 unsigned k[kGroup], v[kGroup];
@@ -639,7 +650,7 @@ __global__ __launch_bounds__(64 * kW, D == 128 && kQ == 2 ? 1 : 2) void prompt_k
                 const char *k[kGroup], *v[kGroup];
 #pragma unroll
                 for (int i = 0; i < kGroup; ++i) {
-                    const unsigned t = min(it * kKv + row_of_load(g + i), seq.m - 1);
+                    const unsigned t = min(first + row_of_load(g + i), seq.m - 1);
                     k[i] = k_first + t * (unsigned long long)(unsigned)k_step + key_piece(g + i) - 1024 * i;
                     v[i] = v_first + t * (unsigned long long)(unsigned)v_step + value_piece(g + i) - 1024 * i;
                 }
@@ -649,14 +660,14 @@ __global__ __launch_bounds__(64 * kW, D == 128 && kQ == 2 ? 1 : 2) void prompt_k
         } else {
 #pragma unroll 4
             for (int i = 0; i < kLoads; ++i) {
-                const long long t = min(it * kKv + row_of_load(i), seq.m - 1);
+                const long long t = min(first + row_of_load(i), seq.m - 1);
                 const int at = 1024 * (wave * kLoads + i) + 16 * lane;
                 *reinterpret_cast<frag_t*>(&keys[kbuf][at]) = load_piece(reinterpret_cast<const T*>(k_first + t * k_step + key_piece(i)), false);
-                *reinterpret_cast<frag_t*>(&vals[vbuf][at]) = load_piece(reinterpret_cast<const T*>(v_first + t * v_step + value_piece(i)), false);
+                *reinterpret_cast<frag_t*>(&vals[vbuf * kLoadBytes + at]) = load_piece(reinterpret_cast<const T*>(v_first + t * v_step + value_piece(i)), false);
             }
         }
-        k_next -= kKv * k_step;
-        v_next -= kKv * v_step;
+        k_next -= kRowsOfLoad * k_step;
+        v_next -= kRowsOfLoad * v_step;
     };
 
     // ---- the wave's state
@@ -901,16 +912,18 @@ __global__ __launch_bounds__(64 * kW, D == 128 && kQ == 2 ? 1 : 2) void prompt_k
     }
     int kbuf = 0, vbuf = 0;
     unsigned v_prev = v_lds;                                   // values of the step before (any, where there is none)
-    if (hi > lo) load_stage(hi - 1, 0, 0);
+    if (hi > lo) load_rows(hi * kKv - kRowsOfLoad, 0, 0);
     const bool works = r0 < n_rows;
     bool begun = false;
     int it = hi - 1;
     const auto stage = [&](auto top_) __attribute__((always_inline)) {
         constexpr bool kTop = decltype(top_)::value;           // some query may not see all of the rows at hand
+        int vnext = vbuf == 2 ? 0 : vbuf + 1;
         wait_vmem<0>();
-        __syncthreads();
-        const int vnext = vbuf == 2 ? 0 : vbuf + 1;
-        if (it > lo) load_stage(it - 1, kbuf ^ 1, vnext);
+        if constexpr (kS == 1) {
+            __syncthreads();
+            if (it > lo) load_rows((it - 1) * kKv, kbuf ^ 1, vnext);
+        }
         unsigned long long live = ~0ull;
         if constexpr (kPaged) {
             live = live_of[it % kHold];
@@ -925,7 +938,12 @@ __global__ __launch_bounds__(64 * kW, D == 128 && kQ == 2 ? 1 : 2) void prompt_k
         if (works && (!kTop || it * kKv < lim_max)) {
 #pragma unroll
             for (int j = 1; j >= 0; --j) {
-                const unsigned here = (unsigned)(live >> (32 * j)), k_at = k_lds + kbuf * St::kBytes + 32 * j * St::kRowBytes;
+                if constexpr (kS > 1) {
+                    wait_vmem<0>();
+                    vnext = vbuf == 2 ? 0 : vbuf + 1;
+                    if (j == 1 || it > lo) load_rows(it * kKv + 32 * j - 32, kbuf ^ 1, vnext);
+                }
+                const unsigned here = (unsigned)(live >> (32 * j)), k_at = k_lds + kbuf * kLoadBytes + (kS > 1 ? 0 : 32 * j * St::kRowBytes);
                 const bool edge = kTop && it * kKv + 32 * j + 32 > lim_min;
                 const Step now{it * kKv + 32 * j, here, edge, edge || (kPaged && !kSome && here != ~0u)};
                 if (rare(before.shown)) hide(j == 1 ? s[1] : s[0], before);
@@ -935,13 +953,13 @@ __global__ __launch_bounds__(64 * kW, D == 128 && kQ == 2 ? 1 : 2) void prompt_k
                     begun = true;
                 } else if (j == 1) turn(ic<0>{}, here, k_at, v_prev);
                 else turn(ic<1>{}, here, k_at, v_prev);
-                v_prev = v_lds + vbuf * St::kBytes + 32 * j * St::kRowBytes;
+                v_prev = v_lds + vbuf * kLoadBytes + (kS > 1 ? 0 : 32 * j * St::kRowBytes);
                 old = before;
                 before = now;
+                if constexpr (kS > 1) { kbuf ^= 1; vbuf = vnext; }
             }
         }
-        kbuf ^= 1;
-        vbuf = vnext;
+        if constexpr (kS == 1) { kbuf ^= 1; vbuf = vnext; }
     };
     // the first stage and those that some query does not see whole, and one more for what is under way; then those that need no look
     const int whole = min(lim_min / kKv, hi) - 1;
@@ -977,6 +995,51 @@ __global__ __launch_bounds__(64 * kW, D == 128 && kQ == 2 ? 1 : 2) void prompt_k
                 for (int c = 0; c < kQ; ++c) add_out(o[c][i], vf[t][i], p[1][c][t]);
     }
     settle_out();
+
+    if constexpr (kS > 1) {
+        // the parts' results, where their rings were
+        typedef float row_t[D + 4];
+        row_t* const mine = reinterpret_cast<row_t*>(&rings[part][0][0]);
+        static_assert(5 * kLoadBytes >= 32 * (int)sizeof(row_t), "rows of a part");
+        const float total = halves_sum(l[0]);
+#pragma unroll
+        for (int i = 0; i < kOut; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; r += 4)
+                *reinterpret_cast<f32x4_t*>(&mine[col][32 * i + acc_row(r, half)]) = f32x4_t{o[0][i][r], o[0][i][r + 1], o[0][i][r + 2], o[0][i][r + 3]};
+        if (half == 0) { mine[col][D] = m[0]; mine[col][D + 1] = total; }
+        __syncthreads();
+        for (int x = threadIdx.x; x < 32 * (D / 4); x += 64 * kS) {
+            const int at = x / (D / 4), d = x % (D / 4) * 4, row = r0 + at;
+            if (row >= n_rows) break;
+            const auto of = [&](int w) { return reinterpret_cast<const row_t*>(&rings[w][0][0])[at]; };
+            float top = of(0)[D];
+#pragma unroll
+            for (int w = 1; w < kS; ++w) top = fmaxf(top, of(w)[D]);
+            const float ref = top > -INFINITY ? top : 0.f;
+            float sum = 0.f;
+            f32x4_t y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < kS; ++w) {
+                const float f = exp2_fast(of(w)[D] - ref);
+                sum += f * of(w)[D + 1];
+                y += f * *reinterpret_cast<const f32x4_t*>(&of(w)[d]);
+            }
+            const int tok = row / a.group, qh = head * a.group + row - tok * a.group;
+            const long long q_token = seq.q_first + tok;
+            if (a.splits > 1) {
+                const long long to = (q_token * a.kv_heads * a.group + qh) * a.splits + blockIdx.y;
+                *reinterpret_cast<f32x4_t*>(a.part_o + to * D + d) = y;
+                if (d == 0) { a.part_ml[2 * to] = top; a.part_ml[2 * to + 1] = sum; }
+                continue;
+            }
+            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+            T* out = reinterpret_cast<T*>(a.out) + qh * a.o_sh + (a.q_start ? q_token * a.o_sn : b * a.o_sb + tok * a.o_sn) + d;
+            store4(out, y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv, a.o_wide);
+            if (a.lse && d == 0) a.lse[(a.q_start ? q_token : b * a.l_sb + tok) + qh * a.l_sh] = (ref + log2_fast(sum)) * 0.6931471805599453f;
+        }
+        return;
+    }
 
     // ---- the lane's queries: columns 32 i + acc_row(r, half)
 #pragma unroll
@@ -1078,12 +1141,12 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a)
 
 // ---- launches
 
-// Rows of a block (32 a wave; 64 a wave where there are 256) and blocks that share a tile's rows of keys and values: what an estimate
+// Rows of a block (256, 64 a wave; 128 or 64, 32 a wave; 32, whose waves share the rows of keys and values) and blocks that share a tile's rows of keys and values: what an estimate
 // of the time (us) finds least.  A compute unit takes `unit` for 32 query rows by 64 rows of keys and values where it has as
 // many blocks as fit; a block alone takes `stage` for 64 rows of them, and no call is shorter than its longest block; a join is a
 // launch and its traffic.  The figures are those of prompts of 77 to 4096 tokens, each size measured with each choice; where two
 // choices are near each other the estimate may take the other.
-PromptPlan plan_prompt(long long sequences, long long rows, long long all_rows, int kv_heads, int group, int head_dim, long long most, bool f32)
+PromptPlan plan_prompt(long long sequences, long long rows, long long all_rows, int kv_heads, int group, int head_dim, long long most, bool paged, bool f32)
 {
     PromptPlan best{};
     const auto tiles = [&](int waves) {
@@ -1097,9 +1160,9 @@ PromptPlan plan_prompt(long long sequences, long long rows, long long all_rows, 
         best.splits = (int)std::max(1ll, std::min({1024 / (best.tiles * kv_heads), most / 128, 8ll}));
         return best;
     }
-    struct Cost { int waves, fit; double unit, stage, begin; };
-    static constexpr Cost kWide[] = {{8, 1, 0.21, 1.7, 11.}, {4, 2, 0.27, 1.2, 5.7}, {2, 2, 0.32, 1.2, 5.3}, {1, 2, 0.58, 1.2, 5.1}};      // head size 128
-    static constexpr Cost kNarrow[] = {{8, 2, 0.13, 1.1, 11.}, {4, 3, 0.19, 0.66, 5.7}, {2, 4, 0.21, 0.62, 5.3}, {1, 4, 0.22, 0.62, 5.1}};     // 64
+    struct Cost { int waves, fit, fit_paged; double unit, stage, begin; };
+    static constexpr Cost kWide[] = {{8, 1, 1, 0.21, 1.7, 11.}, {4, 2, 1, 0.27, 1.2, 5.9}, {2, 2, 1, 0.32, 1.2, 5.3}, {1, 2, 1, 0.42, 0.62, 7.4}};     // head size 128
+    static constexpr Cost kNarrow[] = {{8, 2, 2, 0.13, 1.1, 11.}, {4, 3, 3, 0.19, 0.66, 5.7}, {2, 4, 3, 0.21, 0.62, 5.3}, {1, 2, 1, 0.25, 0.2, 6.8}};    // 64
     const double stages = (double)((most + 63) / 64), seen = 1. - std::min(1., (double)rows / group / most) / 2;         // of them by a query
     double least = 0.;
     for (const Cost& c : head_dim == 128 ? kWide : kNarrow) {
@@ -1107,10 +1170,12 @@ PromptPlan plan_prompt(long long sequences, long long rows, long long all_rows, 
         for (int splits = 1; splits <= 16 && (splits == 1 || most >= 256 * splits); splits *= 2) {
             const double blocks = (double)n * kv_heads * splits;
             const double whole = (double)all_rows / 32 * kv_heads * stages * seen * c.unit / 256;
-            const double crowd = std::min((double)c.fit, blocks / 256);
-            const double longest = (stages / splits + 1) * std::max(c.stage, c.unit * c.waves * crowd);
+            const int fit = paged ? c.fit_paged : c.fit;
+            const double crowd = std::min((double)fit, blocks / 256), stage = std::max(c.stage, c.unit * c.waves * crowd);
+            const double longest = (stages / splits + 1) * stage;
+            const double rounds = std::ceil(blocks / (256. * fit)) * (stages * seen / splits + 1) * stage;
             const double join = splits > 1 ? 5. + (double)all_rows * kv_heads * splits * head_dim * 8 / 3e6 : 0.;
-            const double time = std::max(whole, longest) + c.begin + join;
+            const double time = std::max({whole, longest, rounds}) + c.begin + join;
             if (best.waves == 0 || time < least) {
                 least = time;
                 best.waves = c.waves;
@@ -1126,10 +1191,11 @@ namespace {
 template <int D, bool kPaged, bool kSome>
 void launch_tiles(const PromptArgs& a, int waves, dim3 grid, hipStream_t st)
 {
-    if (waves == 8) prompt_kernel<D, kPaged, kSome, 2, 4><<<grid, 256, 0, st>>>(a);
-    else if (waves == 4) prompt_kernel<D, kPaged, kSome, 1, 4><<<grid, 256, 0, st>>>(a);
-    else if (waves == 2) prompt_kernel<D, kPaged, kSome, 1, 2><<<grid, 128, 0, st>>>(a);
-    else prompt_kernel<D, kPaged, kSome, 1, 1><<<grid, 64, 0, st>>>(a);
+    constexpr int kS = D == 64 ? 4 : 2;
+    if (waves == 8) prompt_kernel<D, kPaged, kSome, 2, 4, 1><<<grid, 256, 0, st>>>(a);
+    else if (waves == 4) prompt_kernel<D, kPaged, kSome, 1, 4, 1><<<grid, 256, 0, st>>>(a);
+    else if (waves == 2) prompt_kernel<D, kPaged, kSome, 1, 2, 1><<<grid, 128, 0, st>>>(a);
+    else prompt_kernel<D, kPaged, kSome, 1, 1, kS><<<grid, 64 * kS, 0, st>>>(a);
 }
 
 template <typename T, int D, bool kPaged>
