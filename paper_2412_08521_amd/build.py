@@ -5,6 +5,8 @@ hipcc cross-compiles without a GPU.  Usage:  python -m paper_2412_08521_amd.buil
 from __future__ import annotations
 
 import os
+import re
+import shutil
 import subprocess
 import sys
 from concurrent.futures import ThreadPoolExecutor
@@ -61,6 +63,61 @@ def _check_no_scratch(src: str, remarks: str) -> None:
         raise RuntimeError(f"{src}: no resource-usage remark found for kernels {guarded}")
 
 
+# Kernels that write their own matrix products (inline assembly) into accumulation registers: the compiler does not know that
+# these are products and keeps no distance between a vector instruction that writes an operand and the product that reads it.
+OWN_PRODUCTS = {"prompt.hip"}
+
+
+def _registers(text: str):
+    """'v[0:3]' or 'a17' -> {('v', 0), ..}; anything else -> the empty set."""
+    m = re.match(r"([va])(?:(\d+)$|\[(\d+):(\d+)\]$)", text.strip())
+    if not m:
+        return set()
+    lo, hi = (int(m.group(2)),) * 2 if m.group(2) else (int(m.group(3)), int(m.group(4)))
+    return {(m.group(1), i) for i in range(lo, hi + 1)}
+
+
+def _check_own_products(src: str, assembly: str) -> None:
+    """Raise if an operand of a product in inline assembly is written by a vector instruction less than two wait states before
+    it (a label counts as unknown: the code there begins with a wait of its own), or if there is no such product."""
+    seen, own, before = 0, False, []                       # before: (wait states, registers written) of what came before
+    for line in assembly.splitlines():
+        text = line.split(";")[0].strip() if "#ASM" not in line else line.strip()
+        if "#ASMSTART" in text or "#ASMEND" in text:
+            own = "#ASMSTART" in text
+            continue
+        if not text or text.startswith(("//", "#")):
+            continue
+        if text.endswith(":"):
+            before = [(0, None)]
+            continue
+        if text.startswith("."):
+            continue
+        op, _, rest = text.partition(" ")
+        args = re.findall(r"[vas]\[\d+:\d+\]|[va]\d+|[^,\s]+", rest)
+        if own and op.startswith("v_mfma"):
+            seen += 1
+            reads, states = set().union(*(_registers(x) for x in args[1:])), 0
+            for n, written in reversed(before):
+                if states >= 2:
+                    break
+                if written is None or written & reads:
+                    raise RuntimeError(f"{src}: an operand of `{text}` may be written less than two wait states before it")
+                states += n
+        if op == "s_nop":
+            before.append((int(args[0], 0) + 1, set()))
+        elif op.startswith("v_") and not op.startswith("v_mfma"):
+            writes = _registers(args[0]) if args else set()
+            if "swap" in op and len(args) > 1:
+                writes |= _registers(args[1])
+            before.append((1, writes))
+        else:
+            before.append((1, set()))
+        before = before[-4:]
+    if not seen:
+        raise RuntimeError(f"{src}: no product in inline assembly found")
+
+
 def _stale(out: str, deps) -> bool:
     if not os.path.exists(out):
         return True
@@ -76,7 +133,12 @@ def build(force: bool = False, verbose: bool = False) -> str:
         s = os.path.join(CSRC, src)
         o = os.path.join(OBJ_DIR, src.replace(".hip", ".o"))
         if force or _stale(o, [s] + hdrs):
+            temps = o.replace(".o", "_temps")
             cmd = [HIPCC] + FLAGS + FILE_FLAGS.get(src, []) + ["-c", s, "-o", o]
+            if src in OWN_PRODUCTS:
+                os.makedirs(temps, exist_ok=True)
+                cmd += ["-save-temps=obj"]
+                cmd[cmd.index(o)] = os.path.join(temps, os.path.basename(o))
             r = subprocess.run(cmd, capture_output=True, text=True)
             err = "\n".join(l for l in r.stderr.splitlines()
                             if "packed-fp32-ops' is not a recognized feature" not in l)
@@ -90,6 +152,11 @@ def build(force: bool = False, verbose: bool = False) -> str:
                     raise
                 err = "\n".join(l for l in err.splitlines() if "kernel-resource-usage" not in l
                                 and not l.lstrip().startswith(("|", "^")) and "{" != l.strip()[-1:])
+            if src in OWN_PRODUCTS:
+                with open(os.path.join(temps, src.replace(".hip", "-hip-amdgcn-amd-amdhsa-gfx950.s"))) as f:
+                    _check_own_products(src, f.read())
+                os.replace(os.path.join(temps, os.path.basename(o)), o)
+                shutil.rmtree(temps)
             if verbose and err.strip():
                 print(err, file=sys.stderr)
         return o

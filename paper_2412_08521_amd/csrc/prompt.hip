@@ -701,9 +701,14 @@ __global__ __launch_bounds__(64 * kW * kS, D == 128 && kQ == 2 ? 1 : 2) void pro
         const s16x4_t y = read_transposed(((v_base + at) ^ (64 * i)) + (16 * t + 8) * St::kRowBytes);
         return __builtin_bit_cast(frag_t, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
     };
+    // Outputs.  Those of the largest tiles are held in the accumulation registers, which the compiler would not do beside logits that
+    // the vector ALU reads: their products are written out, and so are the waits that it would place.  A product's operands
+    // come two instructions before it at least, its results 18 after it (the build looks whether the first holds in what was
+    // compiled, and refuses it otherwise).
     constexpr bool kAcc = D == 128 && kQ == 2;
-    const auto add_out = [&](f32x16_t& x, const frag_t& v, const frag_t& w) __attribute__((always_inline)) {
-        if constexpr (kAcc) asm("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(x) : "v"(v), "v"(w));
+    const auto add_out = [&](f32x16_t& x, const frag_t& v, const frag_t& w, auto apart) __attribute__((always_inline)) {
+        if constexpr (kAcc && decltype(apart)::value) asm volatile("s_nop 1");
+        if constexpr (kAcc) asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+a"(x) : "v"(v), "v"(w));
         else mma<T>(x, v, w);
     };
     const auto settle_weights = [&]() __attribute__((always_inline)) { if constexpr (kAcc) asm volatile("s_nop 1" ::: "memory"); };
@@ -868,7 +873,7 @@ __global__ __launch_bounds__(64 * kW * kS, D == 128 && kQ == 2 ? 1 : 2) void pro
 #pragma unroll
         for (int n = 0; n < kPv; ++n) {
             const int t = n / (kOut * kQ), i = n / kQ % kOut, c = n % kQ;
-            add_out(o[c][i], vf[t][i], p[cur][c][t]);
+            add_out(o[c][i], vf[t][i], p[cur][c][t], std::false_type{});
             if (n < kFrags) kf[n] = lds_frag((k_base + k_at) ^ (32 * n));
 #pragma unroll
             for (int e = n * kElems / kSlots; e < (n + 1) * kElems / kSlots; ++e) element(e);
@@ -975,7 +980,7 @@ __global__ __launch_bounds__(64 * kW * kS, D == 128 && kQ == 2 ? 1 : 2) void pro
 #pragma unroll
         for (int i = 0; i < kOut; ++i)
 #pragma unroll
-            for (int c = 0; c < kQ; ++c) add_out(o[c][i], vf[t][i], p[0][c][t]);
+            for (int c = 0; c < kQ; ++c) add_out(o[c][i], vf[t][i], p[0][c][t], std::true_type{});
         float sum[kQ];
 #pragma unroll
         for (int c = 0; c < kQ; ++c) sum[c] = INFINITY;        // (the weights are formed here)
@@ -992,7 +997,7 @@ __global__ __launch_bounds__(64 * kW * kS, D == 128 && kQ == 2 ? 1 : 2) void pro
 #pragma unroll
             for (int i = 0; i < kOut; ++i)
 #pragma unroll
-                for (int c = 0; c < kQ; ++c) add_out(o[c][i], vf[t][i], p[1][c][t]);
+                for (int c = 0; c < kQ; ++c) add_out(o[c][i], vf[t][i], p[1][c][t], std::true_type{});
     }
     settle_out();
 
