@@ -33,11 +33,12 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
 # ordinary vector registers, never to the accumulation file (which the ALU cannot read).
 _STREAM = ["-mllvm", "-amdgpu-mfma-vgpr-form=1", "-Rpass-analysis=kernel-resource-usage"]
 FILE_FLAGS = {"score.hip": _STREAM, "score_m16.hip": _STREAM, "score_f32.hip": _STREAM, "stats.hip": _STREAM, "merge.hip": _STREAM[:2],
-              "attend.hip": _STREAM[:2], "prompt.hip": _STREAM[:2]}
+              "attend.hip": _STREAM[:2], "prompt.hip": _STREAM}
 # Kernels that count their own vector-memory operations (s_waitcnt vmcnt(n) by hand around the
 # LDS DMA): a register spill would add scratch loads/stores the count does not know about, so
 # such a build is rejected instead of being allowed to run with a silent race.
-NO_SCRATCH = {"score.hip": ("score_pass1", "score_pass2"), "score_m16.hip": ("score_pass1", "score_pass2"), "score_f32.hip": ("score_pass1", "score_pass2"), "stats.hip": ("redundancy_stream",)}
+NO_SCRATCH = {"score.hip": ("score_pass1", "score_pass2"), "score_m16.hip": ("score_pass1", "score_pass2"), "score_f32.hip": ("score_pass1", "score_pass2"), "stats.hip": ("redundancy_stream",),
+              "prompt.hip": ("prompt_kernel",)}        # (whose waits for its DMA a spill's loads would make longer)
 
 
 def _check_no_scratch(src: str, remarks: str) -> None:
@@ -47,7 +48,7 @@ def _check_no_scratch(src: str, remarks: str) -> None:
     for line in remarks.splitlines():
         if "remark:" not in line:
             continue
-        text = line.split("remark:", 1)[1].strip()
+        text = re.sub(r"^\S+:\d+:\d+: ", "", line.split("remark:", 1)[1].strip()).strip()         # (the place comes before or after)
         if text.startswith("Function Name:"):
             name = text.split(":", 1)[1].split("[")[0].strip()
         elif name and any(g in name for g in guarded):
@@ -133,29 +134,32 @@ def build(force: bool = False, verbose: bool = False) -> str:
         s = os.path.join(CSRC, src)
         o = os.path.join(OBJ_DIR, src.replace(".hip", ".o"))
         if force or _stale(o, [s] + hdrs):
+            # with the assembly beside it, where that is looked at too, in a folder that does not stay
             temps = o.replace(".o", "_temps")
-            cmd = [HIPCC] + FLAGS + FILE_FLAGS.get(src, []) + ["-c", s, "-o", o]
+            obj = os.path.join(temps, os.path.basename(o)) if src in OWN_PRODUCTS else o
             if src in OWN_PRODUCTS:
-                os.makedirs(temps, exist_ok=True)
-                cmd += ["-save-temps=obj"]
-                cmd[cmd.index(o)] = os.path.join(temps, os.path.basename(o))
+                shutil.rmtree(temps, ignore_errors=True)
+                os.makedirs(temps)
+            cmd = [HIPCC] + FLAGS + FILE_FLAGS.get(src, []) + ["-c", s, "-o", obj] + (["-save-temps=obj"] if src in OWN_PRODUCTS else [])
             r = subprocess.run(cmd, capture_output=True, text=True)
             err = "\n".join(l for l in r.stderr.splitlines()
-                            if "packed-fp32-ops' is not a recognized feature" not in l)
+                            if "packed-fp32-ops' is not a recognized feature" not in l and not re.match(r"\d+ warnings? generated", l))
             if r.returncode != 0:
                 raise RuntimeError(f"hipcc failed on {src}:\n{err}")
-            if src in NO_SCRATCH:
-                try:
+            try:                              # never link an object that fails a check
+                if src in NO_SCRATCH:
                     _check_no_scratch(src, err)
-                except RuntimeError:
-                    os.remove(o)          # never link an object that failed the check
-                    raise
+                if src in OWN_PRODUCTS:
+                    with open(obj.replace(".o", "-hip-amdgcn-amd-amdhsa-gfx950.s")) as f:
+                        _check_own_products(src, f.read())
+            except RuntimeError:
+                os.remove(obj)
+                raise
+            if src in NO_SCRATCH:
                 err = "\n".join(l for l in err.splitlines() if "kernel-resource-usage" not in l
                                 and not l.lstrip().startswith(("|", "^")) and "{" != l.strip()[-1:])
             if src in OWN_PRODUCTS:
-                with open(os.path.join(temps, src.replace(".hip", "-hip-amdgcn-amd-amdhsa-gfx950.s"))) as f:
-                    _check_own_products(src, f.read())
-                os.replace(os.path.join(temps, os.path.basename(o)), o)
+                os.replace(obj, o)
                 shutil.rmtree(temps)
             if verbose and err.strip():
                 print(err, file=sys.stderr)

@@ -534,15 +534,14 @@ __global__ __launch_bounds__(64 * kW * kS, D == 128 && kQ == 2 ? 1 : 2) void pro
     const Seq seq{scalar(place.seq.n), scalar(place.seq.m), scalar(place.seq.q_first), scalar(place.seq.k_first)};
     const int n_rows = seq.n * a.group;                        // (the host holds it to 31 bits)
     const int r0 = tile * kRowsOf + 32 * kQ * wave;
-    int token[kQ], q_head[kQ], lim[kQ];                        // lim: rows that the lane's query sees (none: <= 0)
-#pragma unroll
-    for (int c = 0; c < kQ; ++c) {
-        const int row = min(r0 + 32 * c + col, n_rows - 1);
-        token[c] = row / a.group;
-        q_head[c] = head * a.group + row - token[c] * a.group;
-        lim[c] = min(token[c] + 1 + seq.m - seq.n, seq.m);
-    }
-    const int lim_min = __builtin_amdgcn_readlane(lim[0], 0), lim_max = __builtin_amdgcn_readlane(lim[kQ - 1], 31);
+    // the query of a lane: its token and q-head
+    struct Query { int token, head; };
+    const auto query = [&](int c, int col) __attribute__((always_inline)) {
+        const int row = min(r0 + 32 * c + col, n_rows - 1), token = row / a.group;
+        return Query{token, head * a.group + row - token * a.group};
+    };
+    const auto sees = [&](int token) __attribute__((always_inline)) { return min(token + 1 + seq.m - seq.n, seq.m); };    // rows (none: <= 0)
+    const int lim_min = scalar(sees(query(0, 0).token)), lim_max = scalar(sees(query(kQ - 1, 31).token));
     const int last_token = min(tile * kRowsOf + kRowsOf - 1, n_rows - 1) / a.group;
     const int rows_end = min(max(last_token + 1 + seq.m - seq.n, 0), seq.m);
     const int n_stages = (rows_end + kKv - 1) / kKv;
@@ -551,7 +550,8 @@ __global__ __launch_bounds__(64 * kW * kS, D == 128 && kQ == 2 ? 1 : 2) void pro
     frag_t qf[kQ][kFrags];
 #pragma unroll
     for (int c = 0; c < kQ; ++c) {
-        const T* q = reinterpret_cast<const T*>(a.q) + q_head[c] * a.q_sh + (a.q_start ? (seq.q_first + token[c]) * a.q_sn : b * a.q_sb + token[c] * a.q_sn);
+        const Query at = query(c, col);
+        const T* q = reinterpret_cast<const T*>(a.q) + at.head * a.q_sh + (a.q_start ? (seq.q_first + at.token) * a.q_sn : b * a.q_sb + at.token * a.q_sn);
 #pragma unroll
         for (int f = 0; f < kFrags; ++f) qf[c][f] = load_piece(q + (2 * f + half) * 8, a.q_wide);
     }
@@ -564,6 +564,7 @@ __global__ __launch_bounds__(64 * kW * kS, D == 128 && kQ == 2 ? 1 : 2) void pro
     const auto page_of = [&](int t) __attribute__((always_inline)) { return (int)(__umulhi(2u * (unsigned)t, a.page_magic) >> a.page_shift); };
     const auto look_up = [&](int batch, int trip) __attribute__((always_inline)) {
         if (batch < 0) return;
+        const int lane = lane_here();
 #pragma unroll
         for (int i = 0; i < kMine; ++i) {
             const int n = wave * kMine + i, it = batch * kBatch + n, t = min(it * kKv + lane, a.max_pages * a.page_size - 1), page = page_of(t);
@@ -590,91 +591,91 @@ __global__ __launch_bounds__(64 * kW * kS, D == 128 && kQ == 2 ? 1 : 2) void pro
     // A stage's rows go to LDS by kDma instructions, neighbouring ones of which are a wave's, in groups under one LDS address.
     constexpr int kDma = kLoadBytes / 1024, kLoads = kDma / kW, kGroup = kLoads < 4 ? kLoads : 4;
     static_assert(kDma % kW == 0 && kLoads % kGroup == 0 && (kGroup == 2 || kGroup == 4), "every wave has whole groups");
-    const auto row_of_load = [&](int i) __attribute__((always_inline)) { return (wave * kLoads + i) * St::kDmaRows + lane / St::kPieces; };
-    const auto key_piece = [&](int i) __attribute__((always_inline)) { return 16 * (lane % St::kPieces ^ St::key(row_of_load(i))); };
-    const auto value_piece = [&](int i) __attribute__((always_inline)) { return 16 * (lane % St::kPieces ^ St::value(row_of_load(i))); };
+    const auto row_of_load = [&](int i, int lane) __attribute__((always_inline)) { return (wave * kLoads + i) * St::kDmaRows + lane / St::kPieces; };
+    const auto key_piece = [&](int i, int lane) __attribute__((always_inline)) { return 16 * (lane % St::kPieces ^ St::key(row_of_load(i, lane))); };
+    const auto value_piece = [&](int i, int lane) __attribute__((always_inline)) { return 16 * (lane % St::kPieces ^ St::value(row_of_load(i, lane))); };
     const char* k_first = nullptr;                             // the sequence's rows
     const char* v_first = nullptr;
     const char* k_next = nullptr;                              // those of the stage that is loaded next
     const char* v_next = nullptr;
     const long long k_step = a.k_sn * (long long)sizeof(T), v_step = a.v_sn * (long long)sizeof(T);       // bytes from row to row
-    unsigned k_off[kLoads], v_off[kLoads];                     // from a stage's first row (the host holds strides to 24 bits)
+    // from a stage's first row (the host holds strides to 24 bits); held, but where the registers do not suffice
+    constexpr bool kHeld = D == 128 || kQ == 1;
+    const auto offset_of = [&](auto values_, int i, int lane) __attribute__((always_inline)) {
+        constexpr bool kValues = decltype(values_)::value;
+        return (unsigned)row_of_load(i, lane) * (unsigned)(kValues ? v_step : k_step) + (kValues ? value_piece(i, lane) : key_piece(i, lane)) + kDmaBias - 1024 * (i % kGroup);
+    };
+    unsigned k_off[kLoads], v_off[kLoads];
     if constexpr (!kPaged) {
         k_first = reinterpret_cast<const char*>(reinterpret_cast<const T*>(a.k) + (a.q_start ? 0 : b * a.k_sb) + head * a.k_sh + seq.k_first * a.k_sn);
         v_first = reinterpret_cast<const char*>(reinterpret_cast<const T*>(a.v) + (a.q_start ? 0 : b * a.v_sb) + head * a.v_sh + seq.k_first * a.v_sn);
         k_next = k_first + (long long)(hi * kKv - kRowsOfLoad) * k_step;
         v_next = v_first + (long long)(hi * kKv - kRowsOfLoad) * v_step;
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            k_off[i] = (unsigned)row_of_load(i) * (unsigned)k_step + key_piece(i) + kDmaBias - 1024 * (i % kGroup);
-            v_off[i] = (unsigned)row_of_load(i) * (unsigned)v_step + value_piece(i) + kDmaBias - 1024 * (i % kGroup);
-        }
+        for (int i = 0; i < kLoads; ++i) { k_off[i] = offset_of(std::false_type{}, i, lane); v_off[i] = offset_of(std::true_type{}, i, lane); }
     }
-    const auto load_rows = [&](int first, int kbuf, int vbuf) __attribute__((always_inline)) {       // kRowsOfLoad rows, of one stage
-        const unsigned k_to = scalar((int)(k_lds + kbuf * kLoadBytes)) + 1024 * kLoads * wave, v_to = scalar((int)(v_lds + vbuf * kLoadBytes)) + 1024 * kLoads * wave;
-        const int it = first / kKv;
+    // kRowsOfLoad rows of one stage from row `first` on, keys or values, to LDS at `to`
+    const auto load_rows = [&](auto values_, int first, unsigned to) __attribute__((always_inline)) {
+        constexpr bool kValues = decltype(values_)::value;
+        const int lane = lane_here();
+        const auto piece = [&](int i) __attribute__((always_inline)) { return kValues ? value_piece(i, lane) : key_piece(i, lane); };
+        const int it = first / kKv, mine = kLoads * wave;
+        to = scalar((int)to) + 1024 * mine;
+        typedef __attribute__((address_space(3))) frag_t* lds_frag_t;
         if constexpr (kPaged) {
-            if (live_of[it % kHold] == 0) {                  // nothing there: zeros, which count nothing
+            const char* rows = reinterpret_cast<const char*>(kValues ? a.v : a.k);
+            if (live_of[it % kHold] == 0) {                    // nothing there: zeros, which count nothing
 #pragma unroll
-                for (int i = 0; i < kLoads; ++i) {
-                    const int at = 1024 * (wave * kLoads + i) + 16 * lane;
-                    *reinterpret_cast<frag_t*>(&keys[kbuf][at]) = zero_frag();
-                    *reinterpret_cast<frag_t*>(&vals[vbuf * kLoadBytes + at]) = zero_frag();
-                }
+                for (int i = 0; i < kLoads; ++i) *(lds_frag_t)(uintptr_t)(to + 1024 * i + 16 * lane) = zero_frag();
                 return;
             }
 #pragma unroll
             for (int g = 0; g < kLoads; g += kGroup) {
-                const char *k[kGroup], *v[kGroup];
+                const char* from[kGroup];
 #pragma unroll
-                for (int i = 0; i < kGroup; ++i) {
-                    const unsigned long long at = (unsigned long long)(unsigned)row_of[it % kHold][first % kKv + row_of_load(g + i)] * St::kRowBytes;
-                    k[i] = reinterpret_cast<const char*>(a.k) + key_piece(g + i) - 1024 * i + at;
-                    v[i] = reinterpret_cast<const char*>(a.v) + value_piece(g + i) - 1024 * i + at;
-                }
-                dma_group<kGroup>(k, k_to + 1024 * g);
-                dma_group<kGroup>(v, v_to + 1024 * g);
+                for (int i = 0; i < kGroup; ++i)
+                    from[i] = rows + piece(g + i) - 1024 * i + (unsigned long long)(unsigned)row_of[it % kHold][first % kKv + row_of_load(g + i, lane)] * St::kRowBytes;
+                dma_group<kGroup>(from, to + 1024 * g);
             }
-        } else if (!rare(!a.kv_wide || first + kRowsOfLoad > seq.m)) {
+            return;
+        }
+        const char* rows = kValues ? v_first : k_first;
+        const long long step = kValues ? v_step : k_step;
+        const char*& next = kValues ? v_next : k_next;
+        if (!rare(!a.kv_wide || first + kRowsOfLoad > seq.m)) {
 #pragma unroll
             for (int g = 0; g < kLoads; g += kGroup) {
-                unsigned k[kGroup], v[kGroup];
+                unsigned off[kGroup];
 #pragma unroll
-                for (int i = 0; i < kGroup; ++i) { k[i] = k_off[g + i]; v[i] = v_off[g + i]; }
-                dma_group<kGroup>(k_next, k, k_to + 1024 * g);
-                dma_group<kGroup>(v_next, v, v_to + 1024 * g);
+                for (int i = 0; i < kGroup; ++i) off[i] = !kHeld ? offset_of(values_, g + i, lane) : kValues ? v_off[g + i] : k_off[g + i];
+                dma_group<kGroup>(next, off, to + 1024 * g);
             }
         } else if (a.kv_wide) {                                // rows past the last are read as the last
 #pragma unroll
             for (int g = 0; g < kLoads; g += kGroup) {
-                const char *k[kGroup], *v[kGroup];
+                const char* from[kGroup];
 #pragma unroll
                 for (int i = 0; i < kGroup; ++i) {
-                    const unsigned t = min(first + row_of_load(g + i), seq.m - 1);
-                    k[i] = k_first + t * (unsigned long long)(unsigned)k_step + key_piece(g + i) - 1024 * i;
-                    v[i] = v_first + t * (unsigned long long)(unsigned)v_step + value_piece(g + i) - 1024 * i;
+                    const unsigned t = min(first + row_of_load(g + i, lane), seq.m - 1);
+                    from[i] = rows + t * (unsigned long long)(unsigned)step + piece(g + i) - 1024 * i;
                 }
-                dma_group<kGroup>(k, k_to + 1024 * g);
-                dma_group<kGroup>(v, v_to + 1024 * g);
+                dma_group<kGroup>(from, to + 1024 * g);
             }
         } else {
 #pragma unroll 4
             for (int i = 0; i < kLoads; ++i) {
-                const long long t = min(first + row_of_load(i), seq.m - 1);
-                const int at = 1024 * (wave * kLoads + i) + 16 * lane;
-                *reinterpret_cast<frag_t*>(&keys[kbuf][at]) = load_piece(reinterpret_cast<const T*>(k_first + t * k_step + key_piece(i)), false);
-                *reinterpret_cast<frag_t*>(&vals[vbuf * kLoadBytes + at]) = load_piece(reinterpret_cast<const T*>(v_first + t * v_step + value_piece(i)), false);
+                const long long t = min(first + row_of_load(i, lane), seq.m - 1);
+                *(lds_frag_t)(uintptr_t)(to + 1024 * i + 16 * lane) = load_piece(reinterpret_cast<const T*>(rows + t * step + piece(i)), false);
             }
         }
-        k_next -= kRowsOfLoad * k_step;
-        v_next -= kRowsOfLoad * v_step;
+        next -= kRowsOfLoad * step;
     };
 
     // ---- the wave's state
     f32x16_t o[kQ][kOut], s[2][kQ];                            // s: of the step whose products run, and of the one before
     frag_t p[2][kQ][2];                                        // weights, the same way
     frag_t kf[kFrags], vf[2][kOut];
-    float m[kQ], l[kQ];                                        // of the lane's queries; l: this lane's rows only
+    float m[kQ], l[kQ];                                        // of the lane's queries (m: NaN before the first); l: this lane's rows only
 #pragma unroll
     for (int c = 0; c < kQ; ++c) {
 #pragma unroll
@@ -682,7 +683,7 @@ __global__ __launch_bounds__(64 * kW * kS, D == 128 && kQ == 2 ? 1 : 2) void pro
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[1][c][r] = -INFINITY;
         p[1][c][0] = p[1][c][1] = zero_frag();
-        m[c] = -INFINITY; l[c] = 0.f;
+        m[c] = NAN; l[c] = 0.f;
     }
 #pragma unroll
     for (int t = 0; t < 2; ++t)
@@ -720,7 +721,7 @@ __global__ __launch_bounds__(64 * kW * kS, D == 128 && kQ == 2 ? 1 : 2) void pro
     };
     // which of a step's rows 4 half + (0..3) + 8 (0..3) the lane's query sees, bit acc_row(r, 0)
     const auto seen = [&](const Step& st, int c) __attribute__((always_inline)) {
-        const int left = lim[c] - st.row;
+        const int lane = lane_here(), half = lane / 32, left = sees(query(c, lane % 32).token) - st.row;       // (formed anew, as below)
         return ((left >= 32 ? ~0u : left <= 0 ? 0u : (1u << left) - 1) & st.live) >> (4 * half);
     };
     const auto hide = [&](f32x16_t (&x)[kQ], const Step& st) __attribute__((always_inline)) {
@@ -785,9 +786,9 @@ __global__ __launch_bounds__(64 * kW * kS, D == 128 && kQ == 2 ? 1 : 2) void pro
             }
     };
     // The reference m stays where it is while the weights' sum has room: a row's weights are relative to it, and nothing is lost by
-    // their size.  Else it goes up to the largest logit, and the step's weights are formed again.
+    // their size.  Else it goes up to the largest logit, and the step's weights are formed again.  (A reference that is NaN makes a sum
+    // that has none: the first one is found this way.)
     constexpr float kRoom = 0x1p30f;
-    const auto has_room = [&](float sum, int c) __attribute__((always_inline)) { return sum <= kRoom && m[c] > -INFINITY; };
     const auto raise = [&](const f32x16_t (&x)[kQ], frag_t (&w)[kQ][2], float (&sum)[kQ]) __attribute__((always_inline)) {
         float shrink[kQ];
         bool shrinks = false;
@@ -797,10 +798,10 @@ __global__ __launch_bounds__(64 * kW * kS, D == 128 && kQ == 2 ? 1 : 2) void pro
 #pragma unroll
             for (int r = 1; r < 16; ++r) top = fmaxf(top, x[c][r]);
             top = fmaxf(m[c], halves_max(top) * a.scale_log2e);
-            const bool full = halves_max(has_room(sum[c], c) ? 0.f : 1.f) > 0.f;
-            const float m_new = full ? top : m[c], ref = m_new > -INFINITY ? m_new : 0.f;
-            shrink[c] = exp2_fast(m[c] - ref);                 // (what there is of a query without a reference is 0)
-            shrinks |= full && m[c] > -INFINITY;
+            const bool set = m[c] > -INFINITY, full = halves_max(sum[c] <= kRoom ? 0.f : 1.f) > 0.f;
+            const float m_new = !full ? m[c] : top > -INFINITY ? top : NAN, ref = m_new > -INFINITY ? m_new : 0.f;
+            shrink[c] = set ? exp2_fast(m[c] - ref) : 1.f;     // (what there is of a query without a reference is 0)
+            shrinks |= full && set;
             m[c] = m_new;
             sum[c] = 0.f;
 #pragma unroll
@@ -812,17 +813,23 @@ __global__ __launch_bounds__(64 * kW * kS, D == 128 && kQ == 2 ? 1 : 2) void pro
                     sum[c] += z;
                     y[e] = (bf16_t)z;
                 }
-                w[c][t] = __builtin_bit_cast(frag_t, y);
+                // (into the registers that hold the others: else every turn would move the one or the other)
+                const frag_t z = __builtin_bit_cast(frag_t, y);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    int to = w[c][t][e];
+                    asm volatile("v_mov_b32 %0, %1" : "+v"(to) : "v"(z[e]));
+                    w[c][t][e] = to;
+                }
             }
         }
         if (rare(__any(shrinks))) {
             settle_out();
 #pragma unroll
             for (int c = 0; c < kQ; ++c) {
-                const float f = m[c] > -INFINITY ? shrink[c] : 1.f;
-                l[c] *= f;
+                l[c] *= shrink[c];
 #pragma unroll
-                for (int i = 0; i < kOut; ++i) o[c][i] *= f;
+                for (int i = 0; i < kOut; ++i) o[c][i] *= shrink[c];
             }
         }
     };
@@ -855,11 +862,11 @@ __global__ __launch_bounds__(64 * kW * kS, D == 128 && kQ == 2 ? 1 : 2) void pro
         constexpr int cur = decltype(cur_)::value;
         if constexpr (kSome) begin(s[cur], live);
         settle_weights();
-        float sum[kQ], ref[kQ], y[kElems];
+        float sum[kQ], y[kElems];
 #pragma unroll
-        for (int c = 0; c < kQ; ++c) { sum[c] = 0.f; ref[c] = m[c] > -INFINITY ? m[c] : 0.f; }
+        for (int c = 0; c < kQ; ++c) sum[c] = 0.f;
         const auto element = [&](int e) __attribute__((always_inline)) {
-            if (e < kElems) y[e] = __builtin_fmaf(s[1 - cur][e / 16][e % 16], a.scale_log2e, -ref[e / 16]);
+            if (e < kElems) y[e] = __builtin_fmaf(s[1 - cur][e / 16][e % 16], a.scale_log2e, -m[e / 16]);
             if (e >= 1 && e - 1 < kElems) y[e - 1] = exp2_fast(y[e - 1]);
             if (e >= 2 && e - 2 < kElems) {
                 sum[(e - 2) / 16] += y[e - 2];
@@ -874,7 +881,7 @@ __global__ __launch_bounds__(64 * kW * kS, D == 128 && kQ == 2 ? 1 : 2) void pro
         for (int n = 0; n < kPv; ++n) {
             const int t = n / (kOut * kQ), i = n / kQ % kOut, c = n % kQ;
             add_out(o[c][i], vf[t][i], p[cur][c][t], std::false_type{});
-            if (n < kFrags) kf[n] = lds_frag((k_base + k_at) ^ (32 * n));
+            if (n >= kPv - kFrags) kf[n - (kPv - kFrags)] = lds_frag((k_base + k_at) ^ (32 * (n - (kPv - kFrags))));
 #pragma unroll
             for (int e = n * kElems / kSlots; e < (n + 1) * kElems / kSlots; ++e) element(e);
             __builtin_amdgcn_sched_barrier(0);
@@ -893,10 +900,8 @@ __global__ __launch_bounds__(64 * kW * kS, D == 128 && kQ == 2 ? 1 : 2) void pro
         }
         element(kElems);
         element(kElems + 1);
-        bool room = true;
-#pragma unroll
-        for (int c = 0; c < kQ; ++c) room &= has_room(sum[c], c);
-        if (rare(!__all(room))) raise(s[1 - cur], p[1 - cur], sum);
+        const float all = kQ == 2 ? sum[0] + sum[kQ - 1] : sum[0];
+        if (rare(__builtin_amdgcn_ballot_w64(!(all <= kRoom)) != 0)) raise(s[1 - cur], p[1 - cur], sum);
 #pragma unroll
         for (int c = 0; c < kQ; ++c) l[c] += sum[c];
     };
@@ -917,7 +922,10 @@ __global__ __launch_bounds__(64 * kW * kS, D == 128 && kQ == 2 ? 1 : 2) void pro
     }
     int kbuf = 0, vbuf = 0;
     unsigned v_prev = v_lds;                                   // values of the step before (any, where there is none)
-    if (hi > lo) load_rows(hi * kKv - kRowsOfLoad, 0, 0);
+    if (hi > lo) {
+        load_rows(std::false_type{}, hi * kKv - kRowsOfLoad, k_lds);
+        load_rows(std::true_type{}, hi * kKv - kRowsOfLoad, v_lds);
+    }
     const bool works = r0 < n_rows;
     bool begun = false;
     int it = hi - 1;
@@ -927,7 +935,7 @@ __global__ __launch_bounds__(64 * kW * kS, D == 128 && kQ == 2 ? 1 : 2) void pro
         wait_vmem<0>();
         if constexpr (kS == 1) {
             __syncthreads();
-            if (it > lo) load_rows((it - 1) * kKv, kbuf ^ 1, vnext);
+            if (it > lo) load_rows(std::false_type{}, (it - 1) * kKv, k_lds + (kbuf ^ 1) * kLoadBytes);
         }
         unsigned long long live = ~0ull;
         if constexpr (kPaged) {
@@ -940,14 +948,21 @@ __global__ __launch_bounds__(64 * kW * kS, D == 128 && kQ == 2 ? 1 : 2) void pro
                 else if (trip == 2) look_up(it / kBatch - 1, 2);
             }
         }
+        const auto load_values = [&]() __attribute__((always_inline)) {
+            if (kS == 1 && it > lo) load_rows(std::true_type{}, (it - 1) * kKv, v_lds + vnext * kLoadBytes);
+        };
         if (works && (!kTop || it * kKv < lim_max)) {
 #pragma unroll
             for (int j = 1; j >= 0; --j) {
                 if constexpr (kS > 1) {
                     wait_vmem<0>();
                     vnext = vbuf == 2 ? 0 : vbuf + 1;
-                    if (j == 1 || it > lo) load_rows(it * kKv + 32 * j - 32, kbuf ^ 1, vnext);
+                    if (j == 1 || it > lo) {
+                        load_rows(std::false_type{}, it * kKv + 32 * j - 32, k_lds + (kbuf ^ 1) * kLoadBytes);
+                        load_rows(std::true_type{}, it * kKv + 32 * j - 32, v_lds + vnext * kLoadBytes);
+                    }
                 }
+                if (j == 0) load_values();             // (a stage's loads in two parts: a burst of them holds the wave up)
                 const unsigned here = (unsigned)(live >> (32 * j)), k_at = k_lds + kbuf * kLoadBytes + (kS > 1 ? 0 : 32 * j * St::kRowBytes);
                 const bool edge = kTop && it * kKv + 32 * j + 32 > lim_min;
                 const Step now{it * kKv + 32 * j, here, edge, edge || (kPaged && !kSome && here != ~0u)};
@@ -964,6 +979,7 @@ __global__ __launch_bounds__(64 * kW * kS, D == 128 && kQ == 2 ? 1 : 2) void pro
                 if constexpr (kS > 1) { kbuf ^= 1; vbuf = vnext; }
             }
         }
+        else load_values();
         if constexpr (kS == 1) { kbuf ^= 1; vbuf = vnext; }
     };
     // the first stage and those that some query does not see whole, and one more for what is under way; then those that need no look
@@ -1001,6 +1017,8 @@ __global__ __launch_bounds__(64 * kW * kS, D == 128 && kQ == 2 ? 1 : 2) void pro
     }
     settle_out();
 
+#pragma unroll
+    for (int c = 0; c < kQ; ++c) m[c] = m[c] > -INFINITY ? m[c] : -INFINITY;
     if constexpr (kS > 1) {
         // the parts' results, where their rings were
         typedef float row_t[D + 4];
@@ -1046,25 +1064,29 @@ __global__ __launch_bounds__(64 * kW * kS, D == 128 && kQ == 2 ? 1 : 2) void pro
         return;
     }
 
-    // ---- the lane's queries: columns 32 i + acc_row(r, half)
+    // ---- the lane's queries: columns 32 i + acc_row(r, half)  (all that is derived from the lane's number is formed anew: nothing of
+    // it is held through the loops)
+    const int lane2 = lane_here(), col2 = lane2 % 32, half2 = lane2 / 32;
 #pragma unroll
     for (int c = 0; c < kQ; ++c) {
         const float total = halves_sum(l[c]);
+        const Query at = query(c, col2);
+        const bool here = r0 + 32 * c + col2 < n_rows;
         const float ref = m[c] > -INFINITY ? m[c] : 0.f;
-        const long long q_token = seq.q_first + token[c];
+        const long long q_token = seq.q_first + at.token;
         if (a.splits > 1) {
-            if (r0 + 32 * c + col >= n_rows) continue;
-            const long long at = (q_token * a.kv_heads * a.group + q_head[c]) * a.splits + split;
+            if (!here) continue;
+            const long long to = (q_token * a.kv_heads * a.group + at.head) * a.splits + split;
 #pragma unroll
             for (int i = 0; i < kOut; ++i)
 #pragma unroll
                 for (int r = 0; r < 16; r += 4)
-                    *reinterpret_cast<f32x4_t*>(a.part_o + at * D + 32 * i + acc_row(r, half)) = f32x4_t{o[c][i][r], o[c][i][r + 1], o[c][i][r + 2], o[c][i][r + 3]};
-            if (half == 0) { a.part_ml[2 * at] = m[c]; a.part_ml[2 * at + 1] = total; }
+                    *reinterpret_cast<f32x4_t*>(a.part_o + to * D + 32 * i + acc_row(r, half2)) = f32x4_t{o[c][i][r], o[c][i][r + 1], o[c][i][r + 2], o[c][i][r + 3]};
+            if (half2 == 0) { a.part_ml[2 * to] = m[c]; a.part_ml[2 * to + 1] = total; }
             continue;
         }
         const float inv = total == 0.f ? 0.f : 1.f / total;    // (NaN stays)
-        T* out = reinterpret_cast<T*>(a.out) + q_head[c] * a.o_sh + (a.q_start ? q_token * a.o_sn : b * a.o_sb + token[c] * a.o_sn);
+        T* out = reinterpret_cast<T*>(a.out) + at.head * a.o_sh + (a.q_start ? q_token * a.o_sn : b * a.o_sb + at.token * a.o_sn);
         // eight neighbouring elements a lane: four of its own and the four that the lane 32 away has
         frag_t pieces[kOut][2];
 #pragma unroll
@@ -1081,8 +1103,8 @@ __global__ __launch_bounds__(64 * kW * kS, D == 128 && kQ == 2 ? 1 : 2) void pro
                     pieces[i][q][x] = (int)both[0];
                     pieces[i][q][2 + x] = (int)both[1];
                 }
-        if (r0 + 32 * c + col >= n_rows) continue;
-        out += 8 * half;
+        if (!here) continue;
+        out += 8 * half2;
         if (a.o_wide) {
 #pragma unroll
             for (int i = 0; i < kOut; ++i)
@@ -1098,7 +1120,7 @@ __global__ __launch_bounds__(64 * kW * kS, D == 128 && kQ == 2 ? 1 : 2) void pro
                     for (int e = 0; e < 8; ++e) out[32 * i + 16 * q + e] = x[e];
                 }
         }
-        if (a.lse && half == 0) a.lse[(a.q_start ? q_token : b * a.l_sb + token[c]) + q_head[c] * a.l_sh] = (ref + log2_fast(total)) * 0.6931471805599453f;
+        if (a.lse && half2 == 0) a.lse[(a.q_start ? q_token : b * a.l_sb + at.token) + at.head * a.l_sh] = (ref + log2_fast(total)) * 0.6931471805599453f;
     }}
 
 // ---- joining
