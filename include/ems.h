@@ -490,7 +490,7 @@ int ems_paged_attention(const ems_paged_params* p, const ems_paged_cache* cache,
  *     out = sum_t p_t v_t / sum_t p_t        lse = ln sum_t p_t        p_t = exp(scale q.k_t), t <= lens[b] - n_b + i
  * A token-head that sees no live row gives zeros and -inf.  What masked rows, rows behind the length and rows that a
  * token does not see hold does not matter to it; infinities and NaN as in ems_paged_attention.
- *   n_new          tokens per sequence in q, >= 1 (B * n_new * Hq < 2^31)
+ *   n_new          tokens per sequence in q, >= 1 (B * n_new * Hq at most 2^30)
  *   lens           in : device [B] i32 rows of every sequence, its new tokens' among them (ems_paged_append's len_out)
  *   new_len_opt    in : device [B] i32 how many of the n_new tokens there are, or NULL = all.  What q holds behind
  *                       them is not read; what out and lse hold there is left as it is.
@@ -498,8 +498,8 @@ int ems_paged_attention(const ems_paged_params* p, const ems_paged_cache* cache,
  *                  inputs
  *   lse_opt        out: device [B, Hq, n_new] f32, or NULL
  *   ws             device scratch of at least ems_paged_chunk_workspace_bytes (of the same n_new)
- * 16-bit products take the weights p_t rounded to bf16, relative to the largest so far (the sum in the denominator
- * is of the weights themselves).  The result depends on nothing but the arguments.
+ * Weights enter 16-bit products rounded to bf16, half a step each at most (the sum in the denominator and lse are of
+ * the weights themselves); where n_new * Hq / Hkv is 32 or less, whole.  The result depends on nothing but the arguments.
  */
 int ems_paged_chunk_workspace_bytes(const ems_paged_params* p, int32_t n_new, size_t* chunk_ws);
 int ems_paged_chunk_attention(const ems_paged_params* p, const ems_paged_cache* cache, int32_t n_new,
@@ -514,7 +514,7 @@ int ems_paged_chunk_attention(const ems_paged_params* p, const ems_paged_cache* 
  * t <= i + m - n (so with n = m the usual causal mask, with n < m the queries are the last tokens of m):
  *     out = sum_t p_t v_t / sum_t p_t        lse = ln sum_t p_t        p_t = exp(scale q.k_t)
  * A query that sees no row gives zeros and -inf; what rows hold that a query does not see does not matter to it.
- * lse is what ems_global_local_score_from_lse takes.  Weights in 16-bit products as in ems_paged_chunk_attention.
+ * lse is what ems_global_local_score_from_lse takes.  Weights enter 16-bit products rounded to bf16, as above.
  *   q, out         device [B, Hq, q_rows, D] with any strides, or with q_start [Hq, q_rows, D] (the batch stride is
  *                  not used); out: every row in a place of its own, apart from the inputs
  *   k, v           in : device [B, Hkv, k_rows, D], or with q_start [Hkv, k_rows, D], any strides
@@ -531,8 +531,8 @@ typedef struct {
     int32_t q_heads;       /* Hq >= 1 */
     int32_t kv_heads;      /* Hkv >= 1, divides Hq */
     int32_t head_dim;      /* D in {64, 128} */
-    int32_t q_rows;        /* queries of every sequence, or of all of them together, >= 1 (B * Hq * q_rows < 2^31; */
-                           /*   together: (B + q_rows) * Hq < 2^31) */
+    int32_t q_rows;        /* queries of every sequence, or of all of them together, >= 1 (B * Hq * q_rows at most */
+                           /*   2^30; together: (B + q_rows) * Hq at most 2^30) */
     int32_t k_rows;        /* rows of keys and values, the same way, 0 .. 2^30 (0: k and v may be NULL) */
     float   softmax_scale; /* <= 0 means 1/sqrt(D) */
     int32_t dtype;         /* ems_dtype of q, k, v and out */

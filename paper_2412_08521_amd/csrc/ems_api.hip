@@ -902,8 +902,9 @@ static int many_queries(ems::PromptArgs& a, const PromptSizes& s, int head_dim, 
     return e == hipSuccess ? EMS_OK : EMS_ERR_LAUNCH;
 }
 
-// Blocks of a launch: less than 2^32 threads in x.
-static bool prompt_grid_ok(const ems::PromptPlan& plan, int kv_heads) { return plan.tiles * kv_heads * plan.waves < (1ll << 26); }
+// Blocks of 256 threads at most; query rows and what rounds them up to whole tiles are 32-bit numbers.
+static bool prompt_grid_ok(const ems::PromptPlan& plan, int kv_heads) { return plan.tiles * kv_heads < kMostBlocks; }
+constexpr long long kMostQueryRows = 1ll << 30;
 
 // Few columns (new tokens x q-heads of a kv-head) go by the kernel of single tokens, whose products have 32 of them at most.
 constexpr int kFewColumns = 2 * ems::kAttendQ;
@@ -925,7 +926,7 @@ static bool chunk_params_ok(const ems_paged_params* p, int32_t n_new, PromptSize
     *why = EMS_ERR_INVALID_ARG;
     if (n_new < 1) return false;
     *why = EMS_ERR_UNSUPPORTED;
-    if ((long long)p->batch * n_new > 0x7fffffffll / p->q_heads) return false;
+    if ((long long)p->batch * n_new > kMostQueryRows / p->q_heads) return false;
     const long long rows = (long long)n_new * (p->q_heads / p->kv_heads), tokens = (long long)p->batch * n_new;
     *s = prompt_sizes(ems::plan_prompt(p->batch, rows, p->batch * rows, p->kv_heads, p->q_heads / p->kv_heads, p->head_dim,
                                         (long long)p->max_pages * p->page_size, true, p->dtype == EMS_F32), tokens, p->q_heads, p->head_dim);
@@ -989,7 +990,7 @@ static bool prompt_params_ok(const ems_prompt_params* p, int* why)
     if (std::isnan(p->softmax_scale) || std::isinf(p->softmax_scale)) return false;
     *why = EMS_ERR_UNSUPPORTED;
     if (p->head_dim != 64 && p->head_dim != 128) return false;
-    return p->k_rows <= (1 << 30) && ((long long)p->batch + p->q_rows) * p->q_heads <= 0x7fffffffll;
+    return p->k_rows <= (1 << 30) && ((long long)p->batch + p->q_rows) * p->q_heads <= kMostQueryRows;
 }
 
 // (The workspace's size is asked for without the starts: it is what either form needs.)
@@ -1001,7 +1002,7 @@ static PromptSizes plan_prompts(const ems_prompt_params* p, bool packed)
                                         std::max(p->k_rows, 1), false, p->dtype == EMS_F32), tokens, p->q_heads, p->head_dim);
 }
 
-static bool dense_prompt_ok(const ems_prompt_params* p) { return (long long)p->batch * p->q_rows <= 0x7fffffffll / p->q_heads; }
+static bool dense_prompt_ok(const ems_prompt_params* p) { return (long long)p->batch * p->q_rows <= kMostQueryRows / p->q_heads; }
 
 int ems_prompt_workspace_bytes(const ems_prompt_params* p, size_t* prompt_ws)
 {

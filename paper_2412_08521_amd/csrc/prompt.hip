@@ -1,12 +1,24 @@
 // Attention of many queries: o_i = sum_t p_t v_t / sum_t p_t with p_t = exp(scale q_i.k_t - m), lse_i = m + ln sum_t p_t, over the
-// live rows t <= i + m - n that query i of n sees of m rows.  One pass with the running maximum m and sum.
+// live rows t <= i + m - n that query i of n sees of m rows.  One pass with a running reference m and sum.
 //
-// prompt_kernel  a block takes a tile of query rows of one kv-head, the group's q-heads of a token side by side (row token *
-//                group + head), 32 rows a wave, and walks the rows of keys and values in stages through LDS that all its
-//                waves read:
-//                  S^T = K Q^T    32x32 products; a lane holds one query's column, 16 of a tile's 32 rows
+// prompt_kernel  bfloat16.  A block takes a tile of query rows of one kv-head, the group's q-heads of a token side by side (row
+//                token * group + head), and walks the rows of keys and values in stages through LDS that all its waves read:
+//                  S^T = K Q^T    32x32x16 products; a lane holds one query's column, 16 of a tile's 32 rows
 //                  O^T = V^T P^T  S^T's registers are the right operand as they are; the left one is read transposed
-// prompt_join    a tile whose rows several blocks share: their outputs, weighted by their maxima and sums
+// prompt_f32     the same with 32-bit rows and products, plain
+// prompt_join    a tile whose rows several blocks share: their outputs, weighted by their references and sums
+//
+// What bounds it.  A 32x32x16 product takes a SIMD 8 passes (32 clocks) and needs, at 32 query rows a wave, 1 KiB of LDS; a tile
+// of 32 x 32 weights takes three and a half instructions a weight (multiply-add, exponential, sum, half a conversion) beside D/4 products.  64
+// query rows a wave halve the reads of LDS, and with products of one step beside the weights of another the matrix units
+// are what is left: 32 q-heads on 8, D = 128, a prompt of 32768 tokens takes 7.1 ms (1.24 PFLOP/s; a plain product of matrices
+// reaches 1.37 at its best size on the same card).  With one step at a time and one register tile it took 22.0 ms, with three in
+// flight 7.8 ms, with fewer instructions for addresses and edges 7.2 ms.  The same without the weights' instructions would run at
+// 1.47 PFLOP/s, without the loads of stages at 1.36; tiles drawn from a counter at run time gained 1.5 % at that size and lost 1 %
+// at 1024 tokens, so a block has one tile.
+//
+// The weights are rounded to bfloat16 for the second product (relative 2^-8 each, as the values and the output are); their sum is
+// of the 32-bit ones.
 #include <cmath>
 
 #include "ems_common.h"
@@ -61,7 +73,7 @@ __device__ __forceinline__ Place find_tile(const PromptArgs& a, int j, int rows_
         // tile t of a sequence has level base + t: the tiles' worth of rows that its queries see, about
         const Seq s = lane < a.batch ? sequence<kPaged>(a, lane) : Seq{0, 0, 0, 0};
         const int n = tiles_of_rows((long long)s.n * a.group, rows_of);
-        const int base = s.m > s.n ? (int)((long long)(s.m - s.n) * a.group / rows_of) : 0;
+        const int base = s.m > s.n ? (int)min((long long)(s.m - s.n) * a.group / rows_of, 1ll << 29) : 0;
         const auto from = [&](int level) { return total(min(max(base + n - level, 0), n)); };         // tiles of that level and above
         int lo = 0, hi = n ? base + n : 0;                     // from(lo) > j >= from(hi)
         for (int x = 1; x < kWave; x *= 2) hi = max(hi, __shfl_xor(hi, x));
@@ -158,14 +170,14 @@ __device__ __forceinline__ void dma16(const char* from, unsigned lds)
 
 // The same for two or four instructions on neighbouring KiB of LDS, from `base` on by 32-bit offsets or from 64-bit addresses.  An
 // instruction's own offset (0, 1024, ..) counts on both sides, so those that are passed are that much lower (kDmaBias higher).
-constexpr unsigned kDmaBias = 3072;
+constexpr unsigned kDmaBias = 3 * 1024;
 template <int kN>
 __device__ __forceinline__ void dma_group(const void* base, const unsigned (&off)[kN], unsigned lds)
 {
     const char* b = static_cast<const char*>(base) - kDmaBias;
     if constexpr (kN == 4)
         asm volatile("s_mov_b32 m0, %5\n\tglobal_load_lds_dwordx4 %0, %4\n\tglobal_load_lds_dwordx4 %1, %4 offset:1024\n\t"
-                     "global_load_lds_dwordx4 %2, %4 offset:2048\n\tglobal_load_lds_dwordx4 %3, %4 offset:3072"
+                     "global_load_lds_dwordx4 %2, %4 offset:2*1024\n\tglobal_load_lds_dwordx4 %3, %4 offset:3*1024"
                      ::"v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(b), "s"(lds) : "memory", "m0");
     else
         asm volatile("s_mov_b32 m0, %3\n\tglobal_load_lds_dwordx4 %0, %2\n\tglobal_load_lds_dwordx4 %1, %2 offset:1024"
@@ -176,7 +188,7 @@ __device__ __forceinline__ void dma_group(const char* const (&from)[kN], unsigne
 {
     if constexpr (kN == 4)
         asm volatile("s_mov_b32 m0, %4\n\tglobal_load_lds_dwordx4 %0, off\n\tglobal_load_lds_dwordx4 %1, off offset:1024\n\t"
-                     "global_load_lds_dwordx4 %2, off offset:2048\n\tglobal_load_lds_dwordx4 %3, off offset:3072"
+                     "global_load_lds_dwordx4 %2, off offset:2*1024\n\tglobal_load_lds_dwordx4 %3, off offset:3*1024"
                      ::"v"(from[0]), "v"(from[1]), "v"(from[2]), "v"(from[3]), "s"(lds) : "memory", "m0");
     else
         asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, off\n\tglobal_load_lds_dwordx4 %1, off offset:1024"
@@ -185,17 +197,21 @@ __device__ __forceinline__ void dma_group(const char* const (&from)[kN], unsigne
 
 }  // namespace
 
-template <typename T, int D, bool kPaged, int kW>
-__global__ __launch_bounds__(64 * kW, 2) void prompt_simple_kernel(PromptArgs a)
+// 32-bit rows: a wave takes a tile of 32 query rows, a stage is 32 rows, and its products come one after the other (32x32x2, a value
+// a lane).  The products bound it: 16 x the time of 16-bit ones, beside which the loads and weights do not show.
+template <int D, bool kPaged>
+__global__ __launch_bounds__(128, 2) void prompt_f32_kernel(PromptArgs a)
 {
+    typedef float T;
     using St = Stage<T, D>;
-    constexpr int kKv = St::kRows, kSubs = kKv / 32;
+    constexpr int kW = 2, kKv = St::kRows;
+    static_assert(kKv == 32, "a tile of rows");
     constexpr int kFrags = Tile<T, D>::kFrags, kOut = D / 32;
     constexpr int kRowsOf = 32 * kW;
     constexpr int kHold = 4;                                   // tiles whose rows are known
     __shared__ __align__(1024) char stage[2][2][St::kBytes];
     __shared__ int row_of[kPaged ? kHold : 1][kKv];
-    __shared__ unsigned long long live_of[kPaged ? kHold : 1];
+    __shared__ unsigned live_of[kPaged ? kHold : 1];
 
     const int lane = threadIdx.x % kWave, wave = scalar((int)threadIdx.x / kWave);
     const int col = lane % 32, half = lane / 32;
@@ -219,10 +235,7 @@ __global__ __launch_bounds__(64 * kW, 2) void prompt_simple_kernel(PromptArgs a)
     {
         const T* q = reinterpret_cast<const T*>(a.q) + q_head * a.q_sh + (a.q_start ? (seq.q_first + token) * a.q_sn : b * a.q_sb + token * a.q_sn);
 #pragma unroll
-        for (int f = 0; f < kFrags; ++f) {
-            const T* at = q + (2 * f + half) * (16 / (int)sizeof(T));
-            qf[f] = load_piece(at, a.q_wide);
-        }
+        for (int f = 0; f < kFrags; ++f) qf[f] = load_piece(q + (2 * f + half) * 4, a.q_wide);
     }
 
     // ---- rows of a stage
@@ -242,8 +255,8 @@ __global__ __launch_bounds__(64 * kW, 2) void prompt_simple_kernel(PromptArgs a)
     };
     const auto settle = [&](int it, int r, int mask) {
         if (mask < 0) r = kNoRow;
-        const unsigned long long live = __ballot(r != kNoRow);
-        const int spare = live ? __builtin_amdgcn_readlane(r, __builtin_ctzll(live)) : 0;
+        const unsigned live = (unsigned)__ballot(r != kNoRow); // (of lanes 0 .. 31: the others have no row)
+        const int spare = live ? __builtin_amdgcn_readlane(r, __builtin_ctz(live)) : 0;
         if (lane < kKv) row_of[it % kHold][lane] = r != kNoRow ? r : spare;
         if (lane == 0) live_of[it % kHold] = live;
     };
@@ -287,41 +300,27 @@ __global__ __launch_bounds__(64 * kW, 2) void prompt_simple_kernel(PromptArgs a)
     unsigned v_base[kOut];
 #pragma unroll
     for (int i = 0; i < kOut; ++i) {
-        const int r = 4 * half + lane % 16 / 4;
-        if constexpr (sizeof(T) == 2)
-            v_base[i] = lds + St::kBytes + r * St::kRowBytes + 16 * ((4 * i + 2 * (lane / 16 % 2) + lane % 4 / 2) ^ St::value(r)) + 8 * (lane % 2);
-        else
-            v_base[i] = lds + St::kBytes + 4 * half * St::kRowBytes + 4 * (32 * i + col);
+        v_base[i] = lds + St::kBytes + 4 * half * St::kRowBytes + 4 * (32 * i + col);
     }
     const auto lds_frag = [](unsigned at) { return *(const __attribute__((address_space(3))) frag_t*)(uintptr_t)at; };
     const auto lds_float = [](unsigned at) { return *(const __attribute__((address_space(3))) float*)(uintptr_t)at; };
 
-    const auto compute = [&](int it, int buf, auto masked, unsigned long long live, bool edge) {
+    const auto compute = [&](int it, int buf, auto masked, unsigned live, bool edge) {
         constexpr bool kMasked = decltype(masked)::value;
         const unsigned off = 2 * buf * St::kBytes;
-        f32x16_t s[kSubs];
+        f32x16_t s = zero_acc();
 #pragma unroll
-        for (int j = 0; j < kSubs; ++j) s[j] = zero_acc();
-#pragma unroll
-        for (int f = 0; f < kFrags; ++f)
-#pragma unroll
-            for (int j = 0; j < kSubs; ++j) mma<T>(s[j], lds_frag((k_base ^ (32 * f)) + off + 32 * j * St::kRowBytes), qf[f]);
-        unsigned seen[kSubs];
+        for (int f = 0; f < kFrags; ++f) mma<T>(s, lds_frag((k_base ^ (32 * f)) + off), qf[f]);
+        unsigned seen = 0;
         if constexpr (kMasked) {
             const int left = lim - it * kKv;                   // rows of this stage that the query sees
-            const unsigned long long bits = (left >= 64 ? ~0ull : left <= 0 ? 0ull : (1ull << left) - 1) & live;
+            seen = ((left >= 32 ? ~0u : left <= 0 ? 0u : (1u << left) - 1) & live) >> (4 * half);
 #pragma unroll
-            for (int j = 0; j < kSubs; ++j) {
-                seen[j] = (unsigned)(bits >> (32 * j)) >> (4 * half);
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[j][r] = (seen[j] >> acc_row(r, 0)) & 1 ? s[j][r] : -INFINITY;
-            }
+            for (int r = 0; r < 16; ++r) s[r] = (seen >> acc_row(r, 0)) & 1 ? s[r] : -INFINITY;
         }
-        float top = s[0][0];
+        float top = s[0];
 #pragma unroll
-        for (int j = 0; j < kSubs; ++j)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) top = fmaxf(top, s[j][r]);
+        for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);
         top = halves_max(top) * a.scale_log2e;
         // the reference stays until a logit exceeds it by 8 powers of two: sums and outputs have the room
         if (__any(top > m + 8.f)) {
@@ -334,104 +333,37 @@ __global__ __launch_bounds__(64 * kW, 2) void prompt_simple_kernel(PromptArgs a)
         }
         const float ref = m > -INFINITY ? m : 0.f;
 #pragma unroll
-        for (int j = 0; j < kSubs; ++j)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                s[j][r] = exp2_fast(__builtin_fmaf(s[j][r], a.scale_log2e, -ref));
-                l += s[j][r];
-            }
-        const auto value_frag = [&](int t, int i) {            // rows 16 t .. 16 t + 15 (16-bit)
-            const s16x4_t x = read_transposed(v_base[i] + off + 16 * t * St::kRowBytes);
-            const s16x4_t y = read_transposed(v_base[i] + off + (16 * t + 8) * St::kRowBytes);
-            return __builtin_bit_cast(frag_t, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
-        };
-        const auto value_row = [&](int j, int r, int i) { return lds_float(v_base[i] + off + (32 * j + acc_row(r, 0)) * St::kRowBytes); };
+        for (int r = 0; r < 16; ++r) {
+            s[r] = exp2_fast(__builtin_fmaf(s[r], a.scale_log2e, -ref));
+            l += s[r];
+        }
+        const auto value_row = [&](int r, int i) { return lds_float(v_base[i] + off + acc_row(r, 0) * St::kRowBytes); };
         // Where some query does not see a row, the row's value counts 0 times: an infinity or NaN there must not.  Such a stage
         // (hardly ever there) adds values that are finite, and sees by a second product which queries see one that is not.
         bool odd = false;
         if constexpr (kMasked) if (edge) {
-            if constexpr (sizeof(T) == 2) {
-                typedef short s16x8_t __attribute__((ext_vector_type(8)));
-                typedef unsigned short u16x8_t __attribute__((ext_vector_type(8)));
-                s16x8_t up = 0;
-                u16x8_t down = 0;
 #pragma unroll
-                for (int t = 0; t < 2 * kSubs; ++t)
+            for (int r = 0; r < 16; ++r)
 #pragma unroll
-                    for (int i = 0; i < kOut; ++i) {
-                        const frag_t x = value_frag(t, i);
-                        up = __builtin_elementwise_max(up, __builtin_bit_cast(s16x8_t, x));
-                        down = __builtin_elementwise_max(down, __builtin_bit_cast(u16x8_t, x));
-                    }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) odd |= up[e] >= 0x7f80 || down[e] >= 0xff80;
-            } else {
-#pragma unroll
-                for (int j = 0; j < kSubs; ++j)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-#pragma unroll
-                        for (int i = 0; i < kOut; ++i) odd |= !(fabsf(value_row(j, r, i)) < INFINITY);
-            }
+                for (int i = 0; i < kOut; ++i) odd |= !(fabsf(value_row(r, i)) < INFINITY);
             odd = __any(odd);
         }
-        if constexpr (sizeof(T) == 2) {
-            frag_t p[2 * kSubs];
 #pragma unroll
-            for (int t = 0; t < 2 * kSubs; ++t) {
-                bf16x8_t x;
+        for (int i = 0; i < kOut; ++i) {
+            f32x16_t count = zero_acc();
 #pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = (bf16_t)s[t / 2][8 * (t % 2) + e];
-                p[t] = __builtin_bit_cast(frag_t, x);
-            }
-            if (kMasked && odd) {
-#pragma unroll 1
-                for (int i = 0; i < kOut; ++i) {
-                    f32x16_t sum = zero_acc(), count = zero_acc();
-#pragma unroll
-                    for (int t = 0; t < 2 * kSubs; ++t) {
-                        bf16x8_t x = __builtin_bit_cast(bf16x8_t, value_frag(t, i)), not_finite, sees;
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const bool fine = fabsf((float)x[e]) < INFINITY;
-                            x[e] = fine ? x[e] : (bf16_t)0.f;
-                            not_finite[e] = (bf16_t)(fine ? 0.f : 1.f);
-                            sees[e] = (bf16_t)((seen[t / 2] >> acc_row(8 * (t % 2) + e, 0)) & 1 ? 1.f : 0.f);
-                        }
-                        mma<T>(sum, __builtin_bit_cast(frag_t, x), p[t]);
-                        mma<T>(count, __builtin_bit_cast(frag_t, not_finite), __builtin_bit_cast(frag_t, sees));
-                    }
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) sum[r] = count[r] > 0.f ? NAN : sum[r];
-#pragma unroll
-                    for (int n = 0; n < kOut; ++n) if (n == i) o[n] += sum;
+            for (int r = 0; r < 16; ++r) {
+                float x = value_row(r, i);
+                if (kMasked && odd) {
+                    const bool fine = fabsf(x) < INFINITY;
+                    count = __builtin_amdgcn_mfma_f32_32x32x2f32(fine ? 0.f : 1.f, (seen >> acc_row(r, 0)) & 1 ? 1.f : 0.f, count, 0, 0, 0);
+                    x = fine ? x : 0.f;
                 }
-            } else {
-#pragma unroll
-                for (int t = 0; t < 2 * kSubs; ++t)
-#pragma unroll
-                    for (int i = 0; i < kOut; ++i) mma<T>(o[i], value_frag(t, i), p[t]);
+                o[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, s[r], o[i], 0, 0, 0);
             }
-        } else {
+            if (kMasked && odd)
 #pragma unroll
-            for (int i = 0; i < kOut; ++i) {
-                f32x16_t count = zero_acc();
-#pragma unroll
-                for (int j = 0; j < kSubs; ++j)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        float x = value_row(j, r, i);
-                        if (kMasked && odd) {
-                            const bool fine = fabsf(x) < INFINITY;
-                            count = __builtin_amdgcn_mfma_f32_32x32x2f32(fine ? 0.f : 1.f, (seen[j] >> acc_row(r, 0)) & 1 ? 1.f : 0.f, count, 0, 0, 0);
-                            x = fine ? x : 0.f;
-                        }
-                        o[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, s[j][r], o[i], 0, 0, 0);
-                    }
-                if (kMasked && odd)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) o[i][r] = count[r] > 0.f ? NAN : o[i][r];
-            }
+                for (int r = 0; r < 16; ++r) o[i][r] = count[r] > 0.f ? NAN : o[i][r];
         }
     };
 
@@ -455,10 +387,9 @@ __global__ __launch_bounds__(64 * kW, 2) void prompt_simple_kernel(PromptArgs a)
         wait_vmem_all_visible();
         __syncthreads();
         if (it > lo) load_stage(it - 1, buf ^ 1);
-        unsigned long long live = ~0ull;
+        unsigned live = ~0u;
         if constexpr (kPaged) {
-            live = live_of[it % kHold];
-            live = ((unsigned long long)(unsigned)scalar((int)(live >> 32)) << 32) | (unsigned)scalar((int)live);
+            live = (unsigned)scalar((int)live_of[it % kHold]);
             if (wave == 0) {
                 settle(it - 2 + kHold, far, far_mask);
                 far = row_trip(it - 3, entry, far_mask);
@@ -466,10 +397,9 @@ __global__ __launch_bounds__(64 * kW, 2) void prompt_simple_kernel(PromptArgs a)
             }
         }
         if (r0 < n_rows && it * kKv < lim_max && live) {
-            const unsigned long long all = kKv == 64 ? ~0ull : (1ull << kKv) - 1;
             const bool edge = it * kKv + kKv > lim_min;
-            if (edge || (kPaged && live != all)) compute(it, buf, std::true_type{}, live, edge);
-            else compute(it, buf, std::false_type{}, live, false);
+            if (edge || (kPaged && live != ~0u)) compute(it, buf, std::true_type{}, live, edge);
+            else compute(it, buf, std::false_type{}, ~0u, false);
         }
     }
 
@@ -989,14 +919,14 @@ __global__ __launch_bounds__(64 * kW * kS, D == 128 && kQ == 2 ? 1 : 2) void pro
 
     // the last two steps' ends: weights of s[1], values of vf and of v_prev
     if (begun) {
-    if (before.shown) hide(s[1], before);
-    if (old.edge) take_out(old);
+        if (before.shown) hide(s[1], before);
+        if (old.edge) take_out(old);
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int i = 0; i < kOut; ++i)
+            for (int i = 0; i < kOut; ++i)
 #pragma unroll
-            for (int c = 0; c < kQ; ++c) add_out(o[c][i], vf[t][i], p[0][c][t], std::true_type{});
+                for (int c = 0; c < kQ; ++c) add_out(o[c][i], vf[t][i], p[0][c][t], std::true_type{});
         float sum[kQ];
 #pragma unroll
         for (int c = 0; c < kQ; ++c) sum[c] = INFINITY;        // (the weights are formed here)
@@ -1121,9 +1051,12 @@ __global__ __launch_bounds__(64 * kW * kS, D == 128 && kQ == 2 ? 1 : 2) void pro
                 }
         }
         if (a.lse && half2 == 0) a.lse[(a.q_start ? q_token : b * a.l_sb + at.token) + at.head * a.l_sh] = (ref + log2_fast(total)) * 0.6931471805599453f;
-    }}
+    }
+}
 
 // ---- joining
+
+// A thread has four columns of a query's output.
 
 template <typename T, int D, bool kPaged>
 __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a)
@@ -1168,11 +1101,17 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(PromptArgs a)
 
 // ---- launches
 
-// Rows of a block (256, 64 a wave; 128 or 64, 32 a wave; 32, whose waves share the rows of keys and values) and blocks that share a tile's rows of keys and values: what an estimate
-// of the time (us) finds least.  A compute unit takes `unit` for 32 query rows by 64 rows of keys and values where it has as
-// many blocks as fit; a block alone takes `stage` for 64 rows of them, and no call is shorter than its longest block; a join is a
-// launch and its traffic.  The figures are those of prompts of 77 to 4096 tokens, each size measured with each choice; where two
-// choices are near each other the estimate may take the other.
+// How a call is cut: rows of a block (256, 64 a wave; 128 or 64, 32 a wave; 32, whose waves share the rows of keys and values), and
+// blocks that share a tile's rows of keys and values.  It is what an estimate of the time (us) finds least.  A compute unit takes
+// `unit` for 32 query rows by 64 rows of keys and values where it has as many blocks as fit; a block alone takes `stage` for 64
+// rows of them, and no call is shorter than its longest block; a join is a launch and its traffic.  The figures are those of prompts
+// of 77 to 8192 tokens, each size measured with each choice (us; waves of 32 rows):
+//     8 q-heads on 8, D 128, 2048 tokens      1: 26.9   2, split in 2: 34.9
+//     8 q-heads on 2, D 64, 4096 tokens       1: 34.9   2: 44.9
+//     64 tokens behind 8128                   1, split in 8: 27.2   16: 30.4
+//     32 q-heads on 8, D 128, 2048 tokens     2: 51   4: 52   8: 63
+//     the same, 4096 tokens                   4: 144   8: 152   (from 8192 on 8 waves' rows are best: 0.21 against 0.27 a unit)
+// Where two choices are near each other the estimate may take the other.
 PromptPlan plan_prompt(long long sequences, long long rows, long long all_rows, int kv_heads, int group, int head_dim, long long most, bool paged, bool f32)
 {
     PromptPlan best{};
@@ -1194,7 +1133,7 @@ PromptPlan plan_prompt(long long sequences, long long rows, long long all_rows, 
     double least = 0.;
     for (const Cost& c : head_dim == 128 ? kWide : kNarrow) {
         const long long n = tiles(c.waves);
-        for (int splits = 1; splits <= 16 && (splits == 1 || most >= 256 * splits); splits *= 2) {
+        for (int splits = 1; splits <= 16 && (splits == 1 || (most >= 256 * splits && all_rows * kv_heads <= 1 << 22)); splits *= 2) {
             const double blocks = (double)n * kv_heads * splits;
             const double whole = (double)all_rows / 32 * kv_heads * stages * seen * c.unit / 256;
             const int fit = paged ? c.fit_paged : c.fit;
@@ -1234,13 +1173,10 @@ hipError_t launch(PromptArgs a, const PromptPlan& plan, hipStream_t st)
     a.splits = plan.splits;
     const dim3 grid((unsigned)(plan.tiles * a.kv_heads), plan.splits);
     if constexpr (sizeof(T) == 2) {
-        if (kPaged && a.pos_pages) launch_tiles<D, kPaged, kPaged>(a, plan.waves, grid, st);
+        if (kPaged && a.pos_pages) launch_tiles<D, kPaged, kPaged>(a, plan.waves, grid, st);      // (kSome only with kPaged)
         else launch_tiles<D, kPaged, false>(a, plan.waves, grid, st);
     } else {
-        if (plan.waves == 8) prompt_simple_kernel<T, D, kPaged, 8><<<grid, 512, 0, st>>>(a);
-        else if (plan.waves == 4) prompt_simple_kernel<T, D, kPaged, 4><<<grid, 256, 0, st>>>(a);
-        else if (plan.waves == 2) prompt_simple_kernel<T, D, kPaged, 2><<<grid, 128, 0, st>>>(a);
-        else prompt_simple_kernel<T, D, kPaged, 1><<<grid, 64, 0, st>>>(a);
+        prompt_f32_kernel<D, kPaged><<<grid, 128, 0, st>>>(a);
     }
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && a.splits > 1) {

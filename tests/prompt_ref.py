@@ -42,3 +42,39 @@ def attention_rows(q, k, v, seen, scale, dtype):
 def causal(n, m):
     """Query i of n sees rows t <= i + m - n of m."""
     return torch.arange(m)[None] <= torch.arange(n)[:, None] + (m - n)
+
+
+def plan(batch, q_heads, kv_heads, head_dim, q_rows, k_rows, packed=False, paged=False, f32=False):
+    """(waves of a block's rows, blocks that share a tile's rows of keys and values) that a call takes: the launcher's own choice."""
+    import ctypes as C
+
+    from paper_2412_08521_amd import binding as B
+
+    class Plan(C.Structure):
+        _fields_ = [("waves", C.c_int), ("splits", C.c_int), ("tiles", C.c_longlong)]
+    f = getattr(B.lib(), "_ZN3ems11plan_promptExxxiiixbb")
+    f.restype = Plan
+    f.argtypes = [C.c_longlong] * 3 + [C.c_int] * 3 + [C.c_longlong, C.c_bool, C.c_bool]
+    g = q_heads // kv_heads
+    p = f(batch, q_rows * g, q_rows * g if packed else batch * q_rows * g, kv_heads, g, head_dim, max(k_rows, 1), paged, f32)
+    return p.waves, p.splits
+
+
+# Calls that take each choice of plan(): float32, head size, sequences, q-heads, kv-heads, queries and rows of a sequence, the choice.
+CHOICES = [
+    (False, 64, 1, 4, 4, 300, 300, (1, 1)), (False, 64, 1, 32, 8, 40, 3000, (1, 4)), (False, 64, 1, 4, 4, 40, 3000, (1, 8)),
+    (False, 64, 1, 4, 4, 33, 33, (2, 1)), (False, 64, 4, 16, 8, 520, 1000, (4, 1)), (False, 64, 8, 32, 8, 200, 2000, (8, 1)),
+    (False, 128, 1, 4, 4, 300, 300, (1, 1)), (False, 128, 1, 4, 4, 200, 2000, (1, 4)), (False, 128, 1, 4, 4, 40, 3000, (1, 8)),
+    (False, 128, 1, 4, 4, 33, 33, (2, 1)), (False, 128, 4, 16, 8, 520, 1000, (4, 1)), (False, 128, 1, 4, 4, 4097, 4097, (4, 2)),
+    (False, 128, 8, 32, 8, 200, 2000, (8, 1)),
+    (True, 64, 4, 16, 8, 520, 1000, (2, 1)), (True, 128, 1, 4, 4, 200, 2000, (2, 8)),
+]
+CHUNK_CHOICES = [
+    (False, 64, 1, 4, 4, 300, 304, (1, 1)), (False, 64, 1, 4, 4, 40, 3008, (1, 8)), (False, 64, 1, 4, 4, 33, 48, (2, 1)),
+    (False, 64, 8, 32, 8, 40, 3008, (2, 2)), (False, 64, 4, 16, 8, 520, 1008, (4, 1)), (False, 64, 8, 32, 8, 200, 2000, (8, 1)),
+    (False, 128, 1, 4, 4, 300, 304, (1, 1)), (False, 128, 2, 8, 8, 200, 2000, (1, 2)), (False, 128, 1, 4, 4, 200, 2000, (1, 4)),
+    (False, 128, 1, 4, 4, 40, 3008, (1, 8)), (False, 128, 1, 4, 4, 33, 48, (2, 1)), (False, 128, 1, 32, 8, 40, 3008, (2, 8)),
+    (False, 128, 8, 32, 8, 100, 112, (4, 1)), (False, 128, 4, 16, 8, 200, 2000, (4, 2)), (False, 128, 4, 16, 8, 40, 3008, (4, 8)),
+    (False, 128, 8, 32, 8, 500, 512, (8, 1)),
+    (True, 64, 4, 16, 8, 520, 1008, (2, 1)), (True, 128, 1, 4, 4, 200, 2000, (2, 8)),
+]

@@ -7,7 +7,7 @@ import pytest
 import torch
 
 from paged_ref import assert_within, gather, pages_of
-from prompt_ref import attention_rows, causal
+from prompt_ref import CHOICES, CHUNK_CHOICES, attention_rows, causal
 from paper_2412_08521_amd import binding as B
 
 pytestmark = pytest.mark.gpu
@@ -57,7 +57,7 @@ class Rms:
 
 
 def _prompt_case(lens, hq, hkv, d, mode, before=None, packed=False, layout="tokens", out_layout="tokens", spare=(0, 0), seed=0,
-                 scale=0.0, poison=False, hot=1.0):
+                 scale=0.0, poison=False, hot=1.0, heads=None):
     """lens: queries of every sequence; before: rows of keys and values before them (may be negative: fewer rows than queries)."""
     dt = _dtype(mode)
     gen = torch.Generator().manual_seed(seed)
@@ -89,7 +89,7 @@ def _prompt_case(lens, hq, hkv, d, mode, before=None, packed=False, layout="toke
     o, z, g, rms = od.cpu(), lse.cpu(), hq // hkv, Rms()
     for i in range(b):
         qs, ks = (slice(q_at[i], q_at[i + 1]), slice(k_at[i], k_at[i + 1])) if packed else ((i,), (i,))
-        for h in range(hq):
+        for h in heads or range(hq):
             seen = causal(lens[i], rows[i])
             ki, vi = k[ks][..., h // g, :], v[ks][..., h // g, :]
             fine = torch.ones(lens[i], dtype=torch.bool)
@@ -130,6 +130,8 @@ def _prompt_case(lens, hq, hkv, d, mode, before=None, packed=False, layout="toke
     dict(lens=[0, 40, 0], hq=2, hkv=2, d=64, packed=True, spare=(3, 0), layout="odd", out_layout="odd"),
     dict(lens=[40, 300, 5, 64], hq=7, hkv=1, d=128, packed=True, layout="heads", out_layout="wide", before=[0, 1, 2, 3]),
     dict(lens=[9, 2], hq=4, hkv=2, d=128, packed=True, before=[4000, 2500]),
+    dict(lens=[i * 7 % 71 for i in range(100)], hq=4, hkv=2, d=64, packed=True, spare=(2, 1)),     # more sequences than lanes
+    dict(lens=[1, 0, 40] * 30, hq=2, hkv=1, d=128, packed=True, before=[0, 5, -3] * 30),
 ])
 def test_prompt_matches_64_bits(case, mode):
     _log("prompt", case, mode)
@@ -161,10 +163,20 @@ def test_prompt_rows_that_a_query_does_not_see_may_hold_anything(n, mode):
     _prompt_case([n], 2, 2, 64, mode, poison=True, before=[77])
 
 
+KINDS = [dict(), dict(poison=True), dict(hot=25.0)]
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("f32,d,b,hq,hkv,n,m,choice", CHOICES)
+def test_prompt_by_every_choice_of_blocks(f32, d, b, hq, hkv, n, m, choice, kind):
+    _log("prompt", f32, d, b, hq, hkv, n, m, choice, kind)
+    _prompt_case([n] * b, hq, hkv, d, F32 if f32 else BF16, before=[m - n] * b, heads=sorted({0, hq // 2, hq - 1}), **kind)
+
+
 # ---- chunks over pages
 
 def _chunk_case(n, lens, hq, hkv, d, ps, mode, new_len=None, masked=0.0, layout="tokens", out_layout="tokens", bad_pages=False, seed=0,
-                poison=False, whole_mask=False):
+                poison=False, whole_mask=False, hot=1.0, heads=None):
     dt = _dtype(mode)
     gen = torch.Generator().manual_seed(seed)
     b = len(lens)
@@ -190,7 +202,7 @@ def _chunk_case(n, lens, hq, hkv, d, ps, mode, new_len=None, masked=0.0, layout=
     if poison:                                              # nor what is behind a length
         rows = ~used[:, None].expand(pool, hkv, ps)
         kp[rows], vp[rows] = math.nan, math.nan
-    q = torch.randn((b, n, hq, d), generator=gen).to(dt)
+    q = torch.randn((b, n, hq, d), generator=gen).to(dt) * hot
     t = lambda x: x.transpose(1, 2)  # noqa: E731
     qd, od = t(_laid_out(q, layout)), t(_laid_out(torch.full((b, n, hq, d), 7.0, dtype=dt), out_layout))
     lse = torch.full((b, hq, n), 7.0).cuda()
@@ -203,7 +215,7 @@ def _chunk_case(n, lens, hq, hkv, d, ps, mode, new_len=None, masked=0.0, layout=
     safe = table.clamp(0, pool - 1)
     there = (table >= 0) & (table < pool)
     for i, m in enumerate(lens):
-        for h in range(hq):
+        for h in heads or range(hq):
             live = there[i].repeat_interleave(ps)[:m]
             if pos is not None:
                 live = live & (gather(pos[..., None], safe[i], h // g, m)[:, 0] >= 0)
@@ -233,6 +245,8 @@ def _chunk_case(n, lens, hq, hkv, d, ps, mode, new_len=None, masked=0.0, layout=
     dict(n=70, lens=[300, 70], hq=4, hkv=2, d=64, ps=8, masked=0.3, whole_mask=True),
     dict(n=4, lens=[100, 200], hq=4, hkv=2, d=128, ps=16, bad_pages=True),
     dict(n=60, lens=[100, 200], hq=4, hkv=2, d=64, ps=16, bad_pages=True, masked=0.2),
+    dict(n=20, lens=[i * 13 % 97 for i in range(70)], hq=4, hkv=2, d=64, ps=16, new_len=[i * 5 % 23 for i in range(70)]),
+    dict(n=20, lens=[i * 13 % 97 for i in range(70)], hq=4, hkv=2, d=128, ps=7),
 ])
 def test_chunk_matches_64_bits(case, mode):
     _log("chunk", case, mode)
@@ -264,3 +278,49 @@ def test_chunks_of_one_token_are_the_attention_of_one_token():
         assert (z1 - zn[..., 0]).abs().max() < 1e-5
         off = (one.double() - many[:, :, 0].double()).norm() / one.double().norm()
         assert off < (2.0 ** -7 if mode == BF16 else 1e-5), off
+
+
+@pytest.mark.parametrize("kind", [dict(), dict(masked=0.3, poison=True), dict(hot=25.0), dict(hot=25.0, masked=0.9)])
+@pytest.mark.parametrize("f32,d,b,hq,hkv,n,m,choice", CHUNK_CHOICES)
+def test_chunk_by_every_choice_of_blocks(f32, d, b, hq, hkv, n, m, choice, kind):
+    _log("chunk", f32, d, b, hq, hkv, n, m, choice, kind)
+    lens = [max(n, m - 150 * i) for i in range(b)]
+    _chunk_case(n, lens, hq, hkv, d, 16, F32 if f32 else BF16, heads=sorted({0, hq // 2, hq - 1}), **kind)
+
+
+# ---- addresses that 32 bits do not hold
+
+def test_prompt_with_sequences_far_apart():
+    gen = torch.Generator().manual_seed(4)
+    n, h, d, far = 300, 2, 128, (1 << 31) + 512             # elements from sequence to sequence: 4 GiB and some
+    p = B.PromptParams(2, h, h, d, n, n)
+    near = [torch.randn((2, h, n, d), generator=gen).to(torch.bfloat16).cuda() for _ in range(3)]
+    want, z = B.ems_prompt_attention(p, *near, want_lse=True)
+    apart = []
+    for x in near + [torch.zeros_like(want)]:
+        apart.append(torch.empty(far + n * h * d, dtype=torch.bfloat16, device="cuda").as_strided((2, h, n, d), (far, d, h * d, 1)))
+        apart[-1].copy_(x)
+    got, zg = B.ems_prompt_attention(p, *apart[:3], want_lse=True, out=(apart[3], torch.empty_like(z)))
+    assert torch.equal(got, want) and torch.equal(zg, z)
+
+
+@pytest.mark.parametrize("n", [3, 200])
+def test_chunks_of_a_large_pool(n):
+    """Pages whose bytes are past 2^32 give what pages at the pool's beginning do."""
+    gen = torch.Generator().manual_seed(5)
+    b, hq, h, d, ps, pool = 2, 8, 2, 128, 16, 1 << 20       # 8 GiB of keys
+    lens = torch.tensor([700, 333], dtype=torch.int32).cuda()
+    low = torch.randperm(88, generator=gen).view(2, 44).to(torch.int32).cuda()
+    q = torch.randn((b, hq, n, d), generator=gen).to(torch.bfloat16).cuda()
+    few = B.PagedParams(b, hq, h, d, ps, 88, 44)
+    kp, vp = (torch.randn((88, h, ps, d), generator=gen).to(torch.bfloat16).cuda() for _ in range(2))
+    pos = torch.where(torch.rand((88, h, ps), generator=gen) < 0.2, -1, 0).to(torch.int32).cuda()
+    many = B.PagedParams(b, hq, h, d, ps, pool, 44)
+    big = [torch.empty((pool,) + x.shape[1:], dtype=x.dtype, device="cuda") for x in (kp, vp, pos)]
+    for x, y in zip(big, (kp, vp, pos)):
+        x[-88:] = y
+    for i in (2, 3):                                        # without and with positions
+        mask = lambda x: x if i == 3 else None  # noqa: E731
+        want = B.ems_paged_chunk_attention(few, B.PagedCache(few, kp, vp, low, positions=mask(pos)), lens, q)
+        got = B.ems_paged_chunk_attention(many, B.PagedCache(many, big[0], big[1], low + (pool - 88), positions=mask(big[2])), lens, q)
+        assert torch.equal(got, want)

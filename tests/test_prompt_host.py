@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from paged_ref import attention
-from prompt_ref import attention_rows, causal
+from prompt_ref import CHOICES, CHUNK_CHOICES, attention_rows, causal, plan
 from quant_ref import codes, exponent, top_of
 from paper_2412_08521_amd import binding as B
 
@@ -220,3 +220,41 @@ def test_plain_codes_are_those_of_the_format():
     assert (top_of(x).double() > 224 * torch.exp2(s.double()))[up].all() and s[7] == -126
     near = (x.double() * torch.exp2(-s.double())[:, None]).float().to(torch.float8_e4m3fn).float().double()
     assert torch.equal(codes(x, s), near)                  # torch's own rounding
+
+
+# ---- how a call is cut
+
+def test_the_choices_of_blocks_are_reached():
+    """The cases that stand for a choice take it, and a call needs a workspace where blocks share a tile's rows (a prompt's size is
+    that of packed sequences too, which may share where these do not)."""
+    for paged, cases in ((False, CHOICES), (True, CHUNK_CHOICES)):
+        for f32, d, b, hq, hkv, n, m, choice in cases:
+            assert plan(b, hq, hkv, d, n, m, paged=paged, f32=f32) == choice, (paged, f32, d, b, hq, hkv, n, m)
+            mode = B.EMS_F32 if f32 else B.EMS_BF16
+            if paged:
+                assert m % 16 == 0
+                need = B.ems_paged_chunk_workspace_bytes(B.PagedParams(b, hq, hkv, d, 16, 100, m // 16, dtype=mode), n)
+            else:
+                need = B.ems_prompt_workspace_bytes(B.PromptParams(b, hq, hkv, d, n, m, dtype=mode))
+            assert need > 0 or choice[1] == 1
+            assert not paged or need == 0 or choice[1] > 1
+
+
+def test_any_size_has_a_choice():
+    gen = torch.Generator().manual_seed(11)
+    for _ in range(3000):
+        x = (2.0 ** (torch.rand(6, generator=gen, dtype=torch.float64) * torch.tensor([10, 5, 5, 20, 26, 2]))).long().tolist()
+        b, hkv, group, n, m, d = x[0], x[1], x[2], x[3], x[4], 64 * min(x[5], 2)
+        for paged in (False, True):
+            for f32 in (False, True):
+                waves, splits = plan(b, hkv * group, hkv, d, n, m, paged=paged, f32=f32)
+                assert waves in ((2,) if f32 else (1, 2, 4, 8)) and 1 <= splits <= 16 and (splits == 1 or 128 * splits <= m)
+
+
+def test_sizes_that_no_grid_holds_are_refused():
+    most = 1 << 30                                          # query rows of a kv-head and sequence; rows of keys
+    assert _call_prompt(_prompt(q_heads=2, q_rows=most + 1, k_rows=10), ws=None) == UNSUPPORTED
+    assert _call_prompt(_prompt(q_heads=4, q_rows=most // 2 + 1, k_rows=10), ws=None) == UNSUPPORTED
+    assert _call_prompt(_prompt(k_rows=most + 1), ws=None) == UNSUPPORTED
+    assert _call_chunk(_paged(), n_new=most, ws=None) == UNSUPPORTED
+    assert _call_chunk(_paged(q_heads=200, kv_heads=2), n_new=most // 100 + 1, ws=None) == UNSUPPORTED
