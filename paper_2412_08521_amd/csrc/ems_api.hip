@@ -184,7 +184,7 @@ bool ws_ok(const void* ws, size_t have, size_t need)
 
 extern "C" {
 
-int ems_version(void) { return 300; }
+int ems_version(void) { return 400; }
 
 const char* ems_strerror(int status)
 {
