@@ -514,7 +514,9 @@ int ems_paged_chunk_attention(const ems_paged_params* p, const ems_paged_cache* 
  * t <= i + m - n (so with n = m the usual causal mask, with n < m the queries are the last tokens of m):
  *     out = sum_t p_t v_t / sum_t p_t        lse = ln sum_t p_t        p_t = exp(scale q.k_t)
  * A query that sees no row gives zeros and -inf; what rows hold that a query does not see does not matter to it.
- * lse is what ems_global_local_score_from_lse takes.  Weights enter 16-bit products rounded to bf16, as above.
+ * lse is what ems_global_local_score_from_lse takes.  Weights enter 16-bit products rounded to bf16, as above.  They are
+ * relative to a reference that may lie below the largest logit, so values of a modulus past 2^70 may overflow the 32-bit
+ * sums (here and in the attention of chunks) where their quotient would not.
  *   q, out         device [B, Hq, q_rows, D] with any strides, or with q_start [Hq, q_rows, D] (the batch stride is
  *                  not used); out: every row in a place of its own, apart from the inputs
  *   k, v           in : device [B, Hkv, k_rows, D], or with q_start [Hkv, k_rows, D], any strides
