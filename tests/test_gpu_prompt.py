@@ -324,3 +324,61 @@ def test_chunks_of_a_large_pool(n):
         want = B.ems_paged_chunk_attention(few, B.PagedCache(few, kp, vp, low, positions=mask(pos)), lens, q)
         got = B.ems_paged_chunk_attention(many, B.PagedCache(many, big[0], big[1], low + (pool - 88), positions=mask(big[2])), lens, q)
         assert torch.equal(got, want)
+
+
+# ---- graphs
+
+def test_graphs_that_share_a_workspace():
+    """Two captured calls whose blocks share tiles, with one workspace, replayed in turn, eager calls between them."""
+    gen = torch.Generator().manual_seed(6)
+    pp, p = B.PromptParams(1, 4, 4, 128, 40, 3000), B.PagedParams(1, 4, 4, 128, 16, 200, 188)
+    need = max(B.ems_prompt_workspace_bytes(pp), B.ems_paged_chunk_workspace_bytes(p, 50))
+    assert B.ems_prompt_workspace_bytes(pp) > 0 and B.ems_paged_chunk_workspace_bytes(p, 50) > 0
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    q, k, v, qc = (torch.zeros((1, 4, m, 128), dtype=torch.bfloat16, device="cuda") for m in (40, 3000, 3000, 50))
+    table = torch.randperm(200, generator=gen)[:188].view(1, 188).to(torch.int32).cuda()
+    cache = B.PagedCache(p, *(torch.randn((200, 4, 16, 128), generator=gen).to(torch.bfloat16).cuda() for _ in range(2)), table)
+    lens = torch.tensor([2999], dtype=torch.int32).cuda()
+    outs = [torch.zeros_like(q), torch.zeros_like(qc)]
+    calls = [lambda o, w: B.ems_prompt_attention(pp, q, k, v, ws=w, out=(o, None)),
+             lambda o, w: B.ems_paged_chunk_attention(p, cache, lens, qc, ws=w, out=(o, None))]
+    other = torch.empty_like(ws)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        for call, o in zip(calls, outs):
+            call(o, ws)
+    torch.cuda.current_stream().wait_stream(s)
+    torch.cuda.synchronize()
+    graphs = []
+    for call, o in zip(calls, outs):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            call(o, ws)
+        graphs.append(g)
+    for _ in range(4):
+        for t in (q, k, v, qc):
+            t.copy_(torch.randn(t.shape, generator=gen).to(torch.bfloat16))
+        want = [torch.full_like(o, 5.0) for o in outs]
+        for call, o in zip(calls, want):
+            call(o, other)
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for got, ref in zip(outs, want):
+            assert torch.equal(got, ref)
+
+
+@pytest.mark.parametrize("mode", [BF16, F32])
+def test_prompt_of_large_values(mode):
+    """Values of 2^69 and logits that rise from row to row: sums that stay in 32 bits."""
+    gen = torch.Generator().manual_seed(7)
+    n, d = 700, 128
+    q, k, v = (torch.randn((1, 2, n, d), generator=gen).to(_dtype(mode)) for _ in range(3))
+    v = (torch.sign(v) * 2.0 ** 69).to(v.dtype)
+    q = q * 8
+    p = B.PromptParams(1, 2, 2, d, n, n, dtype=mode)
+    out = B.ems_prompt_attention(p, q.cuda(), k.cuda(), v.cuda()).cpu()
+    for h in range(2):
+        ref, _, bound, _, _ = attention_rows(q[0, h], k[0, h], v[0, h], causal(n, n), d ** -0.5, _dtype(mode))
+        assert_within(out[0, h], ref, bound, f"head {h}")
