@@ -894,7 +894,8 @@ __global__ __launch_bounds__(64 * kW * kS, D == 128 && kQ == 2 ? 1 : 2) void pro
                 }
                 if (j == 0) load_values();             // (a stage's loads in two parts: a burst of them holds the wave up)
                 const unsigned here = (unsigned)(live >> (32 * j)), k_at = k_lds + kbuf * kLoadBytes + (kS > 1 ? 0 : 32 * j * St::kRowBytes);
-                const bool edge = kTop && it * kKv + 32 * j + 32 > lim_min;
+                // (a step without a live row holds copies of one of the stage's other step, and that one some query may not see)
+                const bool edge = kTop && (it * kKv + 32 * j + 32 > lim_min || (kPaged && here == 0 && it * kKv + kKv > lim_min));
                 const Step now{it * kKv + 32 * j, here, edge, edge || (kPaged && !kSome && here != ~0u)};
                 if (rare(before.shown)) hide(j == 1 ? s[1] : s[0], before);
                 if constexpr (kTop) if (rare(old.edge)) take_out(old);
