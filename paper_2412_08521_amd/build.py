@@ -119,6 +119,69 @@ def _check_own_products(src: str, assembly: str) -> None:
         raise RuntimeError(f"{src}: no product in inline assembly found")
 
 
+# Kernels in which a wave fills a ring in LDS for itself, by DMA, with no barrier between what it has read there and what it fills
+# next: a read must have come to its registers before.  (Where a block's waves share a ring, a barrier lies between.)
+OWN_RINGS = {"prompt.hip": r"prompt_kernelILi\d+ELb[01]ELb[01]ELi1ELi1ELi(?!1E)\d+E"}
+
+
+def _blocks_of(assembly: str, names: str):
+    """Every kernel whose name matches `names` -> its name, its basic blocks (label, instructions) in their order."""
+    name, blocks = None, []
+    for line in assembly.splitlines():
+        text = line.split(";")[0].strip()
+        if name is None:
+            m = re.match(r"(\w+):", line)
+            if m and re.search(names, m.group(1)):
+                name, blocks = m.group(1), [("", [])]
+        elif text.startswith(".Lfunc_end"):
+            yield name, blocks
+            name = None
+        elif text.endswith(":"):
+            blocks.append((text[:-1], []))
+        elif text and not text.startswith((".", "#", "//")):
+            blocks[-1][1].append(text)
+
+
+def _check_reads_before_dma(src: str, assembly: str) -> None:
+    """Raise if on some way through one of the kernels of OWN_RINGS a DMA to LDS may be issued while a transposed read of it is under
+    way, or if there is no such kernel."""
+    done, kernels = 1 << 30, 0
+    for name, blocks in _blocks_of(assembly, OWN_RINGS[src]):
+        kernels += 1
+        number = {label: i for i, (label, _) in enumerate(blocks)}
+        at, todo = {0: done}, [0]                          # LDS accesses since the last such read, at a block's begin; done: it is there
+
+        def goes_on(block, since):
+            if since < at.get(block, done + 1):
+                at[block] = since
+                todo.append(block)
+
+        while todo:
+            i = todo.pop()
+            since, falls = at[i], i + 1 < len(blocks)
+            for text in blocks[i][1]:
+                op, _, rest = text.partition(" ")
+                if op.startswith("ds_read_b64_tr"):
+                    since = 0
+                elif op.startswith("ds_") and since < done:
+                    since += 1
+                elif op == "s_waitcnt":                    # (they come in their order)
+                    m = re.search(r"lgkmcnt\((\d+)\)", rest)
+                    if m and int(m.group(1)) <= since:
+                        since = done
+                elif op == "global_load_lds_dwordx4" and since < done:
+                    raise RuntimeError(f"{src}: {name} fills LDS (`{text}`) while a read of it may be under way")
+                elif op.startswith(("s_cbranch", "s_branch")):
+                    goes_on(number[rest.strip()], since)
+                if op in ("s_branch", "s_endpgm"):
+                    falls = False
+                    break
+            if falls:
+                goes_on(i + 1, since)
+    if not kernels:
+        raise RuntimeError(f"{src}: no kernel with rings of its waves' own found")
+
+
 def _stale(out: str, deps) -> bool:
     if not os.path.exists(out):
         return True
@@ -151,7 +214,9 @@ def build(force: bool = False, verbose: bool = False) -> str:
                     _check_no_scratch(src, err)
                 if src in OWN_PRODUCTS:
                     with open(obj.replace(".o", "-hip-amdgcn-amd-amdhsa-gfx950.s")) as f:
-                        _check_own_products(src, f.read())
+                        assembly = f.read()
+                    _check_own_products(src, assembly)
+                    _check_reads_before_dma(src, assembly)
             except RuntimeError:
                 os.remove(obj)
                 raise

@@ -162,6 +162,9 @@ __device__ __forceinline__ void dma4(const void* from, unsigned lds)
     asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(scalar((int)lds)) : "memory", "m0");
 }
 
+// What the wave has read from LDS is in its registers: DMA may write there.
+__device__ __forceinline__ void wait_lds_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
 // From global memory to LDS, a piece of 16 bytes a lane, from the wave's address on; wait_vmem counts it.
 __device__ __forceinline__ void dma16(const char* from, unsigned lds)
 {
@@ -885,6 +888,9 @@ __global__ __launch_bounds__(64 * kW * kS, D == 128 && kQ == 2 ? 1 : 2) void pro
 #pragma unroll
             for (int j = 1; j >= 0; --j) {
                 if constexpr (kS > 1) {
+                    // the values that the last turn read lay where the next ones go, and nothing has waited for them yet (the build
+                    // looks whether every way to these loads has)
+                    wait_lds_reads();
                     wait_vmem<0>();
                     vnext = vbuf == 2 ? 0 : vbuf + 1;
                     if (j == 1 || it > lo) {
