@@ -583,7 +583,7 @@ int ems_quant_append(const ems_paged_params* p, const ems_quant_cache* cache, in
  * The values that the cache stands for, of the first min(lens[b], n_rows) rows of every sequence, to k_out and v_out
  * [B, Hkv, n_rows, D] `dtype` with any strides (every row in a place of its own, apart from the cache).  A bf16 holds
  * them exactly (from 2^-126 up).  Rows whose page is outside the pool give zeros, masked rows what they hold; output
- * rows behind the length are left as they are.  n_rows >= 1, B * Hkv * n_rows < 2^31.
+ * rows behind the length are left as they are.  n_rows >= 1; B * Hkv * n_rows < 2^30, n_rows counted in whole 64s.
  */
 int ems_quant_read(const ems_paged_params* p, const ems_quant_cache* cache, int32_t n_rows, const int32_t* lens,
                     void* k_out, const ems_strides* k_out_strides,

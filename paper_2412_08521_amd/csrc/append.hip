@@ -307,7 +307,7 @@ __global__ __launch_bounds__(256) void read8_kernel(Read8Args a)
 
 hipError_t launch_read8(const Read8Args& a, int head_dim, hipStream_t st)
 {
-    const unsigned blocks = (unsigned)((long long)a.batch * a.kv_heads * ((a.n_rows + kRead8Rows - 1) / kRead8Rows));
+    const unsigned blocks = (unsigned)((long long)a.batch * a.kv_heads * ((a.n_rows + kRead8Rows - 1) / kRead8Rows));       // (the host holds n_rows to 30 bits)
     if (head_dim == 64) read8_kernel<64><<<blocks, 256, 0, st>>>(a);
     else read8_kernel<128><<<blocks, 256, 0, st>>>(a);
     return hipGetLastError();

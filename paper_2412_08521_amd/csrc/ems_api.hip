@@ -839,8 +839,7 @@ int ems_quant_read(const ems_paged_params* p, const ems_quant_cache* cache, int3
     if (!quant_cache_ok(cache)) return EMS_ERR_INVALID_ARG;
     const ems_paged_cache pages = pages_of(cache);
     if (!paged_cache_ok(&pages) || n_rows < 1 || !lens || !k_out || !k_out_strides || !v_out || !v_out_strides) return EMS_ERR_INVALID_ARG;
-    if ((long long)p->batch * n_rows > 0x7fffffffll / p->kv_heads) return EMS_ERR_UNSUPPORTED;
-    if ((long long)p->batch * p->kv_heads * ((n_rows + ems::kRead8Rows - 1) / ems::kRead8Rows) >= kMostBlocks) return EMS_ERR_UNSUPPORTED;
+    if ((long long)p->batch * p->kv_heads * (((long long)n_rows + ems::kRead8Rows - 1) / ems::kRead8Rows) >= kMostBlocks) return EMS_ERR_UNSUPPORTED;
     ems::Read8Args a{};
     a.k_pages = cache->k_pages; a.v_pages = cache->v_pages; a.k_scale = cache->k_scale; a.v_scale = cache->v_scale;
     a.page_table = cache->page_table; a.lens = lens;

@@ -258,3 +258,9 @@ def test_sizes_that_no_grid_holds_are_refused():
     assert _call_prompt(_prompt(k_rows=most + 1), ws=None) == UNSUPPORTED
     assert _call_chunk(_paged(), n_new=most, ws=None) == UNSUPPORTED
     assert _call_chunk(_paged(q_heads=200, kv_heads=2), n_new=most // 100 + 1, ws=None) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("rows", [(1 << 31) - 1, (1 << 31) - 63, (1 << 31) - 64, 1 << 30, (1 << 30) - 63])
+def test_reads_of_more_rows_than_a_grid_holds_are_refused(rows):
+    """One sequence and one head: nothing but the number of rows is too large (rounded up to blocks it passes 31 bits)."""
+    assert _call_read(_paged(batch=1, q_heads=1, kv_heads=1), rows=rows) == UNSUPPORTED
