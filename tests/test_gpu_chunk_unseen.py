@@ -96,3 +96,39 @@ def test_dead_halves_by_every_choice_of_blocks(f32, d, b, hq, hkv, n, m, choice)
         if all(at < x for x in lens):
             _case(n, lens, hq, hkv, d, F32 if f32 else BF16, lambda x: [last(x, at)],
                   lambda x: [s + t for s in range(0, x, 64) if s + 64 > x - n for t in range(at)], heads=sorted({0, hq // 2, hq - 1}))
+
+
+# ---- the newest rows are not finite: tokens before them are as they were
+
+def _last(count):
+    return lambda m: list(range(m - count, m))
+
+
+def _some(count, share):
+    """Rows apart from the last `count`, `share` of them."""
+    def rows(m):
+        gen = torch.Generator().manual_seed(m)
+        return (torch.rand(m - count, generator=gen) < share).nonzero()[:, 0].tolist()
+    return rows
+
+
+@pytest.mark.parametrize("mode", [BF16, F32])
+@pytest.mark.parametrize("share", [None, 0.0, 0.3, 0.9])               # of masked rows; None: a cache without positions
+@pytest.mark.parametrize("holds", HOLDS + [(None, -math.inf), (math.inf, None)])
+@pytest.mark.parametrize("hq,hkv,d,n,lens", [
+    (8, 2, 128, 4, [4, 70, 33, 5]), (4, 1, 64, 8, [64, 700]), (1, 1, 128, 32, [32, 33, 3000]), (2, 1, 64, 16, [16, 47, 128]),
+    (4, 4, 64, 5, [2001, 129, 17]), (20, 2, 128, 3, [131, 3]), (4, 2, 128, 2, [6000]), (3, 1, 64, 10, [48] * 70)])
+def test_few_columns_whose_newest_rows_are_not_finite(hq, hkv, d, n, lens, holds, share, mode):
+    _log("few columns", hq, hkv, d, n, lens, holds, share, mode)
+    count = min(3, n - 1)
+    _case(n, lens, hq, hkv, d, mode, _last(count), _some(count, share) if share else (), "table" if share is None else "positions", holds=holds)
+
+
+@pytest.mark.parametrize("share", [None, 0.0, 0.3, 0.9])
+@pytest.mark.parametrize("holds", HOLDS)
+@pytest.mark.parametrize("f32,d,b,hq,hkv,n,m,choice", CHUNK_CHOICES)
+def test_newest_rows_by_every_choice_of_blocks(f32, d, b, hq, hkv, n, m, choice, holds, share):
+    _log("newest rows", f32, d, b, hq, hkv, n, m, choice, holds, share)
+    lens = [max(n, m - 150 * i) for i in range(b)]
+    _case(n, lens, hq, hkv, d, F32 if f32 else BF16, _last(3), _some(3, share) if share else (), "table" if share is None else "positions",
+          holds=holds, heads=sorted({0, hq // 2, hq - 1}))
