@@ -522,10 +522,10 @@ int ems_paged_chunk_attention(const ems_paged_params* p, const ems_paged_cache* 
  *   k, v           in : device [B, Hkv, k_rows, D], or with q_start [Hkv, k_rows, D], any strides
  *   q_start_opt    in : device [B + 1] i32: sequence b's queries are rows q_start[b] .. q_start[b + 1] - 1 of q, or
  *                       NULL: all q_rows of batch entry b.  Rows before the first and behind the last one are
- *                       neither read nor written.
+ *                       neither read nor written.  Starts do not fall (sequences share no query).
  *   k_start_opt    in : device [B + 1] i32, the same for k and v; NULL iff q_start is
  *   lse_opt        out: device [B, Hq, q_rows] f32, with q_start [Hq, q_rows], or NULL
- *   ws             device scratch of at least ems_prompt_workspace_bytes
+ *   ws             device scratch of at least ems_prompt_workspace_bytes (of both forms the larger)
  * Starts are device data and cannot be checked on the host: they are clamped to [0, rows], an end to its start.
  */
 typedef struct {
@@ -582,8 +582,9 @@ int ems_quant_append(const ems_paged_params* p, const ems_quant_cache* cache, in
 /*
  * The values that the cache stands for, of the first min(lens[b], n_rows) rows of every sequence, to k_out and v_out
  * [B, Hkv, n_rows, D] `dtype` with any strides (every row in a place of its own, apart from the cache).  A bf16 holds
- * them exactly (from 2^-126 up).  Rows whose page is outside the pool give zeros, masked rows what they hold; output
- * rows behind the length are left as they are.  n_rows >= 1; B * Hkv * n_rows < 2^30, n_rows counted in whole 64s.
+ * them exactly (from 2^-126 up; elements from 1.9375 2^127 on round to 2^128, which is infinite there).  Rows whose
+ * page is outside the pool give zeros, masked rows what they hold (positions do not come along); output rows behind
+ * the length are left as they are.  n_rows >= 1; B * Hkv * n_rows < 2^30, n_rows counted in whole 64s.
  */
 int ems_quant_read(const ems_paged_params* p, const ems_quant_cache* cache, int32_t n_rows, const int32_t* lens,
                     void* k_out, const ems_strides* k_out_strides,

@@ -18,7 +18,7 @@
 //                     each in flight; 64 sequences of up to 32768 rows, 8 heads of 128 (4.5 GB): 677 us, 6.6 TB/s.
 //                     8-bit rows (C = uint8_t): the codes are widened with the row's power of two by the scaled conversion, which
 //                     is exact, in front of the same products; a step's rows are half the bytes.  The same ragged
-//                     sequences (2.2 GB): 371 us, 6.07 TB/s.
+//                     sequences (2.2 GB): 371 to 374 us, 6.05 TB/s.
 //                     Several new tokens (kMany): the columns are tokens x q-heads, 32 of them at most.  8 x 4 tokens behind up
 //                     to 8192 rows, 32/8 heads of 128: 44 us, and 78 by the kernel of prompts, whose tiles are 32 rows
 //                     of one sequence.

@@ -11,14 +11,16 @@
 // What bounds it.  A 32x32x16 product takes a SIMD 8 passes (32 clocks) and needs, at 32 query rows a wave, 1 KiB of LDS; a tile
 // of 32 x 32 weights takes three and a half instructions a weight (multiply-add, exponential, sum, half a conversion) beside D/4 products.  64
 // query rows a wave halve the reads of LDS, and with products of one step beside the weights of another the matrix units
-// are what is left: 32 q-heads on 8, D = 128, a prompt of 32768 tokens takes 7.1 ms (1.24 PFLOP/s; a plain product of matrices
-// reaches 1.37 at its best size on the same card).  With one step at a time and one register tile it took 22.0 ms, with three in
-// flight 7.8 ms, with fewer instructions for addresses and edges 7.2 ms.  The same without the weights' instructions would run at
+// are what is left: 32 q-heads on 8, D = 128, a prompt of 32768 tokens takes 7.1 to 7.4 ms from card to card (1.24 to 1.19 PFLOP/s; a
+// plain product of matrices reaches 1.37 at its best size).  With one step at a time and one register tile it took 22.0 ms, with three
+// in flight 7.8 ms, with fewer instructions for addresses and edges 7.2 ms.  The same without the weights' instructions would run at
 // 1.47 PFLOP/s, without the loads of stages at 1.36; tiles drawn from a counter at run time gained 1.5 % at that size and lost 1 %
-// at 1024 tokens, so a block has one tile.
+// at 1024 tokens, so a block has one tile.  (All of these with the wait that the compiler places in a stage, see below.)  At D = 64
+// a tile of 32 x 32 weights is 256 clocks of products and, counted, some 400 of weights' instructions (an exponential as four).
 //
 // The weights are rounded to bfloat16 for the second product (relative 2^-8 each, as the values and the output are); their sum is
-// of the 32-bit ones.
+// of the 32-bit ones.  Beside the output's own rounding (0.0017 of it, root mean square) that leaves 0.0019 to 0.0024; whole weights
+// would be three products for one, as few columns over pages have them, which memory bounds.
 #include <cmath>
 
 #include "ems_common.h"
@@ -370,7 +372,7 @@ __global__ __launch_bounds__(128, 2) void prompt_f32_kernel(PromptArgs a)
         }
     };
 
-    // Stages come last rows first.  One is in flight while one is worked on; rows of pages are looked up two further on.
+    // Stages come last rows first.  One is in flight while one is worked on; rows of pages are looked up two further on, a stage a turn.
     int entry = kNoRow, far = kNoRow, far_mask = 0;
     if constexpr (kPaged) {
         if (wave == 0 && hi > lo) {
@@ -491,7 +493,8 @@ __global__ __launch_bounds__(64 * kW * kS, D == 128 && kQ == 2 ? 1 : 2) void pro
 
     // ---- rows of a stage, found four stages at a time: a batch's stages are the waves', one after the other.  The trips of the
     // batch below are made while one is worked on (the table; positions; then its rows are settled), from memory to LDS, so that
-    // no register waits for them: the loads of the stages are in flight behind them.
+    // no register waits for them: the loads of the stages are in flight behind them.  (Not so where waves share a tile: there
+    // the first step after a trip waits for it before it asks for the next rows, in one stage of four, in two with positions.)
     constexpr int kMine = kBatch / kW;
     static_assert(kBatch % kW == 0, "every wave has as many");
     const auto page_of = [&](int t) __attribute__((always_inline)) { return (int)(__umulhi(2u * (unsigned)t, a.page_magic) >> a.page_shift); };
@@ -839,7 +842,12 @@ __global__ __launch_bounds__(64 * kW * kS, D == 128 && kQ == 2 ? 1 : 2) void pro
         for (int c = 0; c < kQ; ++c) l[c] += sum[c];
     };
 
-    // Stages come last rows first.  One is in flight while one is worked on; rows of pages are looked up two further on.
+    // Stages come last rows first.  One is in flight while one is worked on; rows of pages are found four stages at a time.
+    //
+    // The compiler does not see that wait_vmem ends the queries' loads.  It takes them for under way on every turn and waits for all
+    // loads before the first product of a stage that reads them: the keys that the stage has asked for at its begin have the time
+    // of one turn's products of weights and values; the values, asked for in its second turn, have until the next stage.  (Where waves
+    // share a tile, the keys and values of every next step.)
     const int first_batch = (hi - 1) / kBatch;
     if constexpr (kPaged) {
         if (hi > lo) {
